@@ -53,8 +53,9 @@ enum {
 };
 
 /* Element type of the input tensor and of the packed weights.  The output is
- * always fp32 and accumulation is always fp32. */
-enum { GSPC_F32 = 0, GSPC_BF16 = 1 };
+ * always fp32 and accumulation is always fp32.  (GSPC_I8, 8-bit rows: channels-last
+ * operators only, see there.) */
+enum { GSPC_F32 = 0, GSPC_BF16 = 1, GSPC_I8 = 2 };
 
 /* Kernel families (for gspc_force_path / gspc_last_path). */
 enum { GSPC_PATH_AUTO = -1, GSPC_PATH_DIRECT = 0, GSPC_PATH_MFMA = 1 };
@@ -152,7 +153,8 @@ int gspc_conv2d_grouped(const void *input, const gspc_packed_t *packed_weight,
  * forced family that cannot run a given layer yields GSPC_ERR_ARG. */
 int gspc_force_path(int path);
 
-/* Family used by this thread's most recent convolution, and its kernel's name. */
+/* Family used by this thread's most recent convolution, and the name of its kernel (or of the kernel that wrote the outputs of
+ * a channels-last operator called since). */
 int gspc_last_path(void);
 const char *gspc_last_kernel(void);
 
@@ -225,6 +227,76 @@ int gspc_set_winograd(int on);
 int gspc_run_layer_chain(const gspc_layer_t *layers, int n_layers,
                          void *const *act_bufs, const size_t *act_bytes,
                          int n_bufs, float *per_layer_ms);
+
+/* ---- channels-last operators ------------------------------------------------
+ *
+ * What stands between the convolutions of a network, and the pointwise layers behind
+ * them, on tokens: the pixels of an image, each with its C channels side by side.
+ *
+ *   dense rows  fp32 or bf16, token t at element t * ld, ld >= the number of channels:
+ *               a tensor of its own (ld = C) or some channels of a wider one.  Pointers
+ *               need only the alignment of their element.
+ *   8-bit rows  (GSPC_I8) int8 values [rows][pitch], pitch = gspc_rows8_pitch(cols) (cols
+ *               rounded up to 16), ZERO past the last column, 16-byte aligned, and one
+ *               fp32 scale per row: a row's values are q * scale.
+ *
+ * Tensors may have 2^31 and more elements; rows (N * P, M) are below 2^31 in number.
+ * Zero images, pixels, rows or tokens are no work (pointers may then be NULL) and no error.
+ * Sums are fp32 (products of 8-bit rows: exact integers) and every result is rounded
+ * once.  No atomics: the same call gives the same bits. */
+
+/* Bytes of one 8-bit row of cols values.  0 if cols is not positive or too large. */
+int gspc_rows8_pitch(int cols);
+
+/* out[n][p][c] = in[n][c][p]: the planes a convolution leaves as tokens (P = H * W), fp32 or
+ * bf16 on either side; and back.  Both tensors contiguous. */
+int gspc_pack_channels_last(const void *in, int in_dtype, int N, int C, int P, void *out, int out_dtype);
+int gspc_unpack_channels_last(const void *in, int in_dtype, int N, int C, int P, void *out, int out_dtype);
+
+/* Writes dense rows as 8-bit rows: q = rint(x * (127 / a)), ties to even, scale = a / 127, a the
+ * largest |x| of the row (rows below 2^-64 with x and a multiplied by 2^64 first); a row of zeros has scale 0.  A
+ * row with an infinity or NaN has the scale NaN and zeros: all of it reads back as NaN.
+ * Weights [Cout][Cin] become the second operand of gspc_matmul_i8 by the same call. */
+int gspc_quantize_rows(const void *x, int dtype, int64_t ldx, int64_t rows, int cols, void *q, float *scale);
+/* Reads them back: x = q * scale. */
+int gspc_dequantize_rows(const void *q, const float *scale, int64_t rows, int cols, void *x, int dtype, int64_t ldx);
+
+/* Activation of a group norm.  SILU is z / (1 + exp(-z)). */
+enum { GSPC_ACT_NONE = 0, GSPC_ACT_RELU = 1, GSPC_ACT_SILU = 2 };
+
+/* Device memory that the two calls below need while they run, on any stream.  0 on
+ * invalid arguments, and where there is no work. */
+size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int backward);
+
+/* y = act(gamma * (x - mean) / sqrt(var + eps) + beta) over N images of P tokens of C channels; mean and (biased) variance
+ * are those of the P * C / groups values of a group of one image.
+ *   gamma, beta : dev fp32 [C], or NULL for 1 and 0
+ *   y           : dense rows, fp32 or bf16 (y_dtype, ldy), or 8-bit rows (GSPC_I8; ldy ignored) with y_scale
+ *   stats       : dev fp32 [N][groups][2], receives mean and 1 / sqrt(var + eps) for the gradient, or NULL
+ *   saved       : receives x as 8-bit rows, with saved_scale, in the same pass: what a training step keeps
+ *                 of x for the gradient; or NULL
+ *   workspace   : dev, 16-byte aligned, at least gspc_group_norm_workspace_bytes(..., 0); not initialised */
+int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma, const float *beta, int N, int P, int C,
+                    int groups, float eps, int act, void *y, int y_dtype, int64_t ldy, float *y_scale, float *stats,
+                    void *saved, float *saved_scale, void *workspace, size_t workspace_bytes);
+
+/* Its gradient.  With xh = (x - mean) * rstd and dz = dy * act'(gamma * xh + beta) (ReLU's slope at 0 is 0):
+ *   dbeta = sum dz, dgamma = sum dz * xh (over images and tokens), dx = rstd * (gamma * dz - (A + xh * B) / m), A and B
+ * the sums of gamma * dz and gamma * dz * xh over the m values of the group.
+ *   x     : what the forward call had, or what it saved of it (GSPC_I8 with x_scale; ldx ignored)
+ *   stats : from the forward call
+ *   dx    : type of dy; dgamma, dbeta: dev fp32 [C], overwritten (zeros where there are no tokens), or NULL */
+int gspc_group_norm_backward(const void *dy, int dy_dtype, int64_t lddy, const void *x, int x_dtype, int64_t ldx,
+                             const float *x_scale, const float *stats, const float *gamma, const float *beta, int N, int P,
+                             int C, int groups, int act, void *dx, int64_t lddx, float *dgamma, float *dbeta,
+                             void *workspace, size_t workspace_bytes);
+
+/* out[m][n] = a_scale[m] * w_scale[n] * sum over k < K of a[m][k] * w[n][k] (+ bias[n]): a pointwise layer (or a
+ * classifier) on 8-bit rows, M tokens of K channels, N filters.  The integer sums are exact, so K is at most 133144.
+ *   bias : dev fp32 [N], or NULL
+ *   out  : dense rows, fp32 or bf16 (out_dtype, ldo) */
+int gspc_matmul_i8(const void *a, const float *a_scale, const void *w, const float *w_scale, const float *bias, int64_t M,
+                   int N, int K, void *out, int out_dtype, int64_t ldo);
 
 #ifdef __cplusplus
 }

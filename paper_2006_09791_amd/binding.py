@@ -8,14 +8,16 @@ fallback: if the library is missing or a call fails, an exception is raised.
 """
 import ctypes
 import os
+import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libgspc.so")
 
-GSPC_F32, GSPC_BF16 = 0, 1
+GSPC_F32, GSPC_BF16, GSPC_I8 = 0, 1, 2
 PATH_AUTO, PATH_DIRECT, PATH_MFMA = -1, 0, 1
 OP_CONV, OP_MAXPOOL, OP_ADD, OP_RELU = 0, 1, 2, 3
 FLAG_RELU = 1
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 
 ERROR_NAMES = {0: "GSPC_OK", -1: "GSPC_ERR_NULL", -2: "GSPC_ERR_DIM", -3: "GSPC_ERR_GROUPS",
                -4: "GSPC_ERR_DTYPE", -5: "GSPC_ERR_MISMATCH", -6: "GSPC_ERR_SPACE",
@@ -26,6 +28,8 @@ EXPORTS = [
     "gspc_packed_weight_bytes", "gspc_pack_weights", "gspc_unpack_weights", "gspc_packed_free",
     "gspc_packed_info", "gspc_pack_input_bf16", "gspc_conv2d_grouped", "gspc_force_path",
     "gspc_last_path", "gspc_last_kernel", "gspc_set_graph_mode", "gspc_set_chain_fusion", "gspc_set_winograd", "gspc_run_layer_chain",
+    "gspc_rows8_pitch", "gspc_pack_channels_last", "gspc_unpack_channels_last", "gspc_quantize_rows", "gspc_dequantize_rows",
+    "gspc_group_norm_workspace_bytes", "gspc_group_norm", "gspc_group_norm_backward", "gspc_matmul_i8",
 ]
 
 
@@ -44,6 +48,7 @@ class GspcLayer(ctypes.Structure):
                 ("w", ctypes.c_void_p)]
 
 
+_thread = threading.local()     # stream: the library's, as gspc_set_stream was last given it
 _lib = None
 _conv = None     # gspc_conv2d_grouped through _gspc_call, or _no_conv
 
@@ -103,6 +108,23 @@ def load():
     lib.gspc_run_layer_chain.restype = i
     lib.gspc_run_layer_chain.argtypes = [ctypes.POINTER(GspcLayer), i, ctypes.POINTER(vp),
                                          ctypes.POINTER(sz), i, ctypes.POINTER(ctypes.c_float)]
+    ll, f = ctypes.c_int64, ctypes.c_float
+    lib.gspc_rows8_pitch.restype = i
+    lib.gspc_rows8_pitch.argtypes = [i]
+    lib.gspc_pack_channels_last.restype = lib.gspc_unpack_channels_last.restype = i
+    lib.gspc_pack_channels_last.argtypes = lib.gspc_unpack_channels_last.argtypes = [vp] + [i] * 4 + [vp, i]
+    lib.gspc_quantize_rows.restype = i
+    lib.gspc_quantize_rows.argtypes = [vp, i, ll, ll, i, vp, vp]
+    lib.gspc_dequantize_rows.restype = i
+    lib.gspc_dequantize_rows.argtypes = [vp, vp, ll, i, vp, i, ll]
+    lib.gspc_group_norm_workspace_bytes.restype = sz
+    lib.gspc_group_norm_workspace_bytes.argtypes = [i] * 5
+    lib.gspc_group_norm.restype = i
+    lib.gspc_group_norm.argtypes = [vp, i, ll, vp, vp, i, i, i, i, f, i, vp, i, ll, vp, vp, vp, vp, vp, sz]
+    lib.gspc_group_norm_backward.restype = i
+    lib.gspc_group_norm_backward.argtypes = [vp, i, ll, vp, i, ll, vp, vp, vp, vp, i, i, i, i, i, vp, ll, vp, vp, vp, sz]
+    lib.gspc_matmul_i8.restype = i
+    lib.gspc_matmul_i8.argtypes = [vp, vp, vp, vp, vp, ll, i, i, vp, i, ll]
     try:
         from . import _gspc_call
     except ImportError:          # not built for this interpreter
@@ -138,6 +160,7 @@ def gspc_set_stream(stream=None):
         stream = torch.cuda.current_stream()
     handle = getattr(stream, "cuda_stream", stream)
     _check(load().gspc_set_stream(ctypes.c_void_p(handle)))
+    _thread.stream = handle or 0
 
 
 def gspc_output_dims(H, W, KH, KW, stride, pad):
@@ -284,3 +307,239 @@ def gspc_run_layer_chain(lc, per_layer_ms=False):
     ms = (ctypes.c_float * lc.n_layers)() if per_layer_ms else None
     _check(load().gspc_run_layer_chain(lc.layers, lc.n_layers, lc.bufs, lc.bytes, lc.n_bufs, ms))
     return list(ms) if per_layer_ms else None
+
+
+# ---- channels-last operators -------------------------------------------------------------------
+# Tokens are torch tensors [..., channels] whose rows are a fixed distance apart (a contiguous tensor, or a slice of the
+# channels of one); 8-bit rows are a pair (int8 tensor [rows, pitch], fp32 scales [rows]).
+
+def _empty(shape, dtype, device):
+    """A tensor for the library's stream: torch reuses its memory after work of that stream only."""
+    import torch
+    stream = getattr(_thread, "stream", 0)
+    if stream == torch.cuda.current_stream(device).cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _dtypes():
+    import torch
+    return {torch.float32: GSPC_F32, torch.bfloat16: GSPC_BF16}
+
+
+def _dtype(t, what):
+    kind = _dtypes().get(t.dtype)
+    if kind is None:
+        raise GspcError(-4, f"{what}: {t.dtype} is neither float32 nor bfloat16")
+    return kind
+
+
+def _torch_dtype(dtype):
+    for t, kind in _dtypes().items():
+        if kind == dtype:
+            return t
+    raise GspcError(-4, f"unknown dtype {dtype}")
+
+
+def _on_gpu(t, what):
+    if not t.is_cuda:
+        raise GspcError(-8, f"{what} is not on the GPU")
+    return t
+
+
+def _row_stride(t, what):
+    """Elements between two rows of t's last dimension."""
+    _on_gpu(t, what)
+    if t.is_contiguous():
+        return t.shape[-1]
+    shape, stride = t.shape, t.stride()
+    if len(shape) < 2 or (stride[-1] != 1 and shape[-1] > 1):
+        raise GspcError(-8, f"{what}: channels must be side by side")
+    ld, step = None, None
+    for k in range(len(shape) - 2, -1, -1):
+        if shape[k] == 1:
+            continue
+        if ld is None:
+            ld = step = stride[k]
+        if stride[k] != step:
+            raise GspcError(-8, f"{what}: rows must be a fixed distance apart")
+        step *= shape[k]
+    return shape[-1] if ld is None else ld
+
+
+def _flat(t, dtype, count, what):
+    """A contiguous tensor of that type and number of elements, or None."""
+    if t is None:
+        return None
+    _on_gpu(t, what)
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise GspcError(-8, f"{what}: a contiguous {dtype} tensor of {count} elements is needed")
+    return t.data_ptr()
+
+
+def _rows8(pair, rows, cols, what):
+    import torch
+    q, scale = pair
+    return (_flat(q, torch.int8, rows * gspc_rows8_pitch(cols), what), _flat(scale, torch.float32, rows, what + " scales"))
+
+
+def _same_shape(t, shape, what):
+    if tuple(t.shape) != tuple(shape):
+        raise GspcError(-2, f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def gspc_rows8_pitch(cols):
+    if cols <= 0 or cols > 0x7ffffff0:
+        raise GspcError(-2, f"{cols} columns")
+    return (cols + 15) // 16 * 16
+
+
+def _new_rows8(rows, cols, device):
+    import torch
+    return (_empty((rows, gspc_rows8_pitch(cols)), torch.int8, device), _empty((rows,), torch.float32, device))
+
+
+def _change_layout(call, x, out, dtype, pack):
+    _on_gpu(x, "x")
+    if x.dim() < 3 or not x.is_contiguous():
+        raise GspcError(-8, "x: a contiguous tensor of images, channels and pixels is needed")
+    N = x.shape[0]
+    C = x.shape[1] if pack else x.shape[-1]
+    P = 1
+    for n in x.shape[2:] if pack else x.shape[1:-1]:
+        P *= n
+    shape = (N, P, C) if pack else (N, C, P)
+    if out is None:
+        out = _empty(shape, _torch_dtype(dtype), x.device)
+    elif out.numel() != x.numel() or not _on_gpu(out, "out").is_contiguous():
+        raise GspcError(-8, f"out: a contiguous tensor of {x.numel()} elements is needed")
+    _check(call(x.data_ptr(), _dtype(x, "x"), N, C, P, out.data_ptr(), _dtype(out, "out")))
+    return out
+
+
+def gspc_pack_channels_last(x, out=None, dtype=GSPC_BF16):
+    """x [N, C, ...] (planes) -> [N, P, C] (tokens), P the pixels of a plane."""
+    return _change_layout(load().gspc_pack_channels_last, x, out, dtype, True)
+
+
+def gspc_unpack_channels_last(x, out=None, dtype=GSPC_F32):
+    """x [N, ..., C] (tokens) -> [N, C, P] (planes)."""
+    return _change_layout(load().gspc_unpack_channels_last, x, out, dtype, False)
+
+
+def gspc_quantize_rows(x, out=None):
+    """x [..., cols] -> 8-bit rows (q [rows, pitch], scale [rows]); `out`: such a pair to write into."""
+    lib = load()
+    ld, cols = _row_stride(x, "x"), x.shape[-1]
+    if cols == 0:
+        raise GspcError(-2, "x has no columns")
+    rows = x.numel() // cols
+    if out is None:
+        out = _new_rows8(rows, cols, x.device)
+    q, scale = _rows8(out, rows, cols, "out")
+    _check(lib.gspc_quantize_rows(x.data_ptr(), _dtype(x, "x"), ld, rows, cols, q, scale))
+    return out
+
+
+def gspc_dequantize_rows(rows8, cols, out=None, dtype=GSPC_F32):
+    """8-bit rows of `cols` values -> [rows, cols]; `out`: a tensor [..., cols] to write into."""
+    lib = load()
+    rows = rows8[1].numel()
+    q, scale = _rows8(rows8, rows, cols, "rows8")
+    if out is None:
+        out = _empty((rows, cols), _torch_dtype(dtype), rows8[0].device)
+    elif out.shape[-1] != cols or out.numel() != rows * cols:
+        raise GspcError(-2, f"out has shape {tuple(out.shape)}, expected {rows} rows of {cols}")
+    _check(lib.gspc_dequantize_rows(q, scale, rows, cols, out.data_ptr(), _dtype(out, "out"), _row_stride(out, "out")))
+    return out
+
+
+def gspc_group_norm_workspace_bytes(N, P, C, groups, backward=False):
+    return int(load().gspc_group_norm_workspace_bytes(N, P, C, groups, 1 if backward else 0))
+
+
+def _tokens(x, what):
+    if x.dim() < 3:
+        raise GspcError(-2, f"{what}: [images, pixels, channels] is needed")
+    N, C, P = x.shape[0], x.shape[-1], 1
+    for n in x.shape[1:-1]:
+        P *= n
+    return N, P, C
+
+
+def _workspace(workspace, N, P, C, groups, backward, device):
+    import torch
+    if workspace is None:
+        workspace = _empty((gspc_group_norm_workspace_bytes(N, P, C, groups, backward),), torch.uint8, device)
+    _on_gpu(workspace, "workspace")
+    if not workspace.is_contiguous():
+        raise GspcError(-8, "workspace must be contiguous")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def gspc_group_norm(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, out=None, dtype=None, stats=None, saved=None, workspace=None):
+    """x [N, ..., C] -> y of x's shape (type: `dtype`, by default x's), or 8-bit rows of it where `dtype` is GSPC_I8 or `out` is
+    a pair.  stats: fp32 [N, groups, 2] to write mean and 1 / sqrt(var + eps) to; saved: 8-bit rows to write x to."""
+    import torch
+    lib = load()
+    N, P, C = _tokens(x, "x")
+    if out is None:
+        out = _new_rows8(N * P, C, x.device) if dtype == GSPC_I8 else _empty(x.shape, x.dtype if dtype is None else _torch_dtype(dtype), x.device)
+    if isinstance(out, tuple):
+        (y, y_scale), kind, ldy = _rows8(out, N * P, C, "out"), GSPC_I8, 0
+    else:
+        _same_shape(out, x.shape, "out")
+        y, y_scale, kind, ldy = out.data_ptr(), None, _dtype(out, "out"), _row_stride(out, "out")
+    q, scale = (None, None) if saved is None else _rows8(saved, N * P, C, "saved")
+    ws, ws_bytes = _workspace(workspace, N, P, C, groups, False, x.device)
+    _check(lib.gspc_group_norm(x.data_ptr(), _dtype(x, "x"), _row_stride(x, "x"), _flat(gamma, torch.float32, C, "gamma"),
+                               _flat(beta, torch.float32, C, "beta"), N, P, C, groups, eps, act, y, kind, ldy, y_scale,
+                               _flat(stats, torch.float32, N * groups * 2, "stats"), q, scale, ws.data_ptr(), ws_bytes))
+    return out
+
+
+def gspc_group_norm_backward(dy, x, stats, gamma, beta, groups, act=ACT_NONE, dx=None, dgamma=None, dbeta=None, workspace=None):
+    """dy [N, ..., C], x of its shape or 8-bit rows of it -> (dx, dgamma, dbeta), dx of dy's type."""
+    import torch
+    lib = load()
+    N, P, C = _tokens(dy, "dy")
+    if isinstance(x, tuple):
+        (px, x_scale), kind, ldx = _rows8(x, N * P, C, "x"), GSPC_I8, 0
+    else:
+        _same_shape(x, dy.shape, "x")
+        px, x_scale, kind, ldx = x.data_ptr(), None, _dtype(x, "x"), _row_stride(x, "x")
+    if dx is None:
+        dx = _empty(dy.shape, dy.dtype, dy.device)
+    _same_shape(dx, dy.shape, "dx")
+    if dx.dtype != dy.dtype:
+        raise GspcError(-4, f"dx is {dx.dtype}, dy {dy.dtype}")
+    if dgamma is None:
+        dgamma = _empty((C,), torch.float32, dy.device)
+    if dbeta is None:
+        dbeta = _empty((C,), torch.float32, dy.device)
+    ws, ws_bytes = _workspace(workspace, N, P, C, groups, True, dy.device)
+    _check(lib.gspc_group_norm_backward(dy.data_ptr(), _dtype(dy, "dy"), _row_stride(dy, "dy"), px, kind, ldx, x_scale,
+                                        _flat(stats, torch.float32, N * groups * 2, "stats"), _flat(gamma, torch.float32, C, "gamma"),
+                                        _flat(beta, torch.float32, C, "beta"), N, P, C, groups, act, dx.data_ptr(), _row_stride(dx, "dx"),
+                                        _flat(dgamma, torch.float32, C, "dgamma"), _flat(dbeta, torch.float32, C, "dbeta"),
+                                        ws.data_ptr(), ws_bytes))
+    return dx, dgamma, dbeta
+
+
+def gspc_matmul_i8(a, w, bias=None, out=None, dtype=GSPC_BF16):
+    """8-bit rows a (M tokens) and w (N filters) of the same length -> [M, N]; `out`: a tensor [..., N] to write into."""
+    import torch
+    lib = load()
+    K, M, N = a[0].shape[-1], a[1].numel(), w[1].numel()
+    if w[0].shape[-1] != K:
+        raise GspcError(-5, f"tokens of {K} values, filters of {w[0].shape[-1]}")
+    qa, sa = _rows8(a, M, K, "a")
+    qw, sw = _rows8(w, N, K, "w")
+    if out is None:
+        out = _empty((M, N), _torch_dtype(dtype), a[0].device)
+    elif out.shape[-1] != N or out.numel() != M * N:
+        raise GspcError(-2, f"out has shape {tuple(out.shape)}, expected {M} rows of {N}")
+    _check(lib.gspc_matmul_i8(qa, sa, qw, sw, _flat(bias, torch.float32, N, "bias"), M, N, K, out.data_ptr(), _dtype(out, "out"),
+                              _row_stride(out, "out")))
+    return out

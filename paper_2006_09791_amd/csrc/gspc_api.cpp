@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "gspc_internal.h"
+#include "tokens_internal.h"
 
 namespace {
 
@@ -64,13 +65,7 @@ uint64_t chain_key(const gspc_layer_t *layers, int n_layers, void *const *bufs, 
     return h;
 }
 
-int fail(int code, const char *fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(t_error, sizeof(t_error), fmt, ap);
-    va_end(ap);
-    return code;
-}
+using gspc::fail;
 
 int hip_fail(hipError_t e, const char *what) {
     return fail(GSPC_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -374,6 +369,22 @@ PackGeom merged_geom(const PackGeom &g, int which, int KH, int KW) {
     v.direct_bytes = d.bytes;
     return v;
 }
+
+}  // namespace gspc
+
+namespace gspc {
+
+hipStream_t current_stream() { return t_stream; }
+
+int fail(int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(t_error, sizeof(t_error), fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+void set_last_kernel(const char *name) { t_last_kernel = name; }
 
 }  // namespace gspc
 

@@ -1,0 +1,75 @@
+// NCHW planes to channels-last tokens and back: the transpose of [R][S] to [S][R] in every image, with a change of type.
+#include "tokens.h"
+#include "tokens_internal.h"
+
+namespace gspc {
+
+constexpr int kTile = 64, kTilePitch = kTile + 1;
+
+// One block transposes a 64 x 64 tile through LDS in fp32; the last tiles of a row or column are moved back so that they end
+// with it (what they share with their neighbours is written twice, the same), so that only planes smaller than a tile have
+// lanes without work.  VI, VO: elements per access along S and along R: 8, or 1 where that side has fewer than 8.
+// The pitch of 65 words puts the 64 words that a wave writes (8 rows x 8 vectors, one element of each) and reads (the same
+// the other way) into 64 banks.  Bound by memory: each element is read and written once.
+template <typename TI, typename TO, int VI, int VO>
+__global__ __launch_bounds__(256) void transpose_kernel(const TI *__restrict__ in, TO *__restrict__ out, int R, int S, unsigned rtiles,
+                                                       unsigned tiles, unsigned m_rtiles, unsigned m_tiles) {
+    __shared__ float lds[kTile * kTilePitch];
+    const unsigned n = fast_div_any(blockIdx.x, tiles, m_tiles), t = blockIdx.x - n * tiles;
+    const unsigned st = fast_div_any(t, rtiles, m_rtiles), rt = t - st * rtiles;
+    const int wr = min(R, kTile), ws = min(S, kTile);
+    const int r0 = min((int)rt * kTile, R - wr), s0 = min((int)st * kTile, S - ws);
+    const TI *ip = in + (size_t)n * R * S + (size_t)r0 * S + s0;
+    TO *op = out + (size_t)n * R * S + (size_t)s0 * R + r0;
+    Raw<TI, VI> raw[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = k * 256 + threadIdx.x, r = i >> 3, at = vector_start<VI>(i & 7, ws);
+        if (r < wr && (i & 7) < vectors_of<VI>(ws)) raw[k] = fetch<VI>(ip + (size_t)r * S + at);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = k * 256 + threadIdx.x, r = i >> 3, at = vector_start<VI>(i & 7, ws);
+        if (r < wr && (i & 7) < vectors_of<VI>(ws)) {
+            float v[VI];
+            widen(raw[k], v);
+#pragma unroll
+            for (int e = 0; e < VI; ++e) lds[(at + e) * kTilePitch + r] = v[e];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = k * 256 + threadIdx.x, s = i >> 3, at = vector_start<VO>(i & 7, wr);
+        if (s < ws && (i & 7) < vectors_of<VO>(wr)) {
+            float v[VO];
+#pragma unroll
+            for (int e = 0; e < VO; ++e) v[e] = lds[s * kTilePitch + at + e];
+            store(op + (size_t)s * R + at, v);
+        }
+    }
+}
+
+template <typename TI, typename TO>
+static hipError_t transpose(const void *in, int N, int R, int S, void *out, hipStream_t s) {
+    const unsigned rt = (R + kTile - 1) / kTile, st = (S + kTile - 1) / kTile;
+    const unsigned long long tiles = (unsigned long long)rt * st;
+    const auto kern = R >= 8 ? (S >= 8 ? transpose_kernel<TI, TO, 8, 8> : transpose_kernel<TI, TO, 1, 8>)
+                             : (S >= 8 ? transpose_kernel<TI, TO, 8, 1> : transpose_kernel<TI, TO, 1, 1>);
+    // images of one launch: blocks are numbered in 31 bits
+    const int step = (int)(tiles * N < 0x7fffffffull ? N : 0x7fffffffull / tiles);
+    for (int n = 0; n < N; n += step) {
+        const int count = N - n < step ? N - n : step;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * count)), dim3(256), 0, s, static_cast<const TI *>(in) + (size_t)n * R * S,
+                           static_cast<TO *>(out) + (size_t)n * R * S, R, S, rt, (unsigned)tiles, div_magic(rt), div_magic((unsigned)tiles));
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_transpose(const void *in, int in_dtype, int N, int R, int S, void *out, int out_dtype, hipStream_t s) {
+    if (in_dtype == GSPC_F32)
+        return out_dtype == GSPC_F32 ? transpose<float, float>(in, N, R, S, out, s) : transpose<float, uint16_t>(in, N, R, S, out, s);
+    return out_dtype == GSPC_F32 ? transpose<uint16_t, float>(in, N, R, S, out, s) : transpose<uint16_t, uint16_t>(in, N, R, S, out, s);
+}
+
+}  // namespace gspc

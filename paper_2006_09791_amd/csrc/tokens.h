@@ -1,0 +1,167 @@
+// Device helpers of the channels-last operators: eight consecutive channels of one token at a time, whatever their type.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "divide.h"
+
+namespace gspc {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+// Rows of any stride start at any multiple of their element's size: vector accesses that ask for no more than that.  (The
+// hardware takes them; a 16-byte access that straddles two cache lines costs a second one.)
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef u32x2 __attribute__((aligned(1))) u32x2_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
+constexpr int kWave = 64;
+
+__device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {   // to nearest, ties to even; NaN stays one
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, (bf16x2){(__bf16)lo, (__bf16)hi});
+}
+__device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// Storage types: float, uint16_t (bf16) and int8_t (the values of 8-bit rows, without their scale).
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(uint16_t v) { return __uint_as_float((unsigned)v << 16); }
+__device__ __forceinline__ float as_float(int8_t v) { return (float)v; }
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t *p, float v) { *p = to_bf16(v); }
+
+// V = 8: a vector; V = 1: a single element (rows of fewer than eight channels).
+struct Raw32 { f32x4 a, b; };
+struct Raw16 { u32x4 a; };
+struct Raw8 { u32x2 a; };
+template <typename T, int V> struct RawOf { typedef T type; };
+template <> struct RawOf<float, 8> { typedef Raw32 type; };
+template <> struct RawOf<uint16_t, 8> { typedef Raw16 type; };
+template <> struct RawOf<int8_t, 8> { typedef Raw8 type; };
+template <typename T, int V> using Raw = typename RawOf<T, V>::type;
+
+// Loads stay raw until they are used, so that several can be in flight.
+template <int V> __device__ __forceinline__ Raw<float, V> fetch(const float *p) {
+    if constexpr (V == 1) return *p;
+    else return {*reinterpret_cast<const f32x4_any *>(p), *reinterpret_cast<const f32x4_any *>(p + 4)};
+}
+template <int V> __device__ __forceinline__ Raw<uint16_t, V> fetch(const uint16_t *p) {
+    if constexpr (V == 1) return *p;
+    else return {*reinterpret_cast<const u32x4_any *>(p)};
+}
+template <int V> __device__ __forceinline__ Raw<int8_t, V> fetch(const int8_t *p) {
+    if constexpr (V == 1) return *p;
+    else return {*reinterpret_cast<const u32x2_any *>(p)};
+}
+__device__ __forceinline__ void widen(const Raw32 &r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = r.a[e], v[4 + e] = r.b[e];
+}
+__device__ __forceinline__ void widen(const Raw16 &r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(r.a[e] << 16), v[2 * e + 1] = __uint_as_float(r.a[e] & 0xffff0000u);
+}
+__device__ __forceinline__ void widen(const Raw8 &r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(r.a[e / 4] >> (e % 4 * 8));
+}
+template <typename T> __device__ __forceinline__ void widen(const T &r, float (&v)[1]) { v[0] = as_float(r); }
+
+__device__ __forceinline__ void store(float *p, const float (&v)[8]) {
+    *reinterpret_cast<f32x4_any *>(p) = (f32x4){v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_any *>(p + 4) = (f32x4){v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store(uint16_t *p, const float (&v)[8]) {
+    *reinterpret_cast<u32x4_any *>(p) = (u32x4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+}
+template <typename T> __device__ __forceinline__ void store(T *p, const float (&v)[1]) { put(p, v[0]); }
+
+// A row of C channels in vectors of V: vector i starts at channel 8 i, the last one at C - 8, so that it ends with the row.
+// Its first overlap(i) channels belong to the vector before it too: both write them, with the same values, and sums over
+// channels leave them out here.
+template <int V> __device__ __forceinline__ int vector_start(int i, int C) { return V == 1 ? i : min(i * V, C - V); }
+template <int V> __host__ __device__ __forceinline__ int vectors_of(int C) { return (C + V - 1) / V; }
+
+// Sum, maximum over the `width` lanes (a power of two) that hold one row's parts; every one of them gets it.
+__device__ __forceinline__ float lanes_sum(float v, int width) {
+    for (int d = width / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ float lanes_max(float v, int width) {
+    for (int d = width / 2; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
+// ---- 8-bit rows: q = rint(x * (127 / a)) to even, a = max |x| of the row; x is read back as q * (a / 127) ------------------
+__host__ __device__ constexpr int rows8_pitch(int cols) { return (cols + 15) / 16 * 16; }
+
+// |v| as a number that orders like an integer, infinity above every finite value and NaN above infinity: one maximum over a
+// row says how large it is and whether all of it is finite.
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ __forceinline__ unsigned lanes_umax(unsigned v, int width) {
+    for (int d = width / 2; d > 0; d /= 2) v = max(v, (unsigned)__shfl_xor((int)v, d));
+    return v;
+}
+
+struct RowCode {
+    float up, inv, scale;
+    unsigned keep;
+};
+// top: the largest magnitude of the row.  A row that is not finite gets the scale NaN and zeros, so that all of it is read back
+// as NaN.  A row below 2^-64 is coded 2^64 times larger: 127 / a would overflow.
+__device__ __forceinline__ RowCode row_code(unsigned top) {
+    const float a = __uint_as_float(top);
+    RowCode c;
+    c.keep = top < 0x7f800000u ? 0xffffffffu : 0u;
+    c.up = a < 0x1p-64f ? 0x1p64f : 1.f;
+    c.inv = top ? 127.f / (a * c.up) : 0.f;
+    c.scale = c.keep ? a / 127.f : __uint_as_float(0x7fc00000u);
+    return c;
+}
+// The low byte of the result is the code: adding 1.5 * 2^23 rounds to whole numbers, ties to even.  (Two products and a sum,
+// each rounded: contracted to one operation they would round other values than the definition's.)
+__device__ __forceinline__ unsigned code_bits(float v, const RowCode &c) {
+#pragma clang fp contract(off)
+    const float t = v * c.up * c.inv;
+    return __float_as_uint(t + 12582912.f);
+}
+__device__ __forceinline__ unsigned code_word(float v0, float v1, float v2, float v3, const RowCode &c) {
+    const unsigned lo = __builtin_amdgcn_perm(code_bits(v1, c), code_bits(v0, c), 0x0c0c0400u);
+    const unsigned hi = __builtin_amdgcn_perm(code_bits(v3, c), code_bits(v2, c), 0x04000c0cu);
+    return (lo | hi) & c.keep;
+}
+__device__ __forceinline__ void store_codes(int8_t *p, const float (&v)[8], const RowCode &c) {
+    *reinterpret_cast<u32x2_any *>(p) = (u32x2){code_word(v[0], v[1], v[2], v[3], c), code_word(v[4], v[5], v[6], v[7], c)};
+}
+__device__ __forceinline__ void store_codes(int8_t *p, const float (&v)[1], const RowCode &c) {
+    *p = (int8_t)(code_bits(v[0], c) & c.keep);
+}
+
+// ---- activations ------------------------------------------------------------------------------------------------------------
+enum { kActNone = 0, kActRelu = 1, kActSilu = 2 };
+
+// 1 / (1 + e^-z) by the hardware's 2^x and reciprocal (each within an ulp).  The rounding of z log2(e) is an error of |z| 2^-24
+// of e^-z, which counts where e^-z is not small against 1, and there |z| is a few units: 2e-7 of the result at worst.
+__device__ __forceinline__ float sigmoid(float z) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+}
+template <int ACT> __device__ __forceinline__ float activate(float z) {
+    if constexpr (ACT == kActRelu) return z < 0.f ? 0.f : z;      // NaN stays one
+    if constexpr (ACT == kActSilu) return z * sigmoid(z);
+    return z;
+}
+// act'(z); ReLU's at 0 is 0.
+template <int ACT> __device__ __forceinline__ float slope(float z) {
+    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+    if constexpr (ACT == kActSilu) {
+        const float s = sigmoid(z);
+        return s + z * s * (1.f - s);
+    }
+    return 1.f;
+}
+
+}  // namespace gspc
