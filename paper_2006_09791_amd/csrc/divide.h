@@ -21,7 +21,7 @@ GSPC_HD unsigned fast_div_any(unsigned n, unsigned d, unsigned mul) {
     return n - q * d >= d ? q + 1 : q;
 }
 
-inline unsigned div_magic(unsigned d) { return 0xffffffffu / d; }
+GSPC_HD unsigned div_magic(unsigned d) { return 0xffffffffu / d; }
 
 // Buffer accesses out of range return zero or are dropped by the hardware, so invalid lanes are given this byte offset instead
 // of being branched around.  (Only the lane's own offset counts for that: the scalar offset of the instruction is excluded

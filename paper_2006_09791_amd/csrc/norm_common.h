@@ -65,11 +65,105 @@ inline NormGrid norm_grid(const NormShape &h, int blocks_wanted) {
     return g;
 }
 
-// Lanes that share the sum of a group of `count` values: a power of two up to a wave.
-inline int group_lanes(int count) {
+// Lanes that share a sum of `count` values, where `sums` of them are taken by `threads` threads: a power of two up to a wave.
+inline int group_lanes(int count, long sums, long threads) {
     int w = 1;
-    while (w < count && w < kWave) w *= 2;
+    while (w < count && w < kWave && 2 * w * sums <= threads) w *= 2;
     return w;
+}
+
+__device__ __forceinline__ int group_of(const NormShape &h, int channel) { return fast_div_any(channel, h.D, h.m_D); }
+
+// Blocks that hold an image's `seg` channels (whole groups) of all P tokens in registers: `width` lanes (a power of two) hold a
+// token's vectors, `slots` tokens at a time, `held` times.
+struct HeldGrid {
+    int seg, segs, log_width, slots, threads;
+    int unit, units;        // what group sums are made of: vectors that lie in one group, or single channels; and those of a group
+    unsigned m_segs, m_units;
+    unsigned xcds_more, per_xcd;    // blocks of an XCD: see held_block
+    int log_lanes;          // gradient: lanes that share a channel's sum over the slots
+};
+
+// Workgroups go to the eight XCDs in turn.  Each XCD gets consecutive (image, segment) pairs, so that the pieces of a cache line
+// that several segments share are read through, and joined in, one L2.
+__device__ __forceinline__ unsigned held_block(const HeldGrid &g, unsigned b) {
+    const unsigned xcd = b & 7;
+    return xcd * g.per_xcd + min(xcd, g.xcds_more) + (b >> 3);
+}
+
+// Sums over the tokens of an image and the channels of a group.  `part` holds [slots][row] values, row = seg / unit; one wave
+// takes a group, and leaves f(sum) in out[group].
+template <typename F>
+__device__ __forceinline__ void held_group_sums(const HeldGrid &g, const float *part, int row, int groups, F f) {
+    const int lane = threadIdx.x % kWave, waves = (g.threads + kWave - 1) / kWave;
+    for (int k = threadIdx.x / kWave; k < groups; k += waves) {
+        float sum = 0.f;
+        for (int j = lane; j < g.slots * g.units; j += kWave) {
+            const int slot = fast_div(j, g.m_units);
+            sum += part[slot * row + k * g.units + j - slot * g.units];
+        }
+        sum = lanes_sum(sum, kWave);
+        if (lane == 0) f(k, sum);
+    }
+}
+
+// Bytes of an output from which on it is stored past the caches: what reads it next finds nothing of it there anyway.
+constexpr size_t kPastCaches = 32u << 20;
+
+// Such blocks for segments of `groups` groups and up to `threads` threads that hold up to `held` vectors each, or false.
+inline bool held_grid(const NormShape &h, int groups, int threads, int held, HeldGrid *g) {
+    g->seg = groups * h.D;
+    g->segs = h.groups / groups;
+    const int nv = h.C >= 8 ? (g->seg + 7) / 8 : g->seg;
+    if ((h.C >= 8 && g->seg < 8) || nv > kWave) return false;
+    g->log_width = 0;
+    while ((1 << g->log_width) < nv) ++g->log_width;
+    const long wanted = (long)h.P << g->log_width;          // no more threads than there are vectors
+    g->threads = wanted < threads ? round_up((int)wanted, kWave) : threads;
+    g->slots = g->threads >> g->log_width;
+    if ((h.P + g->slots - 1) / g->slots > held) return false;
+    g->unit = h.D % 8 == 0 ? 8 : 1;
+    g->units = h.D / g->unit;
+    g->m_segs = div_magic(g->segs);
+    g->m_units = div_magic(g->units);
+    const size_t blocks = (size_t)h.N * g->segs;
+    g->per_xcd = (unsigned)(blocks / 8);
+    g->xcds_more = (unsigned)(blocks % 8);
+    return blocks < 0x7fffffffu / 1024;
+}
+
+// The grid that is taken, or false: segments of 64 bytes of a token at least (of `size` bytes a value; half a cache line: with 32
+// the same kernel took 71 instead of 53 us on 64 images of 56x56, 256 channels in bf16), of 128 where that leaves four blocks for
+// each compute unit; as few threads as hold them in `held` vectors each (512 at most), more where the launch does not fill the
+// chip with them (one image of 7x7, 512 channels in fp32: 3.8 us with 64 threads, 3.5 with 128).
+inline bool plan_held(const NormShape &h, int size, int held, HeldGrid *best) {
+    bool found = false;
+    for (int s = 1; s <= h.groups && s * (long)h.D <= 8 * kWave; ++s) {
+        if (h.groups % s) continue;
+        const int bytes = s * h.D * size;
+        if (s < h.groups && bytes < 64) continue;
+        if (found && (long)h.N * (h.groups / s) < 1024) break;
+        for (int t = 64; t <= 512; t *= 2) {
+            HeldGrid g;
+            if (!held_grid(h, s, t, held, &g)) continue;
+            const bool fills = (long)h.N * g.segs * g.threads >= 65536;
+            if (!fills && t < 512 && (h.P + g.slots - 1) / g.slots > 2) continue;
+            *best = g;
+            found = true;
+            break;
+        }
+        if (bytes >= 128) break;
+    }
+    return found;
+}
+
+// V channels' parameters, or `none` for each where there are none.
+template <int V> __device__ __forceinline__ void load_params(const float *__restrict__ p, int at, float none, float (&v)[V]) {
+    if (p) widen(fetch<V>(p + at), v);
+    else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = none;
+    }
 }
 
 template <int V> __device__ __forceinline__ void activate_all(int act, float (&z)[V]) {

@@ -5,84 +5,125 @@
 
 namespace gspc {
 
-template <int V> struct GradAffine {
-    float mean[V], rstd[V], gamma[V], beta[V];
+// With d = x - mean and a = gamma rstd: z = a d + beta; dgamma is rstd times the sum of dz d; dx = a dz + kappa d - lambda with
+// kappa = - rstd^2 B / m, lambda = rstd A / m.  A vector's V channels are of E groups (V: any), V / E side by side in each.
+template <int V, int E> struct GradAffine {
+    float mean[E], rstd[E], a[V], beta[V];
 };
-template <int V>
+template <int V, int E>
 __device__ __forceinline__ void load_grad_affine(const NormShape &h, const float2 *__restrict__ stats, const float *__restrict__ gamma,
-                                                 const float *__restrict__ beta, int n, int at, GradAffine<V> &f) {
-    const float2 *st = stats + (size_t)n * h.groups;
+                                                 const float *__restrict__ beta, int n, int at, GradAffine<V, E> &f) {
+    load_params<V>(gamma, at, 1.f, f.a);
+    load_params<V>(beta, at, 0.f, f.beta);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const float2 s = st[(at + e) / h.D];
+    for (int e = 0; e < E; ++e) {
+        const float2 s = stats[(size_t)n * h.groups + group_of(h, at + e * (V / E))];
         f.mean[e] = s.x;
         f.rstd[e] = s.y;
-        f.gamma[e] = gamma ? gamma[at + e] : 1.f;
-        f.beta[e] = beta ? beta[at + e] : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < V; ++e) f.a[e] *= f.rstd[e * E / V];
 }
 
-// x -> xh, dy -> dz
-template <int V> __device__ __forceinline__ void to_grad(const GradAffine<V> &f, int act, float scale, float (&x)[V], float (&dy)[V]) {
+// x -> d, dy -> dz
+template <int V, int E> __device__ __forceinline__ void to_d(const GradAffine<V, E> &f, float (&x)[V]) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = (x[e] * scale - f.mean[e]) * f.rstd[e];
+    for (int e = 0; e < V; ++e) x[e] -= f.mean[e * E / V];
+}
+template <int V, int E> __device__ __forceinline__ void to_dz(const GradAffine<V, E> &f, int act, const float (&d)[V], float (&dy)[V]) {
     if (act == kActRelu) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) dy[e] *= slope<kActRelu>(fmaf(x[e], f.gamma[e], f.beta[e]));
+        for (int e = 0; e < V; ++e) dy[e] *= slope<kActRelu>(fmaf(d[e], f.a[e], f.beta[e]));
     } else if (act == kActSilu) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) dy[e] *= slope<kActSilu>(fmaf(x[e], f.gamma[e], f.beta[e]));
+        for (int e = 0; e < V; ++e) dy[e] *= slope<kActSilu>(fmaf(d[e], f.a[e], f.beta[e]));
+    }
+}
+// dz -> dx
+template <int E> struct GradGroups {
+    float kappa[E], lambda[E];
+};
+template <int V, int E> __device__ __forceinline__ void set_group(const GradAffine<V, E> &f, int e, float2 ab, GradGroups<E> &s) {
+    s.kappa[e] = -f.rstd[e] * f.rstd[e] * ab.y;
+    s.lambda[e] = f.rstd[e] * ab.x;
+}
+template <int V, int E>
+__device__ __forceinline__ void to_dx(const GradAffine<V, E> &f, const GradGroups<E> &s, const float (&d)[V], float (&dz)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) dz[e] = fmaf(f.a[e], dz[e], fmaf(d[e], s.kappa[e * E / V], -s.lambda[e * E / V]));
+}
+// x of an 8-bit row is q * scale
+template <typename TX, int V> __device__ __forceinline__ void widen_x(const Raw<TX, V> &r, float scale, float (&x)[V]) {
+    widen(r, x);
+    if constexpr (sizeof(TX) == 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] *= scale;
     }
 }
 
+// A batch of rows of x and dy in flight.
+template <typename TX, typename TG, int V> struct GradBatch {
+    static constexpr int DEEP = 4;
+    Raw<TX, V> x[DEEP];
+    Raw<TG, V> g[DEEP];
+    float scale[DEEP];
+    __device__ __forceinline__ void load(const TX *px, size_t ldx, const TG *pg, size_t ldg, const float *ps, int r, int rows, int TY) {
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k)
+            if (r + k * TY < rows) {
+                x[k] = fetch<V>(px + (size_t)(r + k * TY) * ldx);
+                g[k] = fetch<V>(pg + (size_t)(r + k * TY) * ldg);
+                if constexpr (sizeof(TX) == 1) scale[k] = ps[r + k * TY];
+            }
+    }
+};
+
 // Per channel and block: sums of dz and of dz xh over the block's rows, parts [n][chunk][2][C].
-template <typename TX, typename TG, int V>
+template <typename TX, typename TG, int V, int E>
 __global__ __launch_bounds__(kNormThreads) void norm_grad_sums_kernel(NormShape h, NormGrid g, const TG *__restrict__ dy, size_t lddy,
                                                                       const TX *__restrict__ x, size_t ldx,
                                                                       const float *__restrict__ x_scale, const float2 *__restrict__ stats,
                                                                       const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                       float *__restrict__ parts) {
+    typedef GradBatch<TX, TG, V> Batch;
     __shared__ float s_dz[kNormThreads * V], s_dx[kNormThreads * V];
     const NormBlock b = norm_block(h, g, blockIdx.x);
     const int width = b.c1 - b.c0, rows = b.r1 - b.r0;
     if (b.active) {
-        GradAffine<V> f;
-        load_grad_affine<V>(h, stats, gamma, beta, b.n, b.at, f);
         const size_t row0 = (size_t)b.n * h.P + b.r0;
         const TX *px = x + row0 * ldx + b.at;
         const TG *pg = dy + row0 * lddy + b.at;
+        const float *ps = sizeof(TX) == 1 ? x_scale + row0 : nullptr;
+        Batch now, next;
+        now.load(px, ldx, pg, lddy, ps, b.ty, rows, g.TY);
+        GradAffine<V, E> f;
+        load_grad_affine<V, E>(h, stats, gamma, beta, b.n, b.at, f);
         float sz[V] = {}, sx[V] = {};
-        for (int r = b.ty; r < rows; r += 2 * g.TY) {
-            Raw<TX, V> rx[2];
-            Raw<TG, V> rg[2];
-            float scale[2] = {1.f, 1.f};
+        for (int r = b.ty; r < rows; r += Batch::DEEP * g.TY) {
+            next.load(px, ldx, pg, lddy, ps, r + Batch::DEEP * g.TY, rows, g.TY);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < Batch::DEEP; ++k)
                 if (r + k * g.TY < rows) {
-                    rx[k] = fetch<V>(px + (size_t)(r + k * g.TY) * ldx);
-                    rg[k] = fetch<V>(pg + (size_t)(r + k * g.TY) * lddy);
-                    if (sizeof(TX) == 1) scale[k] = x_scale[row0 + r + k * g.TY];
-                }
+                    float d[V], dz[V];
+                    widen_x<TX, V>(now.x[k], now.scale[k], d);
+                    widen(now.g[k], dz);
+                    to_d<V, E>(f, d);
+                    to_dz<V, E>(f, h.act, d, dz);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                if (r + k * g.TY < rows) {
-                    float vx[V], vg[V];
-                    widen(rx[k], vx);
-                    widen(rg[k], vg);
-                    to_grad<V>(f, h.act, scale[k], vx, vg);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) sz[e] += vg[e], sx[e] = fmaf(vg[e], vx[e], sx[e]);
+                    for (int e = 0; e < V; ++e) sz[e] += dz[e], sx[e] = fmaf(dz[e], d[e], sx[e]);
                 }
+            now = next;
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const int c = b.at + e - b.c0;
-            if (c >= 0) s_dz[b.ty * width + c] = sz[e], s_dx[b.ty * width + c] = sx[e];
+            if (c >= 0) s_dz[b.ty * width + c] = sz[e], s_dx[b.ty * width + c] = sx[e] * f.rstd[e * E / V];
         }
     }
     __syncthreads();
     for (int c = threadIdx.x; c < width; c += blockDim.x) {
         float sz = 0.f, sx = 0.f;
+#pragma unroll 4
         for (int ty = 0; ty < g.TY; ++ty) sz += s_dz[ty * width + c], sx += s_dx[ty * width + c];
         float *p = parts + ((size_t)b.n * g.chunks + b.chunk) * 2 * h.C + b.c0 + c;
         p[0] = sz;
@@ -117,101 +158,259 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape h, int ch
 }
 
 // dgamma and dbeta: 64 channels a block, its waves take the images in turn.
-__global__ __launch_bounds__(256) void norm_grad_params_kernel(NormShape h, const float *__restrict__ sums, float *__restrict__ dgamma,
-                                                               float *__restrict__ dbeta) {
-    __shared__ float s_sum[2][4][kWave];
+constexpr int kParamWaves = 16;
+__global__ __launch_bounds__(kParamWaves * kWave) void norm_grad_params_kernel(NormShape h, const float *__restrict__ sums,
+                                                                               float *__restrict__ dgamma, float *__restrict__ dbeta) {
+    __shared__ float s_sum[2][kParamWaves][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
     float sz = 0.f, sx = 0.f;
     if (c < h.C) {
 #pragma unroll 8
-        for (int n = wave; n < h.N; n += 4) sz += sums[(size_t)n * 2 * h.C + c], sx += sums[((size_t)n * 2 + 1) * h.C + c];
+        for (int n = wave; n < h.N; n += kParamWaves) sz += sums[(size_t)n * 2 * h.C + c], sx += sums[((size_t)n * 2 + 1) * h.C + c];
     }
     s_sum[0][wave][lane] = sz;
     s_sum[1][wave][lane] = sx;
     __syncthreads();
-    if (wave == 0 && c < h.C) {
-        if (dbeta) dbeta[c] = (s_sum[0][0][lane] + s_sum[0][1][lane]) + (s_sum[0][2][lane] + s_sum[0][3][lane]);
-        if (dgamma) dgamma[c] = (s_sum[1][0][lane] + s_sum[1][1][lane]) + (s_sum[1][2][lane] + s_sum[1][3][lane]);
+    if (wave < 2 && c < h.C) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kParamWaves; ++w) sum += s_sum[wave][w][lane];
+        if (wave == 0 && dbeta) dbeta[c] = sum;
+        if (wave == 1 && dgamma) dgamma[c] = sum;
     }
 }
 
-template <typename TX, typename TG, int V>
+template <typename TX, typename TG, int V, int E>
 __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape h, NormGrid g, const TG *__restrict__ dy, size_t lddy,
                                                                        const TX *__restrict__ x, size_t ldx,
                                                                        const float *__restrict__ x_scale, const float2 *__restrict__ stats,
                                                                        const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                                       const float2 *__restrict__ ab, TG *__restrict__ dx, size_t lddx) {
+                                                                       const float2 *__restrict__ ab, TG *__restrict__ dx, size_t lddx,
+                                                                       int past) {
+    typedef GradBatch<TX, TG, V> Batch;
     const NormBlock b = norm_block(h, g, blockIdx.x);
     if (!b.active) return;
-    GradAffine<V> f;
-    load_grad_affine<V>(h, stats, gamma, beta, b.n, b.at, f);
-    float2 s[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[e] = ab[(size_t)b.n * h.groups + (b.at + e) / h.D];
     const size_t row0 = (size_t)b.n * h.P + b.r0;
     const TX *px = x + row0 * ldx + b.at;
     const TG *pg = dy + row0 * lddy + b.at;
+    const float *ps = sizeof(TX) == 1 ? x_scale + row0 : nullptr;
     TG *pd = dx + row0 * lddx + b.at;
     const int rows = b.r1 - b.r0;
-    for (int r = b.ty; r < rows; r += 2 * g.TY) {
-        Raw<TX, V> rx[2];
-        Raw<TG, V> rg[2];
-        float scale[2] = {1.f, 1.f};
+    Batch now, next;
+    now.load(px, ldx, pg, lddy, ps, b.ty, rows, g.TY);
+    GradAffine<V, E> f;
+    load_grad_affine<V, E>(h, stats, gamma, beta, b.n, b.at, f);
+    GradGroups<E> s;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+    for (int e = 0; e < E; ++e) set_group(f, e, ab[(size_t)b.n * h.groups + group_of(h, b.at + e * (V / E))], s);
+    for (int r = b.ty; r < rows; r += Batch::DEEP * g.TY) {
+        next.load(px, ldx, pg, lddy, ps, r + Batch::DEEP * g.TY, rows, g.TY);
+#pragma unroll
+        for (int k = 0; k < Batch::DEEP; ++k)
             if (r + k * g.TY < rows) {
-                rx[k] = fetch<V>(px + (size_t)(r + k * g.TY) * ldx);
-                rg[k] = fetch<V>(pg + (size_t)(r + k * g.TY) * lddy);
-                if (sizeof(TX) == 1) scale[k] = x_scale[row0 + r + k * g.TY];
+                float d[V], dz[V];
+                widen_x<TX, V>(now.x[k], now.scale[k], d);
+                widen(now.g[k], dz);
+                to_d<V, E>(f, d);
+                to_dz<V, E>(f, h.act, d, dz);
+                to_dx<V, E>(f, s, d, dz);
+                store(pd + (size_t)(r + k * g.TY) * lddx, dz, past);
             }
+        now = next;
+    }
+}
+
+// All but the sum over images in one launch, x and dy read once: a block holds its channels of an image.  Up to four vectors a
+// thread dz stays in fp32, so that the activation's slope is computed once (256 images of 14x14, 512 channels in bf16 with SiLU:
+// 36 us, 44 with it computed twice); eight leave no room for that (they spill: 69 us instead of 39 on 28x28, 128 channels from
+// 8-bit rows), and it is computed again from what was loaded.  sums: [n][2][C] for the parameters' gradients, or where there is
+// one image these themselves.
+template <typename TX, typename TG, int V, int E, int HELD>
+__global__ __launch_bounds__(512, 4) void norm_grad_held_kernel(NormShape h, HeldGrid g, const TG *__restrict__ dy, size_t lddy,
+                                                             const TX *__restrict__ x, size_t ldx, const float *__restrict__ x_scale,
+                                                             const float2 *__restrict__ stats, const float *__restrict__ gamma,
+                                                             const float *__restrict__ beta, float *__restrict__ sum_dz,
+                                                             float *__restrict__ sum_dx, size_t ld_sums, TG *__restrict__ dx, size_t lddx,
+                                                             int past) {
+    constexpr bool KEEP = HELD <= 4;
+    extern __shared__ float part[];                 // [2][slots][row], then [2][seg] of the channels, [groups][2] of the groups
+    const unsigned block = held_block(g, blockIdx.x), n = fast_div_any(block, g.segs, g.m_segs);
+    const int c0 = (block - n * g.segs) * g.seg, row = g.seg + 1;      // (an odd pitch: sums over slots read one column)
+    const int lane = threadIdx.x & ((1 << g.log_width) - 1), slot = threadIdx.x >> g.log_width;
+    const int nv = vectors_of<V>(g.seg);
+    const bool on = lane < nv;
+    const int at = vector_start<V>(min(lane, nv - 1), g.seg);
+    float *channel = part + 2 * g.slots * row;
+    float2 *group_ab = reinterpret_cast<float2 *>(channel + 2 * g.seg);
+
+    // No branch on a lane's own account from here to the sums: lanes past the last vector repeat it and are left out of the sums,
+    // slots past the last token repeat that with dy = 0.
+    const size_t token0 = (size_t)n * h.P;
+    Raw<TX, V> rx[HELD];
+    Raw<TG, V> rg[HELD];
+    float scale[HELD];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (r + k * g.TY < rows) {
-                float vx[V], vg[V];
-                widen(rx[k], vx);
-                widen(rg[k], vg);
-                to_grad<V>(f, h.act, scale[k], vx, vg);
-                // (the product gamma dz is rounded on its own, as in A: of a group of one value nothing is left)
+    for (int k = 0; k < HELD; ++k)
+        if (k * g.slots < h.P) {
+            const int p = slot + k * g.slots;
+            const size_t token = token0 + min(p, h.P - 1);
+            rx[k] = fetch<V>(x + token * ldx + c0 + at);
+            rg[k] = fetch<V>(dy + token * lddy + c0 + at);
+            if constexpr (sizeof(TX) == 1) scale[k] = x_scale[token];
+        }
+    GradAffine<V, E> f;
+    load_grad_affine<V, E>(h, stats, gamma, beta, n, c0 + at, f);
+    float kept[KEEP ? HELD : 1][V];
+    {
+        float sz[V] = {}, sx[V] = {};
 #pragma unroll
-                for (int e = 0; e < V; ++e) vg[e] = f.rstd[e] * (__fmul_rn(f.gamma[e], vg[e]) - fmaf(vx[e], s[e].y, s[e].x));
-                store(pd + (size_t)(r + k * g.TY) * lddx, vg);
+        for (int k = 0; k < HELD; ++k) {
+            if (k * g.slots < h.P) {
+                float d[V];
+                float (&dz)[V] = kept[KEEP ? k : 0];
+                hold(rx[k]);
+                hold(rg[k]);
+                if ((k + 1) * g.slots > h.P) keep_if(rg[k], slot + k * g.slots < h.P);
+                widen_x<TX, V>(rx[k], scale[k], d);
+                widen(rg[k], dz);
+                to_d<V, E>(f, d);
+                to_dz<V, E>(f, h.act, d, dz);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sz[e] += dz[e], sx[e] = fmaf(dz[e], d[e], sx[e]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (on) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) part[slot * row + at + e] = sz[e], part[(g.slots + slot) * row + at + e] = sx[e] * f.rstd[e * E / V];
+        }
+    }
+    __syncthreads();
+    // sums over the slots: `lanes` lanes for each of the 2 seg columns
+    const int lanes = 1 << g.log_lanes;
+    for (int i = threadIdx.x >> g.log_lanes; i < 2 * g.seg; i += g.threads >> g.log_lanes) {
+        const int which = i >= g.seg, c = i - which * g.seg;
+        float sum = 0.f;
+        for (int j = threadIdx.x & (lanes - 1); j < g.slots; j += lanes) sum += part[(which * g.slots + j) * row + c];
+        sum = lanes_sum(sum, lanes);
+        if ((threadIdx.x & (lanes - 1)) == 0) {
+            channel[i] = sum;
+            float *to = which ? sum_dx : sum_dz;
+            if (to) to[n * ld_sums + c0 + c] = sum;
+        }
+    }
+    __syncthreads();
+    const float m = (float)h.P * (float)h.D;
+    const int groups = g.seg / h.D, wave_lane = threadIdx.x % kWave;
+    for (int k = threadIdx.x / kWave; k < groups; k += g.threads / kWave) {
+        float a = 0.f, b = 0.f;
+        for (int j = wave_lane; j < h.D; j += kWave) {
+            const float w = gamma ? gamma[c0 + k * h.D + j] : 1.f;
+            a = fmaf(w, channel[k * h.D + j], a);
+            b = fmaf(w, channel[g.seg + k * h.D + j], b);
+        }
+        a = lanes_sum(a, kWave);
+        b = lanes_sum(b, kWave);
+        if (wave_lane == 0) group_ab[k] = make_float2(a / m, b / m);
+    }
+    __syncthreads();
+    GradGroups<E> s;
+#pragma unroll
+    for (int e = 0; e < E; ++e) set_group(f, e, group_ab[group_of(h, at + e * (V / E))], s);
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        if (k * g.slots < h.P) {
+            const int p = slot + k * g.slots;
+            float d[V];
+            float (&dz)[V] = kept[KEEP ? k : 0];
+            hold(rx[k]);
+            widen_x<TX, V>(rx[k], scale[k], d);
+            to_d<V, E>(f, d);
+            if constexpr (!KEEP) {
+                hold(rg[k]);
+                widen(rg[k], dz);
+                to_dz<V, E>(f, h.act, d, dz);
+            }
+            to_dx<V, E>(f, s, d, dz);
+            if (on && p < h.P) store(dx + (token0 + p) * lddx + c0 + at, dz, past);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
+constexpr int kBackwardBlocks = 2048;
+
 size_t norm_backward_bytes(const NormShape &h) {
-    const NormGrid g = norm_grid(h, 2048);
+    const NormGrid g = norm_grid(h, kBackwardBlocks);
     return ((size_t)h.N * g.chunks * 2 * h.C + (size_t)h.N * 2 * h.C + (size_t)h.N * h.groups * 2) * sizeof(float);
 }
 
-template <typename TX, typename TG, int V>
-static hipError_t backward(const NormShape &h, const NormBackward &b, void *ws, hipStream_t s, const char **name) {
-    const unsigned param_blocks = (h.C + kWave - 1) / kWave;
-    if ((long)h.N * h.P == 0) {
-        if (b.dgamma || b.dbeta)
-            hipLaunchKernelGGL(norm_grad_params_kernel, dim3(param_blocks), dim3(256), 0, s, NormShape{0, 0, h.C, h.groups, h.D, 0},
-                               (const float *)nullptr, b.dgamma, b.dbeta);
-        *name = "norm_grad_params";
-        return hipGetLastError();
-    }
-    const NormGrid g = norm_grid(h, 2048);
-    float *parts = static_cast<float *>(ws), *sums = parts + (size_t)h.N * g.chunks * 2 * h.C;
-    float2 *ab = reinterpret_cast<float2 *>(sums + (size_t)h.N * 2 * h.C);
+// Four vectors a thread where that can be, else eight where x and dy take 64 registers then.
+template <typename TX, typename TG> constexpr int grad_held_most() { return sizeof(TX) == 4 || sizeof(TG) == 4 ? 4 : 8; }
+template <typename TX, typename TG> static bool plan_grad_held(const NormShape &h, HeldGrid *g) {
+    return plan_held(h, sizeof(TG), 4, g) || (grad_held_most<TX, TG>() > 4 && plan_held(h, sizeof(TG), 8, g));
+}
+
+template <typename TX, typename TG, int V, int E>
+static void launch_grad_held(const NormShape &h, HeldGrid g, const NormBackward &b, float *sums, hipStream_t s) {
+    constexpr int MOST = grad_held_most<TX, TG>();
+    const int held = (h.P + g.slots - 1) / g.slots;
+    const auto kern = held <= 1 ? norm_grad_held_kernel<TX, TG, V, E, 1> : held <= 2 ? norm_grad_held_kernel<TX, TG, V, E, 2>
+                    : held <= 4 ? norm_grad_held_kernel<TX, TG, V, E, 4> : norm_grad_held_kernel<TX, TG, V, E, MOST>;
+    g.log_lanes = 0;
+    while ((1 << g.log_lanes) < g.slots && g.log_lanes < 6 && (4 * g.seg << g.log_lanes) <= g.threads) ++g.log_lanes;
+    const size_t lds = (2 * (size_t)g.slots * (g.seg + 1) + 2 * g.seg + 2 * (g.seg / h.D) + 1) * sizeof(float);
+    const bool one = h.N == 1;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((size_t)h.N * g.segs)), dim3(g.threads), lds, s, h, g, static_cast<const TG *>(b.dy), b.lddy,
+                       static_cast<const TX *>(b.x), b.ldx, b.x_scale, reinterpret_cast<const float2 *>(b.stats), b.gamma, b.beta,
+                       one ? b.dbeta : sums, one ? b.dgamma : sums + h.C, (size_t)2 * h.C, static_cast<TG *>(b.dx), b.lddx, b.past);
+}
+
+template <typename TX, typename TG, int V, int E>
+static void launch_grad(const NormShape &h, const NormGrid &g, const NormBackward &b, float *parts, float *sums, float2 *ab, hipStream_t s) {
     const TX *x = static_cast<const TX *>(b.x);
     const TG *dy = static_cast<const TG *>(b.dy);
     const float2 *stats = reinterpret_cast<const float2 *>(b.stats);
     const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
-    const int lanes = group_lanes(h.D);
-    hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TG, V>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
+    const int lanes = group_lanes(h.D, (long)h.N * h.groups, 1L << 20);
+    hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TG, V, E>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
                        b.gamma, b.beta, parts);
     hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * lanes + 255) / 256)), dim3(256), 0, s, h, g.chunks,
                        lanes, parts, b.gamma, sums, ab);
-    if (b.dgamma || b.dbeta)
-        hipLaunchKernelGGL(norm_grad_params_kernel, dim3(param_blocks), dim3(256), 0, s, h, sums, b.dgamma, b.dbeta);
-    hipLaunchKernelGGL((norm_grad_apply_kernel<TX, TG, V>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
-                       b.gamma, b.beta, ab, static_cast<TG *>(b.dx), b.lddx);
-    *name = "norm_grad_apply";
+    hipLaunchKernelGGL((norm_grad_apply_kernel<TX, TG, V, E>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
+                       b.gamma, b.beta, ab, static_cast<TG *>(b.dx), b.lddx, b.past);
+}
+
+template <typename TX, typename TG, int V>
+static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStream_t s, const char **name) {
+    const dim3 param_blocks((h.C + kWave - 1) / kWave);
+    const bool params = b.dgamma || b.dbeta;
+    if ((long)h.N * h.P == 0) {                     // no tokens: zeros
+        *name = "norm_grad_params";
+        NormShape none = h;
+        none.N = 0;
+        if (params)
+            hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, none, (const float *)nullptr, b.dgamma, b.dbeta);
+        return hipGetLastError();
+    }
+    const NormGrid g = norm_grid(h, kBackwardBlocks);
+    float *parts = static_cast<float *>(ws), *sums = parts + (size_t)h.N * g.chunks * 2 * h.C;
+    float2 *ab = reinterpret_cast<float2 *>(sums + (size_t)h.N * 2 * h.C);
+    b.past = (size_t)h.N * h.P * h.C * sizeof(TG) >= kPastCaches;
+    HeldGrid held;
+    const bool hold = plan_grad_held<TX, TG>(h, &held);
+    *name = hold ? "norm_grad_held" : "norm_grad_apply";
+    const auto run = [&](auto e) {
+        constexpr int E = decltype(e)::value;
+        if (hold) launch_grad_held<TX, TG, V, E>(h, held, b, sums, s);
+        else launch_grad<TX, TG, V, E>(h, g, b, parts, sums, ab, s);
+    };
+    if (V == 8 && h.D % 8 == 0) run(std::integral_constant<int, 1>{});
+    else if (V == 8 && h.D % 4 == 0) run(std::integral_constant<int, V == 8 ? 2 : 1>{});
+    else run(std::integral_constant<int, V>{});
+    if (params && !(hold && h.N == 1))
+        hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h, sums, b.dgamma, b.dbeta);
     return hipGetLastError();
 }
 

@@ -9,42 +9,49 @@ namespace gspc {
 __host__ __device__ __forceinline__ size_t norm_parts(const NormShape &h, const NormGrid &g) { return (size_t)h.groups + g.slabs - 1; }
 
 // Mean and sum of squared deviations of each group over a block's rows.  A thread sums x - x0 and its square, x0 its first value
-// of the channel, so that an offset of the channel does not cancel; the threads' means and deviations are joined as such
-// (total deviation = sum of the parts' own + sum of count * (part's mean - mean)^2), never as sums of squares.
-template <typename T, int V>
+// (of the channel, or of the vector where all its channels are of one group: ONE), so that an offset does not cancel; the threads'
+// means and deviations are joined as such (total deviation = sum of the parts' own + sum of count * (part's mean - mean)^2), never
+// as sums of squares.
+template <typename T, int V, bool ONE>
 __global__ __launch_bounds__(kNormThreads) void norm_stats_kernel(NormShape h, NormGrid g, const T *__restrict__ x, size_t ldx,
                                                                   float2 *__restrict__ parts, int lanes) {
-    __shared__ float s_mean[kNormThreads * V], s_dev[kNormThreads * V];
+    constexpr int E = ONE ? 1 : V, DEEP = sizeof(T) == 4 ? 4 : 8;
+    __shared__ float s_mean[kNormThreads * E], s_dev[kNormThreads * E];
     const NormBlock b = norm_block(h, g, blockIdx.x);
-    const int width = b.c1 - b.c0;
+    const int width = ONE ? b.nv : b.c1 - b.c0, rows = b.r1 - b.r0;
     if (b.active) {
-        const T *p = x + ((size_t)b.n * h.P + b.r0) * ldx + b.at;
-        float first[V], sum[V] = {}, sq[V] = {};
+        const T *p = x + ((size_t)b.n * h.P + b.r0 + b.ty) * ldx + b.at;
+        const size_t step = g.TY * ldx;
+        float first[E], sum[E] = {}, sq[E] = {};
         int count = 0;
-        for (int r = b.ty; r < b.r1 - b.r0; r += 4 * g.TY) {
-            Raw<T, V> raw[4];
+        for (int r = b.ty; r < rows; r += DEEP * g.TY) {
+            Raw<T, V> raw[DEEP];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (r + k * g.TY < b.r1 - b.r0) raw[k] = fetch<V>(p + (size_t)(r + k * g.TY) * ldx);
+            for (int k = 0; k < DEEP; ++k, p += step)
+                if (r + k * g.TY < rows) raw[k] = fetch<V>(p);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (r + k * g.TY < b.r1 - b.r0) {
+            for (int k = 0; k < DEEP; ++k)
+                if (r + k * g.TY < rows) {
                     float v[V];
                     widen(raw[k], v);
+                    if (k == 0 && count == 0) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) first[e] = v[e];
+                    }
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        if (count == 0) first[e] = v[e];
-                        const float d = v[e] - first[e];
-                        sum[e] += d;
-                        sq[e] = fmaf(d, d, sq[e]);
+                        const int f = ONE ? 0 : e;
+                        const float d = v[e] - first[f];
+                        sum[f] += d;
+                        sq[f] = fmaf(d, d, sq[f]);
                     }
                     ++count;
                 }
         }
-        const float inv = 1.f / (float)count;
+        const float inv = 1.f / (float)(count * (V / E));
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const int c = b.at + e - b.c0;
+        for (int e = 0; e < E; ++e) {
+            const int c = ONE ? b.tx : b.at + e - b.c0;
             const float m = sum[e] * inv;
             if (c >= 0 && count) {
                 s_mean[b.ty * width + c] = first[e] + m;
@@ -53,22 +60,22 @@ __global__ __launch_bounds__(kNormThreads) void norm_stats_kernel(NormShape h, N
         }
     }
     __syncthreads();
-    const int rows = b.r1 - b.r0, TY = min(g.TY, rows);
-    const int g0 = b.c0 / h.D, g1 = (b.c1 - 1) / h.D, lane = threadIdx.x & (lanes - 1);
+    constexpr int U = V / E;                        // channels behind one of these
+    const int TY = min(g.TY, rows), each = rows / TY, more = rows - each * TY;   // thread ty had each + (ty < more) rows
+    const int g0 = group_of(h, b.c0), g1 = group_of(h, b.c1 - 1), lane = threadIdx.x & (lanes - 1);
     for (int k = g0 + threadIdx.x / lanes; k <= g1; k += blockDim.x / lanes) {
-        const int lo = max(k * h.D, b.c0) - b.c0, hi = min((k + 1) * h.D, b.c1) - b.c0, n = (hi - lo) * TY;
-        // (the rows of thread ty: all have rows / TY, the first rows % TY one more)
-        const int each = rows / TY, more = rows - each * TY;
+        const int lo = (max(k * h.D, b.c0) - b.c0) / U, hi = (min((k + 1) * h.D, b.c1) - b.c0) / U, wide = hi - lo;
+        const unsigned mul = div_magic(wide);
         float mean = 0.f, dev = 0.f;
-        for (int i = lane; i < n; i += lanes) {
-            const int ty = i / (hi - lo), c = lo + i - ty * (hi - lo);
-            mean += s_mean[ty * width + c] * (float)(each + (ty < more));
+        for (int i = lane; i < wide * TY; i += lanes) {
+            const int ty = fast_div(i, mul);
+            mean += s_mean[ty * width + lo + i - ty * wide] * (float)(each + (ty < more));
         }
-        mean = lanes_sum(mean, lanes) / ((float)rows * (float)(hi - lo));
-        for (int i = lane; i < n; i += lanes) {
-            const int ty = i / (hi - lo), c = lo + i - ty * (hi - lo);
-            const float d = s_mean[ty * width + c] - mean;
-            dev += s_dev[ty * width + c] + d * d * (float)(each + (ty < more));
+        mean = lanes_sum(mean, lanes) / ((float)rows * (float)wide);
+        for (int i = lane; i < wide * TY; i += lanes) {
+            const int ty = fast_div(i, mul), at = ty * width + lo + i - ty * wide;
+            const float d = s_mean[at] - mean;
+            dev += s_dev[at] + d * d * (float)((each + (ty < more)) * U);
         }
         dev = lanes_sum(dev, lanes);
         if (lane == 0)
@@ -114,12 +121,13 @@ template <int V>
 __device__ __forceinline__ void load_affine(const NormShape &h, const float2 *__restrict__ stats, const float *__restrict__ gamma,
                                             const float *__restrict__ beta, int n, int at, Affine<V> &f) {
     const float2 *st = stats + (size_t)n * h.groups;
+    load_params<V>(gamma, at, 1.f, f.a);
+    load_params<V>(beta, at, 0.f, f.b);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const float2 s = st[(at + e) / h.D];
+        const float2 s = st[group_of(h, at + e)];
         f.mean[e] = s.x;
-        f.a[e] = s.y * (gamma ? gamma[at + e] : 1.f);
-        f.b[e] = beta ? beta[at + e] : 0.f;
+        f.a[e] *= s.y;
     }
 }
 template <int V> __device__ __forceinline__ void apply_affine(const Affine<V> &f, int act, float (&v)[V]) {
@@ -128,127 +136,254 @@ template <int V> __device__ __forceinline__ void apply_affine(const Affine<V> &f
     activate_all(act, v);
 }
 
-// y as fp32 or bf16: threads keep their channels' coefficients and walk down the rows.
+// y as fp32 or bf16: threads keep their channels' coefficients and walk down the rows, one batch of loads ahead of the values that
+// they multiply (and ahead of the coefficients' own loads: those are a second trip to memory).
 template <typename TX, typename TY, int V>
 __global__ __launch_bounds__(kNormThreads) void norm_apply_kernel(NormShape h, NormGrid g, const TX *__restrict__ x, size_t ldx,
                                                                   const float2 *__restrict__ stats, const float *__restrict__ gamma,
-                                                                  const float *__restrict__ beta, TY *__restrict__ y, size_t ldy) {
+                                                                  const float *__restrict__ beta, TY *__restrict__ y, size_t ldy, int past) {
+    constexpr int DEEP = 4;
     const NormBlock b = norm_block(h, g, blockIdx.x);
     if (!b.active) return;
-    Affine<V> f;
-    load_affine<V>(h, stats, gamma, beta, b.n, b.at, f);
-    const size_t row0 = (size_t)b.n * h.P + b.r0;
+    const size_t row0 = (size_t)b.n * h.P + b.r0 + b.ty;
+    const int rows = b.r1 - b.r0;
     const TX *p = x + row0 * ldx + b.at;
     TY *q = y + row0 * ldy + b.at;
-    for (int r = b.ty; r < b.r1 - b.r0; r += 4 * g.TY) {
-        Raw<TX, V> raw[4];
+    Raw<TX, V> raw[DEEP], next[DEEP];
+    const auto load = [&](int r, Raw<TX, V> (&to)[DEEP]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (r + k * g.TY < b.r1 - b.r0) raw[k] = fetch<V>(p + (size_t)(r + k * g.TY) * ldx);
+        for (int k = 0; k < DEEP; ++k, p += g.TY * ldx)
+            if (r + k * g.TY < rows) to[k] = fetch<V>(p);
+    };
+    load(b.ty, raw);
+    Affine<V> f;
+    load_affine<V>(h, stats, gamma, beta, b.n, b.at, f);
+    for (int r = b.ty; r < rows; r += DEEP * g.TY) {
+        load(r + DEEP * g.TY, next);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (r + k * g.TY < b.r1 - b.r0) {
+        for (int k = 0; k < DEEP; ++k, q += g.TY * ldy)
+            if (r + k * g.TY < rows) {
                 float v[V];
                 widen(raw[k], v);
                 apply_affine<V>(f, h.act, v);
-                store(q + (size_t)(r + k * g.TY) * ldy, v);
+                store(q, v, past);
             }
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) raw[k] = next[k];
     }
 }
 
 // Outputs in 8-bit rows need all of a row's channels: `width` lanes hold one row, HELD vectors each with their coefficients, and
-// walk down the rows of an image (HELD = 0: rows of any length, read and computed twice).  TY = int8_t: y is 8-bit rows;
-// SAVE: x is written as 8-bit rows too.
+// walk down the rows of an image, several at a time so that their loads are in flight together (HELD = 0: rows of any length,
+// read and computed twice).  TY = int8_t: y is 8-bit rows; SAVE: x is written as 8-bit rows too.
 template <typename TX, typename TY, int V, int HELD, bool SAVE>
-__global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int width, int blocks, int rows, unsigned m_blocks,
+__global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_width, int blocks, int rows, unsigned m_blocks,
                                                         const TX *__restrict__ x, size_t ldx, const float2 *__restrict__ stats,
                                                         const float *__restrict__ gamma, const float *__restrict__ beta,
                                                         TY *__restrict__ y, size_t ldy, float *__restrict__ y_scale,
-                                                        int8_t *__restrict__ saved, float *__restrict__ saved_scale) {
+                                                        int8_t *__restrict__ saved, float *__restrict__ saved_scale, int past) {
     constexpr bool CODES = sizeof(TY) == 1;
-    constexpr int H = HELD ? HELD : 1;
-    const int n = fast_div_any(blockIdx.x, blocks, m_blocks), lane = threadIdx.x & (width - 1);
-    const int r0 = ((int)blockIdx.x - n * blocks) * rows, r1 = min(r0 + rows, h.P);
+    constexpr int H = HELD ? HELD : 1, DEEP = HELD == 0 ? 1 : 4 / HELD;
+    const int n = fast_div_any(blockIdx.x, blocks, m_blocks), width = 1 << log_width, lane = threadIdx.x & (width - 1);
+    const int r0 = ((int)blockIdx.x - n * blocks) * rows, r1 = min(r0 + rows, h.P), slots = 256 >> log_width;
     const int nv = vectors_of<V>(h.C), pitch = rows8_pitch(h.C);
+    Raw<TX, V> raw[DEEP][H], next[DEEP][H];
+    const auto load = [&](int r, Raw<TX, V> (&to)[DEEP][H]) {
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int d = 0; d < DEEP; ++d)
+#pragma unroll
+                for (int k = 0; k < HELD; ++k)
+                    if (r + d * slots < r1 && lane + k * width < nv)
+                        to[d][k] = fetch<V>(x + ((size_t)n * h.P + r + d * slots) * ldx + vector_start<V>(lane + k * width, h.C));
+        }
+    };
+    load(r0 + (threadIdx.x >> log_width), raw);
     Affine<V> f[H];
     if constexpr (HELD > 0) {
 #pragma unroll
         for (int k = 0; k < HELD; ++k)
             if (lane + k * width < nv) load_affine<V>(h, stats, gamma, beta, n, vector_start<V>(lane + k * width, h.C), f[k]);
     }
-    for (int r = r0 + threadIdx.x / width; r < r1; r += 256 / width) {
-        const size_t row = (size_t)n * h.P + r;
-        const TX *p = x + row * ldx;
-        unsigned top_x = 0, top_y = 0;
-        float v[H][V];
-        const auto each = [&](auto body) {       // body(first channel, its values, its coefficients, loop count)
+    for (int r = r0 + (threadIdx.x >> log_width); r < r1; r += DEEP * slots) {
+        load(r + DEEP * slots, next);
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            if (r + d * slots >= r1) continue;
+            const size_t row = (size_t)n * h.P + r + d * slots;
+            float v[H][V];
+            const auto each = [&](auto body) {       // body(first channel, its values, its coefficients)
+                if constexpr (HELD > 0) {
+#pragma unroll
+                    for (int k = 0; k < HELD; ++k)
+                        if (lane + k * width < nv) body(vector_start<V>(lane + k * width, h.C), v[k], f[k]);
+                } else {
+                    for (int i = lane; i < nv; i += width) {
+                        const int at = vector_start<V>(i, h.C);
+                        widen(fetch<V>(x + row * ldx + at), v[0]);
+                        load_affine<V>(h, stats, gamma, beta, n, at, f[0]);
+                        body(at, v[0], f[0]);
+                    }
+                }
+            };
             if constexpr (HELD > 0) {
 #pragma unroll
                 for (int k = 0; k < HELD; ++k)
-                    if (lane + k * width < nv) body(vector_start<V>(lane + k * width, h.C), v[k], f[k]);
-            } else {
-                for (int i = lane; i < nv; i += width) {
-                    const int at = vector_start<V>(i, h.C);
-                    widen(fetch<V>(p + at), v[0]);
-                    load_affine<V>(h, stats, gamma, beta, n, at, f[0]);
-                    body(at, v[0], f[0]);
-                }
+                    if (lane + k * width < nv) widen(raw[d][k], v[k]);
             }
-        };
+            if constexpr (SAVE) {
+                unsigned top = 0;
+                each([&](int, float (&t)[V], Affine<V> &) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) top = max(top, magnitude(t[e]));
+                });
+                const RowCode c = row_code(lanes_umax(top, width));
+                each([&](int at, float (&t)[V], Affine<V> &) { store_codes(saved + row * pitch + at, t, c); });
+                for (int i = h.C + lane; i < pitch; i += width) saved[row * pitch + i] = 0;
+                if (lane == 0) saved_scale[row] = c.scale;
+            }
+            if constexpr (CODES) {
+                unsigned top = 0;
+                each([&](int, float (&t)[V], Affine<V> &fk) {
+                    apply_affine<V>(fk, h.act, t);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) top = max(top, magnitude(t[e]));
+                });
+                const RowCode c = row_code(lanes_umax(top, width));
+                each([&](int at, float (&t)[V], Affine<V> &fk) {
+                    if constexpr (HELD == 0) apply_affine<V>(fk, h.act, t);
+                    store_codes(reinterpret_cast<int8_t *>(y) + row * pitch + at, t, c);
+                });
+                for (int i = h.C + lane; i < pitch; i += width) reinterpret_cast<int8_t *>(y)[row * pitch + i] = 0;
+                if (lane == 0) y_scale[row] = c.scale;
+            } else {
+                each([&](int at, float (&t)[V], Affine<V> &fk) {
+                    apply_affine<V>(fk, h.act, t);
+                    store(y + row * ldy + at, t, past);
+                });
+            }
+        }
         if constexpr (HELD > 0) {
-            Raw<TX, V> raw[H];
 #pragma unroll
-            for (int k = 0; k < HELD; ++k)
-                if (lane + k * width < nv) raw[k] = fetch<V>(p + vector_start<V>(lane + k * width, h.C));
+            for (int d = 0; d < DEEP; ++d)
 #pragma unroll
-            for (int k = 0; k < HELD; ++k)
-                if (lane + k * width < nv) widen(raw[k], v[k]);
-        }
-        if constexpr (SAVE) {
-            each([&](int, float (&t)[V], Affine<V> &) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) top_x = max(top_x, magnitude(t[e]));
-            });
-            const RowCode c = row_code(lanes_umax(top_x, width));
-            each([&](int at, float (&t)[V], Affine<V> &) { store_codes(saved + row * pitch + at, t, c); });
-            for (int i = h.C + lane; i < pitch; i += width) saved[row * pitch + i] = 0;
-            if (lane == 0) saved_scale[row] = c.scale;
-        }
-        if constexpr (CODES) {
-            each([&](int, float (&t)[V], Affine<V> &fk) {
-                apply_affine<V>(fk, h.act, t);
-#pragma unroll
-                for (int e = 0; e < V; ++e) top_y = max(top_y, magnitude(t[e]));
-            });
-            const RowCode c = row_code(lanes_umax(top_y, width));
-            each([&](int at, float (&t)[V], Affine<V> &fk) {
-                if constexpr (HELD == 0) apply_affine<V>(fk, h.act, t);
-                store_codes(reinterpret_cast<int8_t *>(y) + row * pitch + at, t, c);
-            });
-            for (int i = h.C + lane; i < pitch; i += width) reinterpret_cast<int8_t *>(y)[row * pitch + i] = 0;
-            if (lane == 0) y_scale[row] = c.scale;
-        } else {
-            each([&](int at, float (&t)[V], Affine<V> &fk) {
-                apply_affine<V>(fk, h.act, t);
-                store(y + row * ldy + at, t);
-            });
+                for (int k = 0; k < HELD; ++k) raw[d][k] = next[d][k];
         }
     }
 }
 
+// All of it in one launch, x read once: a block holds its channels of an image in registers, HELD vectors a thread, takes the
+// mean, then the squared deviations from it, then writes y (TY = void: only the statistics).  ONE: a vector's channels are of
+// one group (D a multiple of 8).
+template <typename TX, typename TY, int V, int HELD, bool ONE>
+__global__ __launch_bounds__(512) void norm_held_kernel(NormShape h, HeldGrid g, const TX *__restrict__ x, size_t ldx,
+                                                        const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
+                                                        float2 *__restrict__ stats, TY *__restrict__ y, size_t ldy, int past) {
+    constexpr int E = ONE ? 1 : V;                  // groups, and sums, of a vector
+    extern __shared__ float part[];                 // [slots][seg / unit], then the groups' results
+    const unsigned block = held_block(g, blockIdx.x), n = fast_div_any(block, g.segs, g.m_segs);
+    const int c0 = (block - n * g.segs) * g.seg, groups = ONE ? g.seg / 8 / g.units : g.seg / h.D;
+    const int lane = threadIdx.x & ((1 << g.log_width) - 1), slot = threadIdx.x >> g.log_width;
+    const int nv = vectors_of<V>(g.seg), row = ONE ? nv : g.seg, at = vector_start<V>(lane, g.seg);
+    const bool on = lane < nv;
+    float *group_mean = part + g.slots * row, *group_rstd = group_mean + groups;
+
+    const size_t token = (size_t)n * h.P + slot;
+    Raw<TX, V> raw[HELD];
+    {
+        const TX *p = x + token * ldx + c0 + at;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k, p += g.slots * ldx)
+            if (slot + k * g.slots < h.P && on) raw[k] = fetch<V>(p);
+    }
+    float a[V], b[V];
+    if constexpr (!std::is_void<TY>::value) {
+        load_params<V>(gamma, c0 + (on ? at : 0), 1.f, a);
+        load_params<V>(beta, c0 + (on ? at : 0), 0.f, b);
+    }
+    int group[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) group[e] = on ? fast_div(ONE ? lane : at + e, g.m_units) : 0;
+
+    const auto each = [&](auto body) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            if (slot + k * g.slots < h.P && on) {
+                float v[V];
+                hold(raw[k]);
+                widen(raw[k], v);
+                body(v);
+            }
+            __builtin_amdgcn_sched_barrier(0);      // one token's values at a time: the raw ones fill the registers
+        }
+    };
+    const auto leave = [&](const float (&sum)[E]) {
+        if (on) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) part[slot * row + (ONE ? lane : at) + e] = sum[e];   // (shared channels: the same sum twice)
+        }
+        __syncthreads();
+    };
+    const float m = (float)h.P * (float)h.D;
+    float mean[E];
+    {
+        float sum[E] = {};
+        each([&](float (&v)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[ONE ? 0 : e] += v[e];
+        });
+        leave(sum);
+        held_group_sums(g, part, row, groups, [&](int k, float s) { group_mean[k] = s / m; });
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) mean[e] = group_mean[group[e]];
+    }
+    {
+        float sum[E] = {};
+        each([&](float (&v)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = v[e] - mean[ONE ? 0 : e];
+                sum[ONE ? 0 : e] = fmaf(d, d, sum[ONE ? 0 : e]);
+            }
+        });
+        leave(sum);
+        held_group_sums(g, part, row, groups, [&](int k, float s) {
+            const float r = 1.f / sqrtf(s / m + eps);
+            group_rstd[k] = r;
+            if (stats) stats[(size_t)n * h.groups + group_of(h, c0) + k] = make_float2(group_mean[k], r);
+        });
+    }
+    if constexpr (!std::is_void<TY>::value) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[e] *= group_rstd[group[ONE ? 0 : e]];
+        TY *q = y + token * ldy + c0 + at;
+        each([&](float (&v)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = fmaf(v[e] - mean[ONE ? 0 : e], a[e], b[e]);
+            activate_all(h.act, v);
+            store(q, v, past);
+            q += g.slots * ldy;
+        });
+    }
+}
+
 // ---- launches ---------------------------------------------------------------------------------------------------------------
+constexpr int kForwardBlocks = 2048;
+
 static size_t forward_bytes(const NormShape &h, const NormGrid &g) {
     return (size_t)h.N * g.chunks * norm_parts(h, g) * sizeof(float2) + (size_t)h.N * h.groups * sizeof(float2);
 }
 
-size_t norm_forward_bytes(const NormShape &h) { return forward_bytes(h, norm_grid(h, 2048)); }
+size_t norm_forward_bytes(const NormShape &h) { return forward_bytes(h, norm_grid(h, kForwardBlocks)); }
 
 template <typename TX, typename TY, int V, bool SAVE>
 static void launch_rows(const NormShape &h, const NormForward &f, const float2 *stats, hipStream_t s) {
     const int nv = vectors_of<V>(h.C);
-    int width = 1;
-    while (width < nv && width < kWave) width *= 2;
-    const int each = (nv + width - 1) / width;
+    int log_width = 0;
+    while ((1 << log_width) < nv && log_width < 6) ++log_width;
+    const int width = 1 << log_width, each = (nv + width - 1) / width;
     const auto kern = V == 1 || each <= 1 ? norm_rows_kernel<TX, TY, V, 1, SAVE>
                     : each <= 2 ? norm_rows_kernel<TX, TY, V, 2, SAVE>
                     : each <= 4 ? norm_rows_kernel<TX, TY, V, 4, SAVE> : norm_rows_kernel<TX, TY, V, 0, SAVE>;
@@ -258,20 +393,63 @@ static void launch_rows(const NormShape &h, const NormForward &f, const float2 *
     if (blocks > most) blocks = most;
     const int rows = (int)((h.P + blocks - 1) / blocks);
     blocks = (h.P + rows - 1) / rows;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * h.N)), dim3(256), 0, s, h, width, (int)blocks, rows, div_magic((unsigned)blocks),
+    hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * h.N)), dim3(256), 0, s, h, log_width, (int)blocks, rows, div_magic((unsigned)blocks),
                        static_cast<const TX *>(f.x), f.ldx, stats, f.gamma, f.beta, static_cast<TY *>(f.y), f.ldy, f.y_scale, f.saved,
-                       f.saved_scale);
+                       f.saved_scale, f.past);
+}
+
+// Vectors that a thread of norm_held_kernel holds at most: 64 registers of raw values.
+template <typename TX> constexpr int held_most() { return sizeof(TX) == 4 ? 8 : 16; }
+
+template <typename TX, typename TY, int V, bool ONE>
+static void launch_held(const NormShape &h, const HeldGrid &g, const NormForward &f, float2 *stats, hipStream_t s) {
+    constexpr int MOST = held_most<TX>();
+    const int held = (h.P + g.slots - 1) / g.slots, row = ONE ? g.seg / 8 : g.seg;
+    const auto kern = held <= 2 ? norm_held_kernel<TX, TY, V, 2, ONE>
+                    : held <= MOST / 2 ? norm_held_kernel<TX, TY, V, MOST / 2, ONE> : norm_held_kernel<TX, TY, V, MOST, ONE>;
+    const size_t lds = ((size_t)g.slots * row + 2 * (g.seg / h.D)) * sizeof(float);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((size_t)h.N * g.segs)), dim3(g.threads), lds, s, h, g, static_cast<const TX *>(f.x), f.ldx,
+                       f.gamma, f.beta, f.eps, stats, static_cast<TY *>(f.y), f.ldy, f.past);
+}
+template <typename TX, typename TY, int V>
+static void run_held(const NormShape &h, const HeldGrid &g, const NormForward &f, float2 *stats, hipStream_t s) {
+    if constexpr (V == 8) {
+        if (g.unit == 8) return launch_held<TX, TY, V, true>(h, g, f, stats, s);
+    }
+    launch_held<TX, TY, V, false>(h, g, f, stats, s);
+}
+
+// stats of images too large to be held: two launches
+template <typename TX, int V>
+static void launch_stats(const NormShape &h, const NormGrid &g, const NormForward &f, float2 *parts, float2 *stats, hipStream_t s) {
+    const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
+    const TX *x = static_cast<const TX *>(f.x);
+    const int units = V == 8 && h.D % 8 == 0 ? h.D / 8 : h.D;      // of a group in one row of a block's sums
+    const int lanes = group_lanes(g.TY * (units < kSlab ? units : kSlab), (h.C < kSlab ? h.C : kSlab) / h.D + 1, g.threads);
+    if constexpr (V == 8) {
+        const auto kern = h.D % 8 == 0 ? norm_stats_kernel<TX, V, true> : norm_stats_kernel<TX, V, false>;
+        hipLaunchKernelGGL(kern, grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, lanes);
+    } else
+        hipLaunchKernelGGL((norm_stats_kernel<TX, V, false>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, lanes);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * 16 + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
 }
 
 template <typename TX, int V>
-static hipError_t forward(const NormShape &h, const NormForward &f, void *ws, hipStream_t s, const char **name) {
-    const NormGrid g = norm_grid(h, 2048);
-    const TX *x = static_cast<const TX *>(f.x);
+static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream_t s, const char **name) {
+    const NormGrid g = norm_grid(h, kForwardBlocks);
     float2 *parts = static_cast<float2 *>(ws);
     float2 *stats = f.stats ? reinterpret_cast<float2 *>(f.stats) : parts + (size_t)h.N * g.chunks * norm_parts(h, g);
-    const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
-    hipLaunchKernelGGL((norm_stats_kernel<TX, V>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, group_lanes(g.TY * (h.D < kSlab ? h.D : kSlab)));
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * 16 + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
+    f.past = (size_t)h.N * h.P * h.C * (f.y_dtype == GSPC_F32 ? 4 : 2) >= kPastCaches;
+    HeldGrid held;
+    const bool hold = plan_held(h, sizeof(TX), held_most<TX>(), &held);
+    if (f.y_dtype != GSPC_I8 && !f.saved && hold) {
+        *name = "norm_held";
+        if (f.y_dtype == GSPC_F32) run_held<TX, float, V>(h, held, f, reinterpret_cast<float2 *>(f.stats), s);
+        else run_held<TX, uint16_t, V>(h, held, f, reinterpret_cast<float2 *>(f.stats), s);
+        return hipGetLastError();
+    }
+    if (hold) run_held<TX, void, V>(h, held, f, stats, s);
+    else launch_stats<TX, V>(h, g, f, parts, stats, s);
     if (f.y_dtype == GSPC_I8) {
         *name = "norm_rows<i8>";
         if (f.saved) launch_rows<TX, int8_t, V, true>(h, f, stats, s);
@@ -282,12 +460,14 @@ static hipError_t forward(const NormShape &h, const NormForward &f, void *ws, hi
         else launch_rows<TX, uint16_t, V, true>(h, f, stats, s);
     } else {
         *name = "norm_apply";
+        const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
+        const TX *x = static_cast<const TX *>(f.x);
         if (f.y_dtype == GSPC_F32)
             hipLaunchKernelGGL((norm_apply_kernel<TX, float, V>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, stats, f.gamma, f.beta,
-                               static_cast<float *>(f.y), f.ldy);
+                               static_cast<float *>(f.y), f.ldy, f.past);
         else
             hipLaunchKernelGGL((norm_apply_kernel<TX, uint16_t, V>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, stats, f.gamma, f.beta,
-                               static_cast<uint16_t *>(f.y), f.ldy);
+                               static_cast<uint16_t *>(f.y), f.ldy, f.past);
     }
     return hipGetLastError();
 }

@@ -5,6 +5,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "divide.h"
 
 namespace gspc {
@@ -44,6 +46,12 @@ template <> struct RawOf<uint16_t, 8> { typedef Raw16 type; };
 template <> struct RawOf<int8_t, 8> { typedef Raw8 type; };
 template <typename T, int V> using Raw = typename RawOf<T, V>::type;
 
+// Element `off` bytes beyond an address that is the same for the whole wave: the form that needs one register of address.
+template <typename T> __device__ __forceinline__ T *beyond(T *base, unsigned off) {
+    typedef typename std::conditional<std::is_const<T>::value, const char, char>::type byte;
+    return reinterpret_cast<T *>(reinterpret_cast<byte *>(base) + off);
+}
+
 // Loads stay raw until they are used, so that several can be in flight.
 template <int V> __device__ __forceinline__ Raw<float, V> fetch(const float *p) {
     if constexpr (V == 1) return *p;
@@ -57,6 +65,23 @@ template <int V> __device__ __forceinline__ Raw<int8_t, V> fetch(const int8_t *p
     if constexpr (V == 1) return *p;
     else return {*reinterpret_cast<const u32x2_any *>(p)};
 }
+// Nothing computed from r before is used after: values that are held raw over several passes are widened anew in each (kept
+// wide they would take twice the registers).
+__device__ __forceinline__ void hold(Raw32 &r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
+__device__ __forceinline__ void hold(Raw16 &r) { asm volatile("" : "+v"(r.a)); }
+__device__ __forceinline__ void hold(Raw8 &r) { asm volatile("" : "+v"(r.a)); }
+template <typename T> __device__ __forceinline__ void hold(T &) {}
+
+__device__ __forceinline__ void keep_if(Raw32 &r, bool yes) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.a[e] = yes ? r.a[e] : 0.f, r.b[e] = yes ? r.b[e] : 0.f;
+}
+__device__ __forceinline__ void keep_if(Raw16 &r, bool yes) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.a[e] = yes ? r.a[e] : 0u;
+}
+template <typename T> __device__ __forceinline__ void keep_if(T &r, bool yes) { r = yes ? r : T(0); }
+
 __device__ __forceinline__ void widen(const Raw32 &r, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = r.a[e], v[4 + e] = r.b[e];
@@ -71,14 +96,24 @@ __device__ __forceinline__ void widen(const Raw8 &r, float (&v)[8]) {
 }
 template <typename T> __device__ __forceinline__ void widen(const T &r, float (&v)[1]) { v[0] = as_float(r); }
 
-__device__ __forceinline__ void store(float *p, const float (&v)[8]) {
-    *reinterpret_cast<f32x4_any *>(p) = (f32x4){v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_any *>(p + 4) = (f32x4){v[4], v[5], v[6], v[7]};
+// past: beyond the caches (a non-temporal store), for outputs that are too large to be found there by whoever reads them next.
+template <typename T> __device__ __forceinline__ void store_vector(T *p, T v, bool past) {
+    if (past) {
+        asm volatile("");           // (two stores that differ in their hint alone would be merged, without it)
+        __builtin_nontemporal_store(v, p);
+        asm volatile("");
+    } else
+        *p = v;
 }
-__device__ __forceinline__ void store(uint16_t *p, const float (&v)[8]) {
-    *reinterpret_cast<u32x4_any *>(p) = (u32x4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+__device__ __forceinline__ void store(float *p, const float (&v)[8], bool past = false) {
+    store_vector(reinterpret_cast<f32x4_any *>(p), (f32x4_any){v[0], v[1], v[2], v[3]}, past);
+    store_vector(reinterpret_cast<f32x4_any *>(p + 4), (f32x4_any){v[4], v[5], v[6], v[7]}, past);
 }
-template <typename T> __device__ __forceinline__ void store(T *p, const float (&v)[1]) { put(p, v[0]); }
+__device__ __forceinline__ void store(uint16_t *p, const float (&v)[8], bool past = false) {
+    const u32x4_any r = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    store_vector(reinterpret_cast<u32x4_any *>(p), r, past);
+}
+template <typename T> __device__ __forceinline__ void store(T *p, const float (&v)[1], bool = false) { put(p, v[0]); }
 
 // A row of C channels in vectors of V: vector i starts at channel 8 i, the last one at C - 8, so that it ends with the row.
 // Its first overlap(i) channels belong to the vector before it too: both write them, with the same values, and sums over
@@ -86,14 +121,33 @@ template <typename T> __device__ __forceinline__ void store(T *p, const float (&
 template <int V> __device__ __forceinline__ int vector_start(int i, int C) { return V == 1 ? i : min(i * V, C - V); }
 template <int V> __host__ __device__ __forceinline__ int vectors_of(int C) { return (C + V - 1) / V; }
 
-// Sum, maximum over the `width` lanes (a power of two) that hold one row's parts; every one of them gets it.
-__device__ __forceinline__ float lanes_sum(float v, int width) {
-    for (int d = width / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
+// A reduction over groups of `width` lanes (a power of two, the same for the whole wave); every lane gets its group's result.
+// Within 16 lanes by DPP operands, beyond by the row swaps: a step is two instructions without a trip through LDS.
+template <typename T, typename F> __device__ __forceinline__ T lanes_reduce(T v, int width, const F &f) {
+    const auto dpp = [](T x, auto ctrl) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    if (width >= 2) v = f(v, dpp(v, std::integral_constant<int, 0xb1>{}));      // quad_perm: lane ^ 1
+    if (width >= 4) v = f(v, dpp(v, std::integral_constant<int, 0x4e>{}));      // quad_perm: lane ^ 2
+    if (width >= 8) v = f(v, dpp(v, std::integral_constant<int, 0x141>{}));     // row_half_mirror: the other four of eight
+    if (width >= 16) v = f(v, dpp(v, std::integral_constant<int, 0x140>{}));    // row_mirror: the other eight of a row
+    if (width >= 32) {
+        const unsigned u = __builtin_bit_cast(unsigned, v);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);    // the other row of two
+        v = f(__builtin_bit_cast(T, (unsigned)r[0]), __builtin_bit_cast(T, (unsigned)r[1]));
+    }
+    if (width >= 64) {
+        const unsigned u = __builtin_bit_cast(unsigned, v);
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);    // the other half of the wave
+        v = f(__builtin_bit_cast(T, (unsigned)r[0]), __builtin_bit_cast(T, (unsigned)r[1]));
+    }
     return v;
 }
-__device__ __forceinline__ float lanes_max(float v, int width) {
-    for (int d = width / 2; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+__device__ __forceinline__ float lanes_sum(float v, int width) {
+    return lanes_reduce(v, width, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ unsigned lanes_umax(unsigned v, int width) {
+    return lanes_reduce(v, width, [](unsigned a, unsigned b) { return max(a, b); });
 }
 
 // ---- 8-bit rows: q = rint(x * (127 / a)) to even, a = max |x| of the row; x is read back as q * (a / 127) ------------------
@@ -102,10 +156,6 @@ __host__ __device__ constexpr int rows8_pitch(int cols) { return (cols + 15) / 1
 // |v| as a number that orders like an integer, infinity above every finite value and NaN above infinity: one maximum over a
 // row says how large it is and whether all of it is finite.
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-__device__ __forceinline__ unsigned lanes_umax(unsigned v, int width) {
-    for (int d = width / 2; d > 0; d /= 2) v = max(v, (unsigned)__shfl_xor((int)v, d));
-    return v;
-}
 
 struct RowCode {
     float up, inv, scale;
@@ -159,7 +209,7 @@ template <int ACT> __device__ __forceinline__ float slope(float z) {
     if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
     if constexpr (ACT == kActSilu) {
         const float s = sigmoid(z);
-        return s + z * s * (1.f - s);
+        return fmaf(s, fmaf(-s, z, z), s);                        // s + s z (1 - s)
     }
     return 1.f;
 }

@@ -1,6 +1,7 @@
 // Entry points of the channels-last operators: their arguments are checked here, on the host, before anything is launched.
 #include <cmath>
 
+#include "divide.h"
 #include "tokens_internal.h"
 
 namespace {
@@ -45,7 +46,7 @@ int check_norm(int N, int P, int C, int groups, int act, gspc::NormShape *h) {
     if (groups <= 0 || C % groups) return fail(GSPC_ERR_GROUPS, "C=%d must be divisible by groups=%d", C, groups);
     if (act != GSPC_ACT_NONE && act != GSPC_ACT_RELU && act != GSPC_ACT_SILU) return fail(GSPC_ERR_ARG, "unknown activation %d", act);
     if ((int64_t)N * groups > kMaxRows / 64) return fail(GSPC_ERR_DIM, "N * groups = %lld", (long long)N * groups);
-    *h = {N, P, C, groups, C / groups, act};
+    *h = {N, P, C, groups, C / groups, act, gspc::div_magic(C / groups)};
     return GSPC_OK;
 }
 
@@ -132,7 +133,7 @@ int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma,
     if (!x || !y || (codes && !y_scale) || (saved && !saved_scale)) return fail(GSPC_ERR_NULL, "null pointer argument");
     if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_forward_bytes(h)))) return rc;
     const gspc::NormForward f = {x, x_dtype, (size_t)ldx, gamma, beta, eps, y, y_dtype, (size_t)ldy, y_scale, stats,
-                                 static_cast<int8_t *>(saved), saved_scale};
+                                 static_cast<int8_t *>(saved), saved_scale, 0};
     const char *name = "";
     const hipError_t e = gspc::launch_norm_forward(h, f, workspace, gspc::current_stream(), &name);
     gspc::set_last_kernel(name);
@@ -156,7 +157,7 @@ int gspc_group_norm_backward(const void *dy, int dy_dtype, int64_t lddy, const v
     }
     if (codes) ldx = gspc_rows8_pitch(C);
     const gspc::NormBackward b = {dy, dy_dtype, (size_t)lddy, x, x_dtype, (size_t)ldx, x_scale, stats, gamma, beta,
-                                  dx, (size_t)lddx, dgamma, dbeta};
+                                  dx, (size_t)lddx, dgamma, dbeta, 0};
     const char *name = "";
     const hipError_t e = gspc::launch_norm_backward(h, b, workspace, gspc::current_stream(), &name);
     gspc::set_last_kernel(name);

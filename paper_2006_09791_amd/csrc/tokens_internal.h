@@ -20,6 +20,7 @@ hipError_t launch_dequantize_rows(const int8_t *q, const float *scale, size_t ro
 // Group norm.  Rows of the tensors are tokens, ldX elements apart; image n is the rows n P .. (n + 1) P - 1.
 struct NormShape {
     int N, P, C, groups, D, act;    // D = C / groups
+    unsigned m_D;                   // div_magic(D)
 };
 struct NormForward {
     const void *x;
@@ -34,6 +35,7 @@ struct NormForward {
     float *stats;                   // [N][groups][2]: mean, 1 / standard deviation
     int8_t *saved;                  // x as 8-bit rows, or nullptr
     float *saved_scale;
+    int past;                       // y is stored past the caches (set by the launch)
 };
 struct NormBackward {
     const void *dy;
@@ -47,6 +49,7 @@ struct NormBackward {
     void *dx;
     size_t lddx;
     float *dgamma, *dbeta;          // either may be nullptr
+    int past;                       // dx is stored past the caches (set by the launch)
 };
 size_t norm_forward_bytes(const NormShape &h);
 size_t norm_backward_bytes(const NormShape &h);
