@@ -107,9 +107,6 @@ __device__ __forceinline__ void held_group_sums(const HeldGrid &g, const float *
     }
 }
 
-// Bytes of an output from which on it is stored past the caches: what reads it next finds nothing of it there anyway.
-constexpr size_t kPastCaches = 32u << 20;
-
 // Such blocks for segments of `groups` groups and up to `threads` threads that hold up to `held` vectors each, or false.
 inline bool held_grid(const NormShape &h, int groups, int threads, int held, HeldGrid *g) {
     g->seg = groups * h.D;

@@ -14,6 +14,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_at(const void *p, size_t
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)(bytes < kMostBytes ? bytes : kMostBytes), kRsrc);
 }
 
+// Waits until at most LEFT of the wave's loads are under way, and for all of its LDS operations.
+template <int LEFT> __device__ __forceinline__ void wait_loads() {
+    static_assert(LEFT < 64, "six bits");
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
+}
+
 struct ProductArgs {
     const int8_t *a, *w;
     const float *a_scale, *w_scale, *bias;
@@ -21,6 +27,7 @@ struct ProductArgs {
     size_t M, ldo;
     int N, pitch;
     unsigned mtiles, ntiles;
+    int past;               // out is stored past the caches
 };
 
 // Four consecutive outputs of one token.
@@ -46,9 +53,10 @@ __device__ __forceinline__ void channel_terms(const ProductArgs &p, int n, float
 }
 
 // ---- few tokens or few outputs: no staging --------------------------------------------------------------------------------------
-// A block has 16 TN channels x 16 TM tokens; its waves take k-steps of 64 in turn, operands straight from memory into the
-// registers of v_mfma_i32_16x16x64_i8 (channels are the rows, tokens the columns of its result), and join their sums in LDS.
-template <typename T, int TN, int TM, int WAVES>
+// A block has 16 TN channels x 16 TM tokens; its waves split the reduction into stretches, operands straight from memory into the
+// registers of v_mfma_i32_16x16x64_i8 (channels are the rows, tokens the columns of its result), DEEP steps of 64 in flight, and join
+// their sums in LDS.
+template <typename T, int TN, int TM, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void product8_small_kernel(ProductArgs p) {
     __shared__ i32x4 s_part[WAVES][TN * TM][kWave];
     const unsigned nt = blockIdx.x % p.ntiles, mt = blockIdx.x / p.ntiles;
@@ -57,153 +65,269 @@ __global__ __launch_bounds__(64 * WAVES) void product8_small_kernel(ProductArgs 
     const size_t m0 = (size_t)mt * 16 * TM;
     const __amdgpu_buffer_rsrc_t rw = bytes_at(p.w + (size_t)n0 * p.pitch, (size_t)(p.N - n0) * p.pitch);
     const __amdgpu_buffer_rsrc_t ra = bytes_at(p.a + m0 * p.pitch, (p.M - m0) * p.pitch);
-    const unsigned row = lane % 16, col = lane / 16 * 16;
-    i32x4 acc[TN][TM] = {};
-    for (int k = wave * 64; k < p.pitch; k += WAVES * 64) {
-        const unsigned at = row * p.pitch + k + col;
-        const bool in = k + (int)col < p.pitch;
-        i32x4 w[TN], a[TM];
+    const unsigned row = lane % 16, col = lane / 16 * 16, lane_off = row * p.pitch + col;
+    const int steps = (p.pitch + 63) / 64, share = (steps + WAVES - 1) / WAVES;
+    const int first = wave * share, last = min(first + share, steps);
+    i32x4 acc[TN][TM] = {}, w[DEEP][TN], a[DEEP][TM];
+    const auto load = [&](int d, int step) {        // (out of range past the row's end)
+        const int k = step * 64;
+        const unsigned off = k + (int)col < p.pitch ? lane_off + k : kOob;
 #pragma unroll
         for (int i = 0; i < TN; ++i)
-            w[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, in ? at + i * 16 * p.pitch : kOob, 0, 0));
+            w[d][i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off == kOob ? kOob : off + i * 16 * p.pitch, 0, 0));
 #pragma unroll
         for (int j = 0; j < TM; ++j)
-            a[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, in ? at + j * 16 * p.pitch : kOob, 0, 0));
+            a[d][j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off == kOob ? kOob : off + j * 16 * p.pitch, 0, 0));
+    };
+    const auto multiply = [&](int d) {
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], a[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[d][i], a[d][j], acc[i][j], 0, 0, 0);
+    };
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d)
+        if (first + d < last) load(d, first + d);
+    for (int step = first; step < last; step += DEEP) {
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d)
+            if (step + d < last) {
+                multiply(d);
+                if (step + d + DEEP < last) load(d, step + d + DEEP);
+            }
     }
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
         for (int j = 0; j < TM; ++j) s_part[wave][i * TM + j][lane] = acc[i][j];
-    __syncthreads();
-    for (int t = threadIdx.x; t < TN * TM * kWave; t += 64 * WAVES) {
+    // (the scales travel while the waves wait for one another)
+    const auto terms = [&](int t, float (&scale)[4], float (&bias)[4], float &sa, size_t &m, int &n) {
         const int tile = t / kWave, l = t % kWave;
-        i32x4 sum = s_part[0][tile][l];
+        m = m0 + tile % TM * 16 + l % 16;
+        n = n0 + tile / TM * 16 + l / 16 * 4;
+        channel_terms(p, n, scale, bias);
+        sa = p.a_scale[m < p.M ? m : p.M - 1];
+    };
+    constexpr int EACH = (TN * TM + WAVES - 1) / WAVES;
+    float scale[EACH][4], bias[EACH][4], sa[EACH];
+    size_t m[EACH];
+    int n[EACH];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += s_part[v][tile][l];
-        const size_t m = m0 + tile % TM * 16 + l % 16;
-        const int n = n0 + tile / TM * 16 + l / 16 * 4;
-        if (m < p.M && n < p.N) {
-            float scale[4], bias[4], v[4];
-            channel_terms(p, n, scale, bias);
-            const float sa = p.a_scale[m];
+    for (int e = 0; e < EACH; ++e)
+        if ((e * WAVES + wave) < TN * TM) terms(e * 64 * WAVES + threadIdx.x, scale[e], bias[e], sa[e], m[e], n[e]);
+    __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * sa * scale[e] + bias[e];
-            put4<T>(p, m, n, v);
+    for (int e = 0; e < EACH; ++e) {
+        const int tile = e * WAVES + wave;
+        if (tile >= TN * TM) break;
+        i32x4 sum = s_part[0][tile][lane];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) sum += s_part[v][tile][lane];
+        if (m[e] < p.M && n[e] < p.N) {
+            float v[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = (float)sum[c] * sa[e] * scale[e][c] + bias[e][c];
+            put4<T>(p, m[e], n[e], v);
         }
     }
 }
 
-// ---- many tokens: tiles through LDS ---------------------------------------------------------------------------------------------
-constexpr int kStep = 128;              // bytes of a row that one stage holds
+// Workgroups go to the eight XCDs in turn.  Each XCD gets consecutive tiles, and these run through bands of kBand tiles of tokens,
+// so that the 32 tiles that an XCD works on together share rows of both operands in its L2.
+constexpr unsigned kBand = 8;
+__device__ __forceinline__ uint2 tile_of(const ProductArgs &p, unsigned b) {
+    const unsigned tiles = p.mtiles * p.ntiles, each = tiles / 8, more = tiles % 8, xcd = b & 7;
+    const unsigned t = xcd * each + min(xcd, more) + (b >> 3);
+    const unsigned band = t / (kBand * p.ntiles), first = band * kBand, high = min(kBand, p.mtiles - first);
+    const unsigned in = t - band * kBand * p.ntiles;
+    return make_uint2(first + in % high, in / high);
+}
 
-// WM x WN waves of TM x TN products 32x32x32 each.  A stage holds 128 bytes of BM + BN rows, brought by loads that write LDS
-// directly (16 bytes a lane, eight rows a wave), while the other stage is multiplied.  Within a row the 16-byte pieces are
-// permuted by the row's number, so that the lanes that read one column of pieces spread over all banks; a load's lanes fetch
-// from the addresses that this asks for.
-template <typename T, int WM, int WN, int TM, int TN>
+// ---- many tokens: tiles through LDS ---------------------------------------------------------------------------------------------
+constexpr int kStep = 128;              // bytes of a row that one stage holds: a cache line (stages of 64 bytes, twice as many of
+                                        // them, make two requests of a line: 8192 x 4096 x 8192 took 285 us)
+
+// WM x WN waves of TM x TN products 32x32x32 each.  STAGES stages hold 128 bytes of BM + BN rows each, brought by loads that write
+// LDS directly (16 bytes a lane, eight rows a wave), STAGES - 1 ahead of the products.  Within a row the 16-byte pieces are permuted by the row's number, so that the
+// lanes that read one column of pieces spread over all banks; a load's lanes fetch from the addresses that this asks for.
+template <typename T, int WM, int WN, int TM, int TN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs p) {
     constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES;
-    static_assert(ROWS % (8 * WAVES) == 0, "whole loads");
-    __shared__ char stage0[ROWS * kStep], stage1[ROWS * kStep];
+    constexpr int STAGE = ROWS * kStep;
+    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "a load is of one operand");
+    __shared__ __attribute__((aligned(16))) char stages[STAGES * STAGE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const unsigned mt = blockIdx.x / p.ntiles, nt = blockIdx.x % p.ntiles;
-    const size_t m0 = (size_t)mt * BM;
-    const int n0 = nt * BN;
+    const uint2 tile = tile_of(p, blockIdx.x);
+    const size_t m0 = (size_t)tile.x * BM;
+    const int n0 = tile.y * BN;
     const __amdgpu_buffer_rsrc_t ra = bytes_at(p.a + m0 * p.pitch, (p.M - m0) * p.pitch);
     const __amdgpu_buffer_rsrc_t rw = bytes_at(p.w + (size_t)n0 * p.pitch, (size_t)(p.N - n0) * p.pitch);
     const auto swizzle = [](int row) { return (row & 7) ^ (row >> 3 & 1); };
 
-    const auto load = [&](char *stage, int k) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int base = (i * WAVES + wave) * 8, row = base + lane / 8, piece = (lane % 8) ^ swizzle(row);
-            const int at = k + piece * 16;
-            const bool tokens = base < BM;
-            const unsigned off = at < p.pitch ? (unsigned)(tokens ? row : row - BM) * p.pitch + at : kOob;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(tokens ? ra : rw, (__attribute__((address_space(3))) void *)(stage + base * kStep), 16,
-                                                     off, 0, 0, 0);
-        }
+    // Load i of this wave: rows base .. base + 7; lane l has the piece that belongs into its place of row base + l / 8.
+    const int piece[2] = {(lane & 7) ^ swizzle(lane >> 3), (lane & 7) ^ swizzle(8 + (lane >> 3))};
+    const unsigned lane_off = (unsigned)(lane / 8) * p.pitch;
+    const auto load_one = [&](unsigned stage, int k, int i) {
+        const bool tokens = i < BM / (8 * WAVES);
+        const int base = (i * WAVES + wave) * 8, at = k + piece[wave & 1] * 16;     // (WAVES is even)
+        // (out of range past the row's end, from the lane's own offset on: no branch, which would make two loads of one)
+        const unsigned past = at < p.pitch ? 0u : kOob;
+        const unsigned off = (lane_off + at + (unsigned)(base - (tokens ? 0 : BM)) * p.pitch) | past;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(tokens ? ra : rw, (__attribute__((address_space(3))) void *)(stages + stage + base * kStep), 16,
+                                                 off, 0, 0, 0);
     };
     i32x16 acc[TM][TN] = {};
-    const int wm = wave / WN * TM * 32, wn = BM + wave % WN * TN * 32, r = lane % 32, half = lane / 32;
-    const auto multiply = [&](const char *stage) {
-#pragma unroll
-        for (int k = 0; k < kStep / 32; ++k) {
-            i32x4 a[TM], w[TN];
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-                a[i] = *reinterpret_cast<const i32x4 *>(stage + (wm + i * 32 + r) * kStep + (((2 * k + half) ^ swizzle(r)) * 16));
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-                w[j] = *reinterpret_cast<const i32x4 *>(stage + (wn + j * 32 + r) * kStep + (((2 * k + half) ^ swizzle(r)) * 16));
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j], a[i], acc[i][j], 0, 0, 0);
-        }
+    const int wm = wave / WN * TM * 32, wn = wave % WN * TN * 32, r = lane % 32, half = lane / 32;
+    constexpr int PARTS = kStep / 32, READS = TM + TN;
+    i32x4 op[2][READS];                             // operands of this part of a stage, and of the next: tokens, channels
+    const auto read_one = [&](unsigned stage, int k, int i) {
+        const int row = i < TM ? wm + i * 32 : BM + wn + (i - TM) * 32;
+        return *reinterpret_cast<const i32x4 *>(stages + stage + (row + r) * kStep + ((2 * k + half) ^ swizzle(r)) * 16);
     };
-    const auto wait = [] {
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-    };
-    load(stage0, 0);
-    for (int k = 0; k < p.pitch; k += 2 * kStep) {
-        wait();
-        if (k + kStep < p.pitch) load(stage1, k + kStep);
-        multiply(stage0);
-        wait();
-        if (k + 2 * kStep < p.pitch) load(stage0, k + 2 * kStep);
-        if (k + kStep < p.pitch) multiply(stage1);
+
+    constexpr int SCALES = ((BM > BN ? BM : BN) + 64 * WAVES - 1) / (64 * WAVES);
+    float w_scale[SCALES], bias[SCALES], a_scale[SCALES];
+#pragma unroll
+    for (int i = 0; i < SCALES; ++i) {
+        const int t = i * 64 * WAVES + threadIdx.x, n = min(n0 + t, p.N - 1);
+        const size_t m = m0 + t < p.M ? m0 + t : p.M - 1;
+        w_scale[i] = p.w_scale[n];
+        bias[i] = p.bias ? p.bias[n] : 0.f;
+        a_scale[i] = p.a_scale[m];
     }
-    // channels are the rows of a product: a lane has one token and four consecutive channels in each of four places
+    // A stage in parts of 32 bytes of a row.  While a part is multiplied the next part's operands are read, channels first: a part
+    // begins with one token's products.  Before the next stage's are read that has to be there, and every wave has all of this one
+    // in registers: what comes STAGES later is loaded into its place, FIRST loads there and the others behind the next stage's
+    // first products, as evenly as products allow: a wave that waits for the memory path to take its load multiplies nothing.
+    // (That wait stands behind the last part's first products, not before.)
+    constexpr int SLOTS = READS, SKIP = READS / 4, FIRST = (LOADS + 1) / 2;
+    const auto share = [](int all, int slots, int t) { return all * t / slots; };     // of `all`, those before slot t of `slots`
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int t = 0; t < STAGES; ++t)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int n = n0 + wn - BM + j * 32 + 8 * q + 4 * half;
-            if (n >= p.N) continue;
-            float scale[4], bias[4];
-            channel_terms(p, n, scale, bias);
+        for (int i = 0; i < (t + 1 < STAGES ? LOADS : FIRST); ++i) load_one(t * STAGE, t * kStep, i);
+    wait_loads<(STAGES - 2) * LOADS + FIRST>();
+    __builtin_amdgcn_s_barrier();
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const size_t m = m0 + wm + i * 32 + r;
-                if (m >= p.M) continue;
-                const float sa = p.a_scale[m];
-                float v[4];
+    for (int t = 0; t < READS; ++t) op[0][t] = read_one(0, 0, t);
+    unsigned stage = 0, before = (STAGES - 1) * STAGE;      // of step k, and of the one before, where k + STAGES - 1 comes
+    for (int k = 0; k < p.pitch; k += kStep) {
+        const unsigned next = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][4 * q + e] * sa * scale[e] + bias[e];
-                put4<T>(p, m, n, v);
+        for (int q = 0; q < PARTS; ++q) {
+            const bool last = q == PARTS - 1;
+#pragma unroll
+            for (int t = 0; t < SLOTS; ++t) {
+                if (last && t == SKIP) {
+                    wait_loads<(STAGES - 2) * LOADS>();
+                    __builtin_amdgcn_s_barrier();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const int s = last ? t - SKIP : t, slots = last ? SLOTS - SKIP : SLOTS;
+                if (s >= 0) {
+#pragma unroll
+                    for (int u = share(READS, slots, s); u < share(READS, slots, s + 1); ++u) {
+                        const int o = u < TN ? TM + u : u - TN;
+                        op[(q + 1) & 1][o] = last ? read_one(next, 0, o) : read_one(stage, q + 1, o);
+                    }
+                    if (q == 0)
+#pragma unroll
+                        for (int u = share(LOADS - FIRST, slots, s); u < share(LOADS - FIRST, slots, s + 1); ++u)
+                            load_one(before, k + (STAGES - 1) * kStep, FIRST + u);
+                    if (last)
+#pragma unroll
+                        for (int u = share(FIRST, slots, s); u < share(FIRST, slots, s + 1); ++u) load_one(stage, k + STAGES * kStep, u);
+                }
+#pragma unroll
+                for (int c = share(TM * TN, SLOTS, t); c < share(TM * TN, SLOTS, t + 1); ++c)
+                    acc[c / TN][c % TN] =
+                        __builtin_amdgcn_mfma_i32_32x32x32_i8(op[q & 1][TM + c % TN], op[q & 1][c / TN], acc[c / TN][c % TN], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        before = stage;
+        stage = next;
+    }
+    __builtin_amdgcn_s_waitcnt(0);                  // (loads of zeros past the end)
+    // Channels are the rows of a product: a lane has one token and four consecutive channels in each of four places.  Each wave
+    // turns its own 32 tokens at a time through LDS (in the stages' place, which nobody reads any more), so that a store writes whole
+    // lines of a token; so do the scales, loaded before the products.
+    constexpr int WAVE_N = TN * 32, PITCH = WAVE_N * sizeof(T) + 16, LANES = WAVE_N * sizeof(T) / 16, EACH = 16 / sizeof(T);
+    static_assert(WAVES * 32 * PITCH + 4 * (2 * BN + BM) <= STAGES * STAGE, "fits the stages");
+    __syncthreads();
+    float *s_scale = reinterpret_cast<float *>(stages), *s_bias = s_scale + BN, *s_token = s_bias + BN;
+#pragma unroll
+    for (int i = 0; i < SCALES; ++i) {
+        const int t = i * 64 * WAVES + threadIdx.x;
+        if (t < BN) s_scale[t] = w_scale[i], s_bias[t] = bias[i];
+        if (t < BM) s_token[t] = a_scale[i];
+    }
+    __syncthreads();
+    char *turn = stages + 4 * (2 * BN + BM) + wave * 32 * PITCH;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const float sa = s_token[wm + i * 32 + r];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = j * 32 + 8 * q + 4 * half;
+                const f32x4 sw = *reinterpret_cast<const f32x4 *>(s_scale + wn + n), sb = *reinterpret_cast<const f32x4 *>(s_bias + wn + n);
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][4 * q + e] * sa * sw[e] + sb[e];
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(turn + r * PITCH + n * 4) = (f32x4){v[0], v[1], v[2], v[3]};
+                else *reinterpret_cast<u32x2 *>(turn + r * PITCH + n * 2) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            }
+        __builtin_amdgcn_wave_barrier();            // (LDS operations of one wave are in order)
+#pragma unroll
+        for (int t = 0; t < 32; t += kWave / LANES) {
+            const int row = t + lane / LANES, n = lane % LANES * EACH;
+            const size_t m = m0 + wm + i * 32 + row;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(turn + row * PITCH + lane % LANES * 16);
+            if (m < p.M) {
+                T *o = static_cast<T *>(p.out) + m * p.ldo + n0 + wn + n;
+                const int left = p.N - n0 - wn - n;
+                if (left >= EACH) store_vector(reinterpret_cast<u32x4_any *>(o), v, p.past);
+                else {
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e)
+                        if (e < left) {
+                            if constexpr (sizeof(T) == 4) o[e] = __uint_as_float(v[e]);
+                            else o[e] = (uint16_t)(v[e / 2] >> (e % 2 * 16));
+                        }
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------------
 template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t s, const char **name) {
-    ProductArgs p{in.a, in.w, in.a_scale, in.w_scale, in.bias, in.out, in.M, in.ldo, in.N, rows8_pitch(in.K), 0, 0};
+    ProductArgs p{in.a, in.w, in.a_scale, in.w_scale, in.bias, in.out, in.M, in.ldo, in.N, rows8_pitch(in.K), 0, 0, in.M * in.N * sizeof(T) >= kPastCaches};
     const auto tiles = [&](int bm, int bn) {
         p.mtiles = (unsigned)((in.M + bm - 1) / bm);
         p.ntiles = (in.N + bn - 1) / bn;
         return (unsigned long long)p.mtiles * p.ntiles;
     };
-    if (tiles(128, 128) >= 256) {
-        if (tiles(256, 256) >= 256) {
-            *name = "product8_tile<256,256>";
-            hipLaunchKernelGGL((product8_tile_kernel<T, 2, 4, 4, 2>), dim3((unsigned)tiles(256, 256)), dim3(512), 0, s, p);
-        } else {
-            *name = "product8_tile<128,128>";
-            hipLaunchKernelGGL((product8_tile_kernel<T, 2, 2, 2, 2>), dim3((unsigned)tiles(128, 128)), dim3(256), 0, s, p);
-        }
-    } else if (in.M <= 16) {
-        *name = "product8_small<1,1>";
-        hipLaunchKernelGGL((product8_small_kernel<T, 1, 1, 8>), dim3((unsigned)tiles(16, 16)), dim3(512), 0, s, p);
-    } else {
-        *name = "product8_small<2,2>";
-        hipLaunchKernelGGL((product8_small_kernel<T, 2, 2, 4>), dim3((unsigned)tiles(32, 32)), dim3(256), 0, s, p);
-    }
+    const auto run = [&](auto kern, int bm, int bn, int threads, const char *n) {
+        const unsigned blocks = (unsigned)tiles(bm, bn);
+        *name = n;
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), 0, s, p);
+    };
+    // The largest tile that still gives most compute units one (M x N x K, us; both sides):
+    //   256 x 256 from 160 tiles on: 12544 x 1024 x 512 has 196, 15.0 against 17.1 in tiles of 128; 2048 x 4096 x 2048 has 128, 27.8
+    //   against 22.4;
+    //   128 x 128 from 256 tiles on: 2048 x 4096 x 2048 has 512, 22.4 against 29 in 64 x 128; 512 x 4096 x 4096 has 128, 18.3 against 15.8;
+    //   64 x 128 where 32 x 32 without staging would be more than one block for each compute unit: 512 x 4096 x 4096, 15.8 against
+    //   59; 200 x 1024 x 1024 (224 blocks without staging), 5.9 against 4.4.
+    // Up to 16 tokens: 1 x 4096 x 4096, 5.7 in blocks of 16 channels and eight waves, 7.2 in blocks of 32 x 32.
+    if (tiles(256, 256) >= 160) run(product8_tile_kernel<T, 2, 4, 4, 2, 2>, 256, 256, 512, "product8_tile<256,256>");
+    else if (tiles(128, 128) >= 256) run(product8_tile_kernel<T, 2, 2, 2, 2, 2>, 128, 128, 256, "product8_tile<128,128>");
+    else if (in.M <= 16) run(product8_small_kernel<T, 1, 1, 8, 8>, 16, 16, 512, "product8_small<1,1>");
+    else if (tiles(32, 32) <= 256) run(product8_small_kernel<T, 2, 2, 8, 4>, 32, 32, 512, "product8_small<2,2>");
+    else run(product8_tile_kernel<T, 2, 2, 1, 2, 3>, 64, 128, 256, "product8_tile<64,128>");
     return hipGetLastError();
 }
 

@@ -96,21 +96,23 @@ __device__ __forceinline__ void widen(const Raw8 &r, float (&v)[8]) {
 }
 template <typename T> __device__ __forceinline__ void widen(const T &r, float (&v)[1]) { v[0] = as_float(r); }
 
-// past: beyond the caches (a non-temporal store), for outputs that are too large to be found there by whoever reads them next.
-template <typename T> __device__ __forceinline__ void store_vector(T *p, T v, bool past) {
+// past: beyond the caches (a non-temporal store), for outputs of kPastCaches bytes and more, too large to be found there by whoever
+// reads them next.
+constexpr size_t kPastCaches = 32u << 20;
+__device__ __forceinline__ void store_vector(u32x4_any *p, u32x4 v, bool past) {
     if (past) {
         asm volatile("");           // (two stores that differ in their hint alone would be merged, without it)
-        __builtin_nontemporal_store(v, p);
+        __builtin_nontemporal_store((u32x4_any)v, p);
         asm volatile("");
     } else
         *p = v;
 }
 __device__ __forceinline__ void store(float *p, const float (&v)[8], bool past = false) {
-    store_vector(reinterpret_cast<f32x4_any *>(p), (f32x4_any){v[0], v[1], v[2], v[3]}, past);
-    store_vector(reinterpret_cast<f32x4_any *>(p + 4), (f32x4_any){v[4], v[5], v[6], v[7]}, past);
+    store_vector(reinterpret_cast<u32x4_any *>(p), __builtin_bit_cast(u32x4, (f32x4){v[0], v[1], v[2], v[3]}), past);
+    store_vector(reinterpret_cast<u32x4_any *>(p + 4), __builtin_bit_cast(u32x4, (f32x4){v[4], v[5], v[6], v[7]}), past);
 }
 __device__ __forceinline__ void store(uint16_t *p, const float (&v)[8], bool past = false) {
-    const u32x4_any r = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    const u32x4 r = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
     store_vector(reinterpret_cast<u32x4_any *>(p), r, past);
 }
 template <typename T> __device__ __forceinline__ void store(T *p, const float (&v)[1], bool = false) { put(p, v[0]); }
