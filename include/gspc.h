@@ -264,9 +264,11 @@ int gspc_dequantize_rows(const void *q, const float *scale, int64_t rows, int co
 /* Activation of a group norm.  SILU is z / (1 + exp(-z)). */
 enum { GSPC_ACT_NONE = 0, GSPC_ACT_RELU = 1, GSPC_ACT_SILU = 2 };
 
-/* Device memory that the two calls below need while they run, on any stream.  0 on
- * invalid arguments, and where there is no work. */
-size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int backward);
+/* Device memory that a call of gspc_group_norm (rows8 != 0: one that writes 8-bit rows, as y or
+ * as saved) or gspc_group_norm_backward needs while it runs.  0 where it needs none (its
+ * workspace may then be NULL), and on invalid arguments. */
+size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int x_dtype, int rows8);
+size_t gspc_group_norm_backward_workspace_bytes(int N, int P, int C, int groups, int dy_dtype, int x_dtype);
 
 /* y = act(gamma * (x - mean) / sqrt(var + eps) + beta) over N images of P tokens of C channels; mean and (biased) variance
  * are those of the P * C / groups values of a group of one image.
@@ -275,7 +277,8 @@ size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int back
  *   stats       : dev fp32 [N][groups][2], receives mean and 1 / sqrt(var + eps) for the gradient, or NULL
  *   saved       : receives x as 8-bit rows, with saved_scale, in the same pass: what a training step keeps
  *                 of x for the gradient; or NULL
- *   workspace   : dev, 16-byte aligned, at least gspc_group_norm_workspace_bytes(..., 0); not initialised */
+ *   workspace   : dev, 16-byte aligned, as large as said above (GSPC_ERR_SPACE if it is too small; a call that is
+ *                 given stats needs none of it for these); not initialised */
 int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma, const float *beta, int N, int P, int C,
                     int groups, float eps, int act, void *y, int y_dtype, int64_t ldy, float *y_scale, float *stats,
                     void *saved, float *saved_scale, void *workspace, size_t workspace_bytes);

@@ -29,7 +29,7 @@ EXPORTS = [
     "gspc_packed_info", "gspc_pack_input_bf16", "gspc_conv2d_grouped", "gspc_force_path",
     "gspc_last_path", "gspc_last_kernel", "gspc_set_graph_mode", "gspc_set_chain_fusion", "gspc_set_winograd", "gspc_run_layer_chain",
     "gspc_rows8_pitch", "gspc_pack_channels_last", "gspc_unpack_channels_last", "gspc_quantize_rows", "gspc_dequantize_rows",
-    "gspc_group_norm_workspace_bytes", "gspc_group_norm", "gspc_group_norm_backward", "gspc_matmul_i8",
+    "gspc_group_norm_workspace_bytes", "gspc_group_norm_backward_workspace_bytes", "gspc_group_norm", "gspc_group_norm_backward", "gspc_matmul_i8",
 ]
 
 
@@ -51,6 +51,7 @@ class GspcLayer(ctypes.Structure):
 _thread = threading.local()     # stream: the library's, as gspc_set_stream was last given it
 _lib = None
 _conv = None     # gspc_conv2d_grouped through _gspc_call, or _no_conv
+_fast = None     # _gspc_call with the channels-last operators, or _NoFast
 
 
 def _no_conv(*args):
@@ -58,9 +59,14 @@ def _no_conv(*args):
     return NotImplemented
 
 
+class _NoFast:
+    """Every call of a channels-last operator is one that only ctypes converts."""
+    pack = unpack = quantize = dequantize = norm = norm_backward = matmul = staticmethod(_no_conv)
+
+
 def load():
     """Loads libgspc.so (must have been built in-tree) and sets prototypes."""
-    global _lib, _conv
+    global _lib, _conv, _fast
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -69,7 +75,7 @@ def load():
             "(there is no fallback path)")
     # torch first: it brings the HIP runtime whose streams and allocations are
     # handed to the library, and libgspc.so must bind to that same runtime.
-    import torch  # noqa: F401
+    import torch
     lib = ctypes.CDLL(LIB_PATH)
     i, vp, sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
     ip = ctypes.POINTER(ctypes.c_int)
@@ -117,8 +123,8 @@ def load():
     lib.gspc_quantize_rows.argtypes = [vp, i, ll, ll, i, vp, vp]
     lib.gspc_dequantize_rows.restype = i
     lib.gspc_dequantize_rows.argtypes = [vp, vp, ll, i, vp, i, ll]
-    lib.gspc_group_norm_workspace_bytes.restype = sz
-    lib.gspc_group_norm_workspace_bytes.argtypes = [i] * 5
+    lib.gspc_group_norm_workspace_bytes.restype = lib.gspc_group_norm_backward_workspace_bytes.restype = sz
+    lib.gspc_group_norm_workspace_bytes.argtypes = lib.gspc_group_norm_backward_workspace_bytes.argtypes = [i] * 6
     lib.gspc_group_norm.restype = i
     lib.gspc_group_norm.argtypes = [vp, i, ll, vp, vp, i, i, i, i, f, i, vp, i, ll, vp, vp, vp, vp, vp, sz]
     lib.gspc_group_norm_backward.restype = i
@@ -128,10 +134,13 @@ def load():
     try:
         from . import _gspc_call
     except ImportError:          # not built for this interpreter
-        _conv = _no_conv
+        _conv, _fast = _no_conv, _NoFast
     else:
         _gspc_call.bind(ctypes.cast(lib.gspc_conv2d_grouped, vp).value)
-        _conv = _gspc_call.conv
+        _gspc_call.bind_tokens(*[ctypes.cast(f, vp).value for f in (
+            lib.gspc_pack_channels_last, lib.gspc_unpack_channels_last, lib.gspc_quantize_rows, lib.gspc_dequantize_rows, lib.gspc_group_norm,
+            lib.gspc_group_norm_backward, lib.gspc_matmul_i8)], torch.float32, torch.bfloat16, torch.int8)
+        _conv, _fast = _gspc_call.conv, _gspc_call
     _lib = lib
     return lib
 
@@ -400,6 +409,15 @@ def _new_rows8(rows, cols, device):
     return (_empty((rows, gspc_rows8_pitch(cols)), torch.int8, device), _empty((rows,), torch.float32, device))
 
 
+def _done(rc):
+    """Whether the call through _gspc_call was made; its error is raised."""
+    if rc is NotImplemented:
+        return False
+    if rc:
+        _check(rc)
+    return True
+
+
 def _change_layout(call, x, out, dtype, pack):
     _on_gpu(x, "x")
     if x.dim() < 3 or not x.is_contiguous():
@@ -420,16 +438,22 @@ def _change_layout(call, x, out, dtype, pack):
 
 def gspc_pack_channels_last(x, out=None, dtype=GSPC_BF16):
     """x [N, C, ...] (planes) -> [N, P, C] (tokens), P the pixels of a plane."""
+    if out is not None and _fast is not None and _done(_fast.pack(x, out)):
+        return out
     return _change_layout(load().gspc_pack_channels_last, x, out, dtype, True)
 
 
 def gspc_unpack_channels_last(x, out=None, dtype=GSPC_F32):
     """x [N, ..., C] (tokens) -> [N, C, P] (planes)."""
+    if out is not None and _fast is not None and _done(_fast.unpack(x, out)):
+        return out
     return _change_layout(load().gspc_unpack_channels_last, x, out, dtype, False)
 
 
 def gspc_quantize_rows(x, out=None):
     """x [..., cols] -> 8-bit rows (q [rows, pitch], scale [rows]); `out`: such a pair to write into."""
+    if out is not None and _fast is not None and _done(_fast.quantize(x, out)):
+        return out
     lib = load()
     ld, cols = _row_stride(x, "x"), x.shape[-1]
     if cols == 0:
@@ -444,6 +468,8 @@ def gspc_quantize_rows(x, out=None):
 
 def gspc_dequantize_rows(rows8, cols, out=None, dtype=GSPC_F32):
     """8-bit rows of `cols` values -> [rows, cols]; `out`: a tensor [..., cols] to write into."""
+    if out is not None and _fast is not None and _done(_fast.dequantize(rows8, cols, out)):
+        return out
     lib = load()
     rows = rows8[1].numel()
     q, scale = _rows8(rows8, rows, cols, "rows8")
@@ -455,8 +481,12 @@ def gspc_dequantize_rows(rows8, cols, out=None, dtype=GSPC_F32):
     return out
 
 
-def gspc_group_norm_workspace_bytes(N, P, C, groups, backward=False):
-    return int(load().gspc_group_norm_workspace_bytes(N, P, C, groups, 1 if backward else 0))
+def gspc_group_norm_workspace_bytes(N, P, C, groups, x_dtype, rows8=False):
+    return int(load().gspc_group_norm_workspace_bytes(N, P, C, groups, x_dtype, 1 if rows8 else 0))
+
+
+def gspc_group_norm_backward_workspace_bytes(N, P, C, groups, dy_dtype, x_dtype):
+    return int(load().gspc_group_norm_backward_workspace_bytes(N, P, C, groups, dy_dtype, x_dtype))
 
 
 def _tokens(x, what):
@@ -468,19 +498,25 @@ def _tokens(x, what):
     return N, P, C
 
 
-def _workspace(workspace, N, P, C, groups, backward, device):
+def _workspace(workspace, need, device):
+    """(address, bytes) of the caller's workspace, or of one of `need` bytes, and the tensor behind it."""
     import torch
     if workspace is None:
-        workspace = _empty((gspc_group_norm_workspace_bytes(N, P, C, groups, backward),), torch.uint8, device)
-    _on_gpu(workspace, "workspace")
-    if not workspace.is_contiguous():
+        if not need:
+            return None, 0, None
+        workspace = _empty((need,), torch.int8, device)
+    elif not _on_gpu(workspace, "workspace").is_contiguous():
         raise GspcError(-8, "workspace must be contiguous")
-    return workspace, workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def gspc_group_norm(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, out=None, dtype=None, stats=None, saved=None, workspace=None):
     """x [N, ..., C] -> y of x's shape (type: `dtype`, by default x's), or 8-bit rows of it where `dtype` is GSPC_I8 or `out` is
     a pair.  stats: fp32 [N, groups, 2] to write mean and 1 / sqrt(var + eps) to; saved: 8-bit rows to write x to."""
+    if out is not None and workspace is None and _fast is not None:
+        rc = _fast.norm(x, gamma, beta, groups, eps, act, out, stats, saved)
+        if rc != -6 and _done(rc):          # (GSPC_ERR_SPACE: a call that needs a workspace)
+            return out
     import torch
     lib = load()
     N, P, C = _tokens(x, "x")
@@ -492,15 +528,21 @@ def gspc_group_norm(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, out=None, dt
         _same_shape(out, x.shape, "out")
         y, y_scale, kind, ldy = out.data_ptr(), None, _dtype(out, "out"), _row_stride(out, "out")
     q, scale = (None, None) if saved is None else _rows8(saved, N * P, C, "saved")
-    ws, ws_bytes = _workspace(workspace, N, P, C, groups, False, x.device)
-    _check(lib.gspc_group_norm(x.data_ptr(), _dtype(x, "x"), _row_stride(x, "x"), _flat(gamma, torch.float32, C, "gamma"),
+    x_kind = _dtype(x, "x")
+    ws, ws_bytes, held = _workspace(workspace, workspace is None and gspc_group_norm_workspace_bytes(
+        N, P, C, groups, x_kind, kind == GSPC_I8 or saved is not None), x.device)
+    _check(lib.gspc_group_norm(x.data_ptr(), x_kind, _row_stride(x, "x"), _flat(gamma, torch.float32, C, "gamma"),
                                _flat(beta, torch.float32, C, "beta"), N, P, C, groups, eps, act, y, kind, ldy, y_scale,
-                               _flat(stats, torch.float32, N * groups * 2, "stats"), q, scale, ws.data_ptr(), ws_bytes))
+                               _flat(stats, torch.float32, N * groups * 2, "stats"), q, scale, ws, ws_bytes))
     return out
 
 
 def gspc_group_norm_backward(dy, x, stats, gamma, beta, groups, act=ACT_NONE, dx=None, dgamma=None, dbeta=None, workspace=None):
     """dy [N, ..., C], x of its shape or 8-bit rows of it -> (dx, dgamma, dbeta), dx of dy's type."""
+    if dx is not None and dgamma is not None and dbeta is not None and _fast is not None:
+        rc = _fast.norm_backward(dy, x, stats, gamma, beta, groups, act, dx, dgamma, dbeta, workspace)
+        if (workspace is not None or rc != -6) and _done(rc):       # (GSPC_ERR_SPACE: a call that needs a workspace)
+            return dx, dgamma, dbeta
     import torch
     lib = load()
     N, P, C = _tokens(dy, "dy")
@@ -518,17 +560,21 @@ def gspc_group_norm_backward(dy, x, stats, gamma, beta, groups, act=ACT_NONE, dx
         dgamma = _empty((C,), torch.float32, dy.device)
     if dbeta is None:
         dbeta = _empty((C,), torch.float32, dy.device)
-    ws, ws_bytes = _workspace(workspace, N, P, C, groups, True, dy.device)
-    _check(lib.gspc_group_norm_backward(dy.data_ptr(), _dtype(dy, "dy"), _row_stride(dy, "dy"), px, kind, ldx, x_scale,
+    dy_kind = _dtype(dy, "dy")
+    ws, ws_bytes, held = _workspace(workspace, workspace is None and gspc_group_norm_backward_workspace_bytes(
+        N, P, C, groups, dy_kind, kind), dy.device)
+    _check(lib.gspc_group_norm_backward(dy.data_ptr(), dy_kind, _row_stride(dy, "dy"), px, kind, ldx, x_scale,
                                         _flat(stats, torch.float32, N * groups * 2, "stats"), _flat(gamma, torch.float32, C, "gamma"),
                                         _flat(beta, torch.float32, C, "beta"), N, P, C, groups, act, dx.data_ptr(), _row_stride(dx, "dx"),
                                         _flat(dgamma, torch.float32, C, "dgamma"), _flat(dbeta, torch.float32, C, "dbeta"),
-                                        ws.data_ptr(), ws_bytes))
+                                        ws, ws_bytes))
     return dx, dgamma, dbeta
 
 
 def gspc_matmul_i8(a, w, bias=None, out=None, dtype=GSPC_BF16):
     """8-bit rows a (M tokens) and w (N filters) of the same length -> [M, N]; `out`: a tensor [..., N] to write into."""
+    if out is not None and _fast is not None and _done(_fast.matmul(a, w, bias, out)):
+        return out
     import torch
     lib = load()
     K, M, N = a[0].shape[-1], a[1].numel(), w[1].numel()

@@ -341,15 +341,25 @@ __global__ __launch_bounds__(512, 4) void norm_grad_held_kernel(NormShape h, Hel
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 constexpr int kBackwardBlocks = 2048;
 
-size_t norm_backward_bytes(const NormShape &h) {
-    const NormGrid g = norm_grid(h, kBackwardBlocks);
-    return ((size_t)h.N * g.chunks * 2 * h.C + (size_t)h.N * 2 * h.C + (size_t)h.N * h.groups * 2) * sizeof(float);
-}
-
 // Four vectors a thread where that can be, else eight where x and dy take 64 registers then.
 template <typename TX, typename TG> constexpr int grad_held_most() { return sizeof(TX) == 4 || sizeof(TG) == 4 ? 4 : 8; }
 template <typename TX, typename TG> static bool plan_grad_held(const NormShape &h, HeldGrid *g) {
     return plan_held(h, sizeof(TG), 4, g) || (grad_held_most<TX, TG>() > 4 && plan_held(h, sizeof(TG), 8, g));
+}
+
+template <typename TX, typename TG> static size_t backward_bytes(const NormShape &h) {
+    HeldGrid held;
+    const bool hold = plan_grad_held<TX, TG>(h, &held);
+    if (hold && h.N == 1) return 0;
+    const size_t sums = (size_t)h.N * 2 * h.C * sizeof(float);
+    if (hold) return sums;
+    return sums + ((size_t)h.N * norm_grid(h, kBackwardBlocks).chunks * 2 * h.C + (size_t)h.N * h.groups * 2) * sizeof(float);
+}
+
+size_t norm_backward_bytes(const NormShape &h, int dy_dtype, int x_dtype) {
+    if (dy_dtype == GSPC_F32)
+        return x_dtype == GSPC_F32 ? backward_bytes<float, float>(h) : x_dtype == GSPC_BF16 ? backward_bytes<uint16_t, float>(h) : backward_bytes<int8_t, float>(h);
+    return x_dtype == GSPC_F32 ? backward_bytes<float, uint16_t>(h) : x_dtype == GSPC_BF16 ? backward_bytes<uint16_t, uint16_t>(h) : backward_bytes<int8_t, uint16_t>(h);
 }
 
 template <typename TX, typename TG, int V, int E>
@@ -395,8 +405,9 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
         return hipGetLastError();
     }
     const NormGrid g = norm_grid(h, kBackwardBlocks);
-    float *parts = static_cast<float *>(ws), *sums = parts + (size_t)h.N * g.chunks * 2 * h.C;
+    float *sums = static_cast<float *>(ws);
     float2 *ab = reinterpret_cast<float2 *>(sums + (size_t)h.N * 2 * h.C);
+    float *parts = reinterpret_cast<float *>(ab + (size_t)h.N * h.groups);
     b.past = (size_t)h.N * h.P * h.C * sizeof(TG) >= kPastCaches;
     HeldGrid held;
     const bool hold = plan_grad_held<TX, TG>(h, &held);

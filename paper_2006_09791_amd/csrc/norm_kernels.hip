@@ -372,12 +372,6 @@ __global__ __launch_bounds__(512) void norm_held_kernel(NormShape h, HeldGrid g,
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 constexpr int kForwardBlocks = 2048;
 
-static size_t forward_bytes(const NormShape &h, const NormGrid &g) {
-    return (size_t)h.N * g.chunks * norm_parts(h, g) * sizeof(float2) + (size_t)h.N * h.groups * sizeof(float2);
-}
-
-size_t norm_forward_bytes(const NormShape &h) { return forward_bytes(h, norm_grid(h, kForwardBlocks)); }
-
 template <typename TX, typename TY, int V, bool SAVE>
 static void launch_rows(const NormShape &h, const NormForward &f, const float2 *stats, hipStream_t s) {
     const int nv = vectors_of<V>(h.C);
@@ -434,11 +428,22 @@ static void launch_stats(const NormShape &h, const NormGrid &g, const NormForwar
     hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * 16 + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
 }
 
+// Statistics of the caller's that it did not ask for, and the parts of two-launch ones.
+size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8) {
+    HeldGrid held;
+    const bool hold = x_dtype == GSPC_F32 ? plan_held(h, 4, held_most<float>(), &held) : plan_held(h, 2, held_most<uint16_t>(), &held);
+    if (hold && !rows8) return 0;
+    const size_t stats = (size_t)h.N * h.groups * sizeof(float2);
+    if (hold) return stats;
+    const NormGrid g = norm_grid(h, kForwardBlocks);
+    return stats + (size_t)h.N * g.chunks * norm_parts(h, g) * sizeof(float2);
+}
+
 template <typename TX, int V>
 static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream_t s, const char **name) {
     const NormGrid g = norm_grid(h, kForwardBlocks);
-    float2 *parts = static_cast<float2 *>(ws);
-    float2 *stats = f.stats ? reinterpret_cast<float2 *>(f.stats) : parts + (size_t)h.N * g.chunks * norm_parts(h, g);
+    float2 *stats = f.stats ? reinterpret_cast<float2 *>(f.stats) : static_cast<float2 *>(ws);
+    float2 *parts = static_cast<float2 *>(ws) + (size_t)h.N * h.groups;
     f.past = (size_t)h.N * h.P * h.C * (f.y_dtype == GSPC_F32 ? 4 : 2) >= kPastCaches;
     HeldGrid held;
     const bool hold = plan_held(h, sizeof(TX), held_most<TX>(), &held);

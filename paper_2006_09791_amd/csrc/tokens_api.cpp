@@ -52,7 +52,7 @@ int check_norm(int N, int P, int C, int groups, int act, gspc::NormShape *h) {
 
 int check_workspace(const void *ws, size_t given, size_t needed) {
     if (given < needed) return fail(GSPC_ERR_SPACE, "workspace holds %zu bytes, %zu needed", given, needed);
-    if (!ws) return fail(GSPC_ERR_NULL, "null workspace");
+    if (needed && !ws) return fail(GSPC_ERR_NULL, "null workspace");
     if (misaligned(ws, 16)) return fail(GSPC_ERR_ARG, "workspace must be 16-byte aligned");
     return GSPC_OK;
 }
@@ -111,10 +111,18 @@ int gspc_dequantize_rows(const void *q, const float *scale, int64_t rows, int co
                 "dequantize launch");
 }
 
-size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int backward) {
+size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int x_dtype, int rows8) {
     gspc::NormShape h;
     if (check_norm(N, P, C, groups, GSPC_ACT_NONE, &h) || (int64_t)N * P == 0) return 0;
-    return backward ? gspc::norm_backward_bytes(h) : gspc::norm_forward_bytes(h);
+    if (!dense(x_dtype)) return fail(GSPC_ERR_DTYPE, "unknown dtype %d", x_dtype), 0;
+    return gspc::norm_forward_bytes(h, x_dtype, rows8 != 0);
+}
+
+size_t gspc_group_norm_backward_workspace_bytes(int N, int P, int C, int groups, int dy_dtype, int x_dtype) {
+    gspc::NormShape h;
+    if (check_norm(N, P, C, groups, GSPC_ACT_NONE, &h) || (int64_t)N * P == 0) return 0;
+    if (!dense(dy_dtype) || (!dense(x_dtype) && x_dtype != GSPC_I8)) return fail(GSPC_ERR_DTYPE, "unknown dtype (%d, %d)", dy_dtype, x_dtype), 0;
+    return gspc::norm_backward_bytes(h, dy_dtype, x_dtype);
 }
 
 int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma, const float *beta, int N, int P, int C, int groups,
@@ -131,7 +139,7 @@ int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma,
     if (misaligned(stats, 8)) return fail(GSPC_ERR_ARG, "stats must be 8-byte aligned");
     if ((int64_t)N * P == 0) return GSPC_OK;
     if (!x || !y || (codes && !y_scale) || (saved && !saved_scale)) return fail(GSPC_ERR_NULL, "null pointer argument");
-    if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_forward_bytes(h)))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_forward_bytes(h, x_dtype, (codes || saved) && !stats)))) return rc;
     const gspc::NormForward f = {x, x_dtype, (size_t)ldx, gamma, beta, eps, y, y_dtype, (size_t)ldy, y_scale, stats,
                                  static_cast<int8_t *>(saved), saved_scale, 0};
     const char *name = "";
@@ -153,7 +161,7 @@ int gspc_group_norm_backward(const void *dy, int dy_dtype, int64_t lddy, const v
     if (misaligned(stats, 8)) return fail(GSPC_ERR_ARG, "stats must be 8-byte aligned");
     if ((int64_t)N * P > 0) {
         if (!dy || !x || !dx || !stats || (codes && !x_scale)) return fail(GSPC_ERR_NULL, "null pointer argument");
-        if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_backward_bytes(h)))) return rc;
+        if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_backward_bytes(h, dy_dtype, x_dtype)))) return rc;
     }
     if (codes) ldx = gspc_rows8_pitch(C);
     const gspc::NormBackward b = {dy, dy_dtype, (size_t)lddy, x, x_dtype, (size_t)ldx, x_scale, stats, gamma, beta,

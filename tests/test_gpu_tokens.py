@@ -437,7 +437,8 @@ def block_inputs(torch, b, seed, N=3, C=48, P=70, cols=33):
 def block_buffers(torch, b, N=3, C=48, P=70, cols=33):
     e = lambda *s, t=torch.float32: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
     rows8 = lambda: (e(N * P, b.gspc_rows8_pitch(C), t=torch.int8), e(N * P))  # noqa: E731
-    size = b.gspc_group_norm_workspace_bytes(N, P, C, 6, True) + b.gspc_group_norm_workspace_bytes(N, P, C, 6, False)
+    size = max(b.gspc_group_norm_workspace_bytes(N, P, C, 6, b.GSPC_BF16, True),
+               b.gspc_group_norm_backward_workspace_bytes(N, P, C, 6, b.GSPC_BF16, b.GSPC_I8))
     return {"tokens": e(N, P, C, t=torch.bfloat16), "y": e(N, P, C, t=torch.bfloat16), "stats": e(N, 6, 2), "saved": rows8(), "q": rows8(),
             "dx": e(N, P, C, t=torch.bfloat16), "dg": e(C), "db": e(C), "out": e(N, P, cols, t=torch.bfloat16), "planes": e(N, cols, P),
             "ws": e(size, t=torch.uint8)}

@@ -50,13 +50,13 @@ def test_rows_refusals():
 
 def test_norm_refusals():
     lib = b.load()
-    need = lib.gspc_group_norm_workspace_bytes(2, 9, 32, 4, 0)
+    need = lib.gspc_group_norm_workspace_bytes(1, 70000, 8, 1, 0, 0)
     assert need > 0
     # x, dtype, ldx, gamma, beta, N, P, C, groups, eps, act, y, dtype, ldy, y_scale, stats, saved, saved_scale, workspace, bytes
-    good = [P, 0, 32, P, P, 2, 9, 32, 4, 1e-5, 0, P, 0, 32, None, None, None, None, P, need]
-    bad = [(0, None, NULL), (0, ODD4, ARG), (1, 2, DTYPE), (2, 31, DIM), (3, ODD4, ARG), (5, -1, DIM), (6, -1, DIM), (7, 0, DIM),
+    good = [P, 0, 32, P, P, 1, 70000, 8, 1, 1e-5, 0, P, 0, 32, None, None, None, None, P, need]
+    bad = [(0, None, NULL), (0, ODD4, ARG), (1, 2, DTYPE), (2, 7, DIM), (3, ODD4, ARG), (5, -1, DIM), (6, -1, DIM), (7, 0, DIM),
            (8, 5, GROUPS), (8, 0, GROUPS), (9, 0.0, ARG), (9, float("nan"), ARG), (9, float("inf"), ARG), (9, -1.0, ARG), (10, 3, ARG),
-           (11, None, NULL), (11, ODD4, ARG), (12, 9, DTYPE), (13, 16, DIM), (15, ODD4, ARG), (16, P, NULL), (16, ODD8, ARG),
+           (11, None, NULL), (11, ODD4, ARG), (12, 9, DTYPE), (13, 7, DIM), (15, ODD4, ARG), (16, P, NULL), (16, ODD8, ARG),
            (18, None, NULL), (18, ODD8, ARG), (19, need - 1, SPACE)]
     for at, value, code in bad:
         args = list(good)
@@ -75,7 +75,7 @@ def test_norm_refusals():
 
 def test_norm_backward_refusals():
     lib = b.load()
-    need = lib.gspc_group_norm_workspace_bytes(2, 9, 32, 4, 1)
+    need = lib.gspc_group_norm_backward_workspace_bytes(2, 9, 32, 4, 0, 0)
     assert need > 0
     # dy, dtype, lddy, x, dtype, ldx, x_scale, stats, gamma, beta, N, P, C, groups, act, dx, lddx, dgamma, dbeta, workspace, bytes
     good = [P, 0, 32, P, 0, 32, None, P, P, P, 2, 9, 32, 4, 0, P, 32, P, P, P, need]
@@ -90,9 +90,17 @@ def test_norm_backward_refusals():
 
 def test_workspace_sizes():
     lib = b.load()
-    assert lib.gspc_group_norm_workspace_bytes(0, 9, 32, 4, 0) == lib.gspc_group_norm_workspace_bytes(2, 0, 32, 4, 1) == 0
-    assert lib.gspc_group_norm_workspace_bytes(2, 9, 32, 5, 0) == 0 and "divisible" in b.gspc_last_error()
-    assert lib.gspc_group_norm_workspace_bytes(65536, 65536, 8, 1, 0) == 0 and "tokens" in b.gspc_last_error()
+    forward, backward = lib.gspc_group_norm_workspace_bytes, lib.gspc_group_norm_backward_workspace_bytes
+    assert forward(0, 9, 32, 4, 0, 0) == backward(2, 0, 32, 4, 0, 0) == 0
+    assert forward(2, 9, 32, 5, 0, 0) == 0 and "divisible" in b.gspc_last_error()
+    assert backward(65536, 65536, 8, 1, 0, 0) == 0 and "tokens" in b.gspc_last_error()
+    assert forward(2, 9, 32, 4, 2, 0) == 0 and "dtype" in b.gspc_last_error()
+    assert backward(2, 9, 32, 4, 2, 0) == backward(2, 9, 32, 4, 0, 3) == 0
+    # images that a block holds: nothing but the statistics behind 8-bit rows, and sums of several images
+    assert forward(2, 9, 32, 4, 0, 0) == 0 and forward(2, 9, 32, 4, 0, 1) == 2 * 4 * 8
+    assert backward(1, 9, 32, 4, 0, 0) == 0 and backward(2, 9, 32, 4, 1, 2) == 2 * 2 * 32 * 4
+    # images that it does not hold: parts of the sums as well
+    assert forward(1, 70000, 8, 1, 0, 0) > 8 and backward(1, 70000, 8, 1, 0, 0) > 2 * 8 * 4
 
 
 def test_product_refusals():
