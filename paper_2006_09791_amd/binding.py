@@ -326,15 +326,26 @@ def _empty(shape, dtype, device):
     """A tensor for the library's stream: torch reuses its memory after work of that stream only."""
     import torch
     stream = getattr(_thread, "stream", 0)
-    if stream == torch.cuda.current_stream(device).cuda_stream:
+    if stream == _current_stream(device):
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _dtypes():
+def _current_stream(device):
     import torch
-    return {torch.float32: GSPC_F32, torch.bfloat16: GSPC_BF16}
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # a twentieth of the time of a Stream object
+    return raw(device.index) if raw is not None and device.index is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+_DTYPES = {}
+
+
+def _dtypes():
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: GSPC_F32, torch.bfloat16: GSPC_BF16})
+    return _DTYPES
 
 
 def _dtype(t, what):
@@ -498,13 +509,17 @@ def _tokens(x, what):
     return N, P, C
 
 
+def _scratch(nbytes, device):
+    import torch
+    return _empty((nbytes,), torch.int8, device)
+
+
 def _workspace(workspace, need, device):
     """(address, bytes) of the caller's workspace, or of one of `need` bytes, and the tensor behind it."""
-    import torch
     if workspace is None:
         if not need:
             return None, 0, None
-        workspace = _empty((need,), torch.int8, device)
+        workspace = _scratch(need, device)
     elif not _on_gpu(workspace, "workspace").is_contiguous():
         raise GspcError(-8, "workspace must be contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
@@ -513,9 +528,13 @@ def _workspace(workspace, need, device):
 def gspc_group_norm(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, out=None, dtype=None, stats=None, saved=None, workspace=None):
     """x [N, ..., C] -> y of x's shape (type: `dtype`, by default x's), or 8-bit rows of it where `dtype` is GSPC_I8 or `out` is
     a pair.  stats: fp32 [N, groups, 2] to write mean and 1 / sqrt(var + eps) to; saved: 8-bit rows to write x to."""
-    if out is not None and workspace is None and _fast is not None:
-        rc = _fast.norm(x, gamma, beta, groups, eps, act, out, stats, saved)
-        if rc != -6 and _done(rc):          # (GSPC_ERR_SPACE: a call that needs a workspace)
+    if out is not None and _fast is not None:
+        rc = _fast.norm(x, gamma, beta, groups, eps, act, out, stats, saved, workspace)
+        if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
+            N, P, C = _tokens(x, "x")
+            need = gspc_group_norm_workspace_bytes(N, P, C, groups, _dtype(x, "x"), isinstance(out, tuple) or saved is not None)
+            rc = _fast.norm(x, gamma, beta, groups, eps, act, out, stats, saved, _scratch(need, x.device))
+        if _done(rc):
             return out
     import torch
     lib = load()
@@ -541,7 +560,11 @@ def gspc_group_norm_backward(dy, x, stats, gamma, beta, groups, act=ACT_NONE, dx
     """dy [N, ..., C], x of its shape or 8-bit rows of it -> (dx, dgamma, dbeta), dx of dy's type."""
     if dx is not None and dgamma is not None and dbeta is not None and _fast is not None:
         rc = _fast.norm_backward(dy, x, stats, gamma, beta, groups, act, dx, dgamma, dbeta, workspace)
-        if (workspace is not None or rc != -6) and _done(rc):       # (GSPC_ERR_SPACE: a call that needs a workspace)
+        if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
+            N, P, C = _tokens(dy, "dy")
+            need = gspc_group_norm_backward_workspace_bytes(N, P, C, groups, _dtype(dy, "dy"), GSPC_I8 if isinstance(x, tuple) else _dtype(x, "x"))
+            rc = _fast.norm_backward(dy, x, stats, gamma, beta, groups, act, dx, dgamma, dbeta, _scratch(need, dy.device))
+        if _done(rc):
             return dx, dgamma, dbeta
     import torch
     lib = load()

@@ -157,39 +157,55 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape h, int ch
     if (lane == 0) ab[pair] = make_float2(a / m, b / m);
 }
 
-// dgamma and dbeta: 64 channels a block, its waves take the images in turn.
-constexpr int kParamWaves = 16;
-__global__ __launch_bounds__(kParamWaves * kWave) void norm_grad_params_kernel(NormShape h, const float *__restrict__ sums,
-                                                                               float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    __shared__ float s_sum[2][kParamWaves][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+// dgamma and dbeta: 64 channels a block, its waves (MOST at most) take the rows of sums ([rows][2][C]: of images, or of their parts)
+// in turn.
+template <int MOST>
+__device__ __forceinline__ void sum_params(int C, int block, int rows, const float *__restrict__ sums, float *__restrict__ dgamma,
+                                           float *__restrict__ dbeta) {
+    __shared__ float s_sum[2][MOST][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave, c = block * kWave + lane;
     float sz = 0.f, sx = 0.f;
-    if (c < h.C) {
+    if (c < C) {
 #pragma unroll 8
-        for (int n = wave; n < h.N; n += kParamWaves) sz += sums[(size_t)n * 2 * h.C + c], sx += sums[((size_t)n * 2 + 1) * h.C + c];
+        for (int n = wave; n < rows; n += waves) sz += sums[(size_t)n * 2 * C + c], sx += sums[((size_t)n * 2 + 1) * C + c];
     }
     s_sum[0][wave][lane] = sz;
     s_sum[1][wave][lane] = sx;
     __syncthreads();
-    if (wave < 2 && c < h.C) {
+    for (int which = wave; which < 2; which += waves) {
+        if (c >= C) continue;
         float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kParamWaves; ++w) sum += s_sum[wave][w][lane];
-        if (wave == 0 && dbeta) dbeta[c] = sum;
-        if (wave == 1 && dgamma) dgamma[c] = sum;
+        for (int w = 0; w < waves; ++w) sum += s_sum[which][w][lane];
+        if (which == 0 && dbeta) dbeta[c] = sum;
+        if (which == 1 && dgamma) dgamma[c] = sum;
     }
 }
 
-template <typename TX, typename TG, int V, int E>
+constexpr int kParamWaves = 16;
+__global__ __launch_bounds__(kParamWaves * kWave) void norm_grad_params_kernel(int C, int rows, const float *__restrict__ sums,
+                                                                               float *__restrict__ dgamma, float *__restrict__ dbeta) {
+    sum_params<kParamWaves>(C, blockIdx.x, rows, sums, dgamma, dbeta);
+}
+
+// An image's groups whose A and B a block of norm_grad_apply_kernel takes from the parts itself, and the channels' sums behind them: in
+// small launches, where a third one costs more.
+constexpr int kFoldGroups = 64, kFoldSums = 4096, kFoldBlocks = 512;
+
+// The first param_blocks blocks sum the parameters' gradients, the others write dx.  FOLD: sums are the blocks' parts, and a block
+// takes its image's A and B from them (ab is not read).
+template <typename TX, typename TG, int V, int E, bool FOLD>
 __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape h, NormGrid g, const TG *__restrict__ dy, size_t lddy,
                                                                        const TX *__restrict__ x, size_t ldx,
                                                                        const float *__restrict__ x_scale, const float2 *__restrict__ stats,
                                                                        const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                        const float2 *__restrict__ ab, TG *__restrict__ dx, size_t lddx,
-                                                                       int past) {
+                                                                       int past, int param_blocks, int param_rows,
+                                                                       const float *__restrict__ sums, float *__restrict__ dgamma,
+                                                                       float *__restrict__ dbeta) {
     typedef GradBatch<TX, TG, V> Batch;
-    const NormBlock b = norm_block(h, g, blockIdx.x);
-    if (!b.active) return;
+    __shared__ float2 s_ab[FOLD ? kFoldGroups : 1];
+    if ((int)blockIdx.x < param_blocks) return sum_params<kNormThreads / kWave>(h.C, blockIdx.x, param_rows, sums, dgamma, dbeta);
+    const NormBlock b = norm_block(h, g, blockIdx.x - param_blocks);
     const size_t row0 = (size_t)b.n * h.P + b.r0;
     const TX *px = x + row0 * ldx + b.at;
     const TG *pg = dy + row0 * lddy + b.at;
@@ -197,12 +213,33 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape
     TG *pd = dx + row0 * lddx + b.at;
     const int rows = b.r1 - b.r0;
     Batch now, next;
-    now.load(px, ldx, pg, lddy, ps, b.ty, rows, g.TY);
+    if (b.active) now.load(px, ldx, pg, lddy, ps, b.ty, rows, g.TY);
+    if constexpr (FOLD) {
+        const int lane = threadIdx.x % kWave;
+        const float m = (float)h.P * (float)h.D, *part = sums + (size_t)b.n * g.chunks * 2 * h.C;
+        for (int k = threadIdx.x / kWave; k < h.groups; k += g.threads / kWave) {
+            float a = 0.f, bb = 0.f;
+            for (int j = lane; j < g.chunks * h.D; j += kWave) {
+                const int chunk = group_of(h, j), c = k * h.D + j - chunk * h.D;
+                const float w = gamma ? gamma[c] : 1.f, *p = part + (size_t)chunk * 2 * h.C + c;
+                a = fmaf(w, p[0], a);
+                bb = fmaf(w, p[h.C], bb);
+            }
+            a = lanes_sum(a, kWave);
+            bb = lanes_sum(bb, kWave);
+            if (lane == 0) s_ab[k] = make_float2(a / m, bb / m);
+        }
+        __syncthreads();
+    }
+    if (!b.active) return;
     GradAffine<V, E> f;
     load_grad_affine<V, E>(h, stats, gamma, beta, b.n, b.at, f);
     GradGroups<E> s;
 #pragma unroll
-    for (int e = 0; e < E; ++e) set_group(f, e, ab[(size_t)b.n * h.groups + group_of(h, b.at + e * (V / E))], s);
+    for (int e = 0; e < E; ++e) {
+        const int k = group_of(h, b.at + e * (V / E));
+        set_group(f, e, FOLD ? s_ab[k] : ab[(size_t)b.n * h.groups + k], s);
+    }
     for (int r = b.ty; r < rows; r += Batch::DEEP * g.TY) {
         next.load(px, ldx, pg, lddy, ps, r + Batch::DEEP * g.TY, rows, g.TY);
 #pragma unroll
@@ -383,13 +420,20 @@ static void launch_grad(const NormShape &h, const NormGrid &g, const NormBackwar
     const TG *dy = static_cast<const TG *>(b.dy);
     const float2 *stats = reinterpret_cast<const float2 *>(b.stats);
     const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
-    const int lanes = group_lanes(h.D, (long)h.N * h.groups, 1L << 20);
     hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TG, V, E>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
                        b.gamma, b.beta, parts);
+    const bool fold = h.groups <= kFoldGroups && (long)g.chunks * 2 * h.C <= kFoldSums && grid.x <= kFoldBlocks;
+    const unsigned param_blocks = b.dgamma || b.dbeta ? (h.C + kWave - 1) / kWave : 0;
+    const auto apply = [&](auto kern, int rows, const float *from) {
+        hipLaunchKernelGGL(kern, dim3(grid.x + param_blocks), dim3(g.threads), 0, s, h, g, dy,
+                           b.lddy, x, b.ldx, b.x_scale, stats, b.gamma, b.beta, ab, static_cast<TG *>(b.dx), b.lddx, b.past, (int)param_blocks,
+                           rows, from, b.dgamma, b.dbeta);
+    };
+    if (fold) return apply(norm_grad_apply_kernel<TX, TG, V, E, true>, h.N * g.chunks, parts);
+    const int lanes = group_lanes(h.D, (long)h.N * h.groups, 1L << 20);
     hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * lanes + 255) / 256)), dim3(256), 0, s, h, g.chunks,
                        lanes, parts, b.gamma, sums, ab);
-    hipLaunchKernelGGL((norm_grad_apply_kernel<TX, TG, V, E>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
-                       b.gamma, b.beta, ab, static_cast<TG *>(b.dx), b.lddx, b.past);
+    apply(norm_grad_apply_kernel<TX, TG, V, E, false>, h.N, sums);
 }
 
 template <typename TX, typename TG, int V>
@@ -398,10 +442,8 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
     const bool params = b.dgamma || b.dbeta;
     if ((long)h.N * h.P == 0) {                     // no tokens: zeros
         *name = "norm_grad_params";
-        NormShape none = h;
-        none.N = 0;
         if (params)
-            hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, none, (const float *)nullptr, b.dgamma, b.dbeta);
+            hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h.C, 0, (const float *)nullptr, b.dgamma, b.dbeta);
         return hipGetLastError();
     }
     const NormGrid g = norm_grid(h, kBackwardBlocks);
@@ -420,8 +462,8 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
     if (V == 8 && h.D % 8 == 0) run(std::integral_constant<int, 1>{});
     else if (V == 8 && h.D % 4 == 0) run(std::integral_constant<int, V == 8 ? 2 : 1>{});
     else run(std::integral_constant<int, V>{});
-    if (params && !(hold && h.N == 1))
-        hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h, sums, b.dgamma, b.dbeta);
+    if (params && hold && h.N > 1)
+        hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h.C, h.N, sums, b.dgamma, b.dbeta);
     return hipGetLastError();
 }
 

@@ -83,12 +83,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_stats_kernel(NormShape h, N
     }
 }
 
-// The blocks' parts joined: stats[n][g] = mean, 1 / sqrt(var + eps).  16 lanes for a group of an image.
-__global__ __launch_bounds__(256) void norm_join_kernel(NormShape h, NormGrid g, const float2 *__restrict__ parts, float eps,
-                                                        float2 *__restrict__ stats) {
-    const unsigned pair = (blockIdx.x * 256 + threadIdx.x) / 16, lane = threadIdx.x & 15;
-    if (pair >= (unsigned)h.N * h.groups) return;
-    const int n = pair / h.groups, k = pair - n * h.groups;
+// The blocks' parts of group k of image n joined by `lanes` lanes: mean, 1 / sqrt(var + eps).
+__device__ __forceinline__ float2 join_parts(const NormShape &h, const NormGrid &g, const float2 *__restrict__ parts, int n, int k, float eps,
+                                             int lane, int lanes) {
     const int s0 = (k * h.D) / kSlab, s1 = ((k + 1) * h.D - 1) / kSlab, count = (s1 - s0 + 1) * g.chunks;
     const float2 *p = parts + (size_t)n * g.chunks * norm_parts(h, g) + k;
     const auto weight = [&](int s, int chunk) {
@@ -97,20 +94,32 @@ __global__ __launch_bounds__(256) void norm_join_kernel(NormShape h, NormGrid g,
     };
     const float total = (float)h.P * (float)h.D;
     float mean = 0.f, dev = 0.f;
-    for (int i = lane; i < count; i += 16) {
-        const int s = s0 + i / g.chunks, chunk = i % g.chunks;
-        mean += p[chunk * norm_parts(h, g) + s].x * weight(s, chunk);
+    for (int i = lane; i < count; i += lanes) {
+        const int s = fast_div_any(i, g.chunks, g.m_chunks), chunk = i - s * g.chunks;
+        mean += p[chunk * norm_parts(h, g) + s0 + s].x * weight(s0 + s, chunk);
     }
-    mean = lanes_sum(mean, 16) / total;
-    for (int i = lane; i < count; i += 16) {
-        const int s = s0 + i / g.chunks, chunk = i % g.chunks;
-        const float2 v = p[chunk * norm_parts(h, g) + s];
+    mean = lanes_sum(mean, lanes) / total;
+    for (int i = lane; i < count; i += lanes) {
+        const int s = fast_div_any(i, g.chunks, g.m_chunks), chunk = i - s * g.chunks;
+        const float2 v = p[chunk * norm_parts(h, g) + s0 + s];
         const float d = v.x - mean;
-        dev += v.y + d * d * weight(s, chunk);
+        dev += v.y + d * d * weight(s0 + s, chunk);
     }
-    dev = lanes_sum(dev, 16);
-    if (lane == 0) stats[pair] = make_float2(mean, 1.f / sqrtf(dev / total + eps));
+    dev = lanes_sum(dev, lanes);
+    return make_float2(mean, 1.f / sqrtf(dev / total + eps));
 }
+
+__global__ __launch_bounds__(256) void norm_join_kernel(NormShape h, NormGrid g, const float2 *__restrict__ parts, float eps,
+                                                        float2 *__restrict__ stats) {
+    const unsigned pair = (blockIdx.x * 256 + threadIdx.x) / 16, lane = threadIdx.x & 15;
+    if (pair >= (unsigned)h.N * h.groups) return;
+    const float2 s = join_parts(h, g, parts, pair / h.groups, pair % h.groups, eps, lane, 16);
+    if (lane == 0) stats[pair] = s;
+}
+
+// An image's groups that a block of norm_apply_kernel joins itself instead, and the parts behind them: in small launches, where a
+// third one costs more (in 2048 blocks, 64 images of 56x56, 256 channels: 10 us).
+constexpr int kFoldGroups = 64, kFoldParts = 1024, kFoldBlocks = 512;
 
 // What a channel's values are multiplied with: z = (x - mean) a + b, a = gamma / sqrt(var + eps).  (x a + (b - mean a) would
 // save an operation and lose what mean a has more than z.)
@@ -119,13 +128,12 @@ template <int V> struct Affine {
 };
 template <int V>
 __device__ __forceinline__ void load_affine(const NormShape &h, const float2 *__restrict__ stats, const float *__restrict__ gamma,
-                                            const float *__restrict__ beta, int n, int at, Affine<V> &f) {
-    const float2 *st = stats + (size_t)n * h.groups;
+                                            const float *__restrict__ beta, int at, Affine<V> &f) {
     load_params<V>(gamma, at, 1.f, f.a);
     load_params<V>(beta, at, 0.f, f.b);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        const float2 s = st[group_of(h, at + e)];
+        const float2 s = stats[group_of(h, at + e)];
         f.mean[e] = s.x;
         f.a[e] *= s.y;
     }
@@ -138,13 +146,15 @@ template <int V> __device__ __forceinline__ void apply_affine(const Affine<V> &f
 
 // y as fp32 or bf16: threads keep their channels' coefficients and walk down the rows, one batch of loads ahead of the values that
 // they multiply (and ahead of the coefficients' own loads: those are a second trip to memory).
-template <typename TX, typename TY, int V>
+// FOLD: the block joins the parts of its image's groups itself; stats, where asked for, are then an output.
+template <typename TX, typename TY, int V, bool FOLD>
 __global__ __launch_bounds__(kNormThreads) void norm_apply_kernel(NormShape h, NormGrid g, const TX *__restrict__ x, size_t ldx,
-                                                                  const float2 *__restrict__ stats, const float *__restrict__ gamma,
-                                                                  const float *__restrict__ beta, TY *__restrict__ y, size_t ldy, int past) {
+                                                                  const float2 *__restrict__ parts, float eps, float2 *__restrict__ stats,
+                                                                  const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                  TY *__restrict__ y, size_t ldy, int past) {
     constexpr int DEEP = 4;
+    __shared__ float2 s_stats[FOLD ? kFoldGroups : 1];
     const NormBlock b = norm_block(h, g, blockIdx.x);
-    if (!b.active) return;
     const size_t row0 = (size_t)b.n * h.P + b.r0 + b.ty;
     const int rows = b.r1 - b.r0;
     const TX *p = x + row0 * ldx + b.at;
@@ -155,9 +165,21 @@ __global__ __launch_bounds__(kNormThreads) void norm_apply_kernel(NormShape h, N
         for (int k = 0; k < DEEP; ++k, p += g.TY * ldx)
             if (r + k * g.TY < rows) to[k] = fetch<V>(p);
     };
-    load(b.ty, raw);
+    if (b.active) load(b.ty, raw);
+    if constexpr (FOLD) {
+        const int lane = threadIdx.x % kWave;
+        for (int k = threadIdx.x / kWave; k < h.groups; k += g.threads / kWave) {
+            const float2 s = join_parts(h, g, parts, b.n, k, eps, lane, kWave);
+            if (lane == 0) {
+                s_stats[k] = s;
+                if (stats && b.chunk == 0 && b.c0 == 0) stats[(size_t)b.n * h.groups + k] = s;
+            }
+        }
+        __syncthreads();
+    }
+    if (!b.active) return;
     Affine<V> f;
-    load_affine<V>(h, stats, gamma, beta, b.n, b.at, f);
+    load_affine<V>(h, FOLD ? s_stats : stats + (size_t)b.n * h.groups, gamma, beta, b.at, f);
     for (int r = b.ty; r < rows; r += DEEP * g.TY) {
         load(r + DEEP * g.TY, next);
 #pragma unroll
@@ -187,6 +209,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
     const int n = fast_div_any(blockIdx.x, blocks, m_blocks), width = 1 << log_width, lane = threadIdx.x & (width - 1);
     const int r0 = ((int)blockIdx.x - n * blocks) * rows, r1 = min(r0 + rows, h.P), slots = 256 >> log_width;
     const int nv = vectors_of<V>(h.C), pitch = rows8_pitch(h.C);
+    stats += (size_t)n * h.groups;
     Raw<TX, V> raw[DEEP][H], next[DEEP][H];
     const auto load = [&](int r, Raw<TX, V> (&to)[DEEP][H]) {
         if constexpr (HELD > 0) {
@@ -203,7 +226,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
     if constexpr (HELD > 0) {
 #pragma unroll
         for (int k = 0; k < HELD; ++k)
-            if (lane + k * width < nv) load_affine<V>(h, stats, gamma, beta, n, vector_start<V>(lane + k * width, h.C), f[k]);
+            if (lane + k * width < nv) load_affine<V>(h, stats, gamma, beta, vector_start<V>(lane + k * width, h.C), f[k]);
     }
     for (int r = r0 + (threadIdx.x >> log_width); r < r1; r += DEEP * slots) {
         load(r + DEEP * slots, next);
@@ -221,7 +244,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                     for (int i = lane; i < nv; i += width) {
                         const int at = vector_start<V>(i, h.C);
                         widen(fetch<V>(x + row * ldx + at), v[0]);
-                        load_affine<V>(h, stats, gamma, beta, n, at, f[0]);
+                        load_affine<V>(h, stats, gamma, beta, at, f[0]);
                         body(at, v[0], f[0]);
                     }
                 }
@@ -413,9 +436,9 @@ static void run_held(const NormShape &h, const HeldGrid &g, const NormForward &f
     launch_held<TX, TY, V, false>(h, g, f, stats, s);
 }
 
-// stats of images too large to be held: two launches
+// Statistics of images too large to be held: parts, and with `join` a second launch.
 template <typename TX, int V>
-static void launch_stats(const NormShape &h, const NormGrid &g, const NormForward &f, float2 *parts, float2 *stats, hipStream_t s) {
+static void launch_stats(const NormShape &h, const NormGrid &g, const NormForward &f, float2 *parts, float2 *stats, bool join, hipStream_t s) {
     const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
     const TX *x = static_cast<const TX *>(f.x);
     const int units = V == 8 && h.D % 8 == 0 ? h.D / 8 : h.D;      // of a group in one row of a block's sums
@@ -425,7 +448,7 @@ static void launch_stats(const NormShape &h, const NormGrid &g, const NormForwar
         hipLaunchKernelGGL(kern, grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, lanes);
     } else
         hipLaunchKernelGGL((norm_stats_kernel<TX, V, false>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, lanes);
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * 16 + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
+    if (join) hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * 16 + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
 }
 
 // Statistics of the caller's that it did not ask for, and the parts of two-launch ones.
@@ -453,8 +476,10 @@ static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream
         else run_held<TX, uint16_t, V>(h, held, f, reinterpret_cast<float2 *>(f.stats), s);
         return hipGetLastError();
     }
+    const bool rows8 = f.y_dtype == GSPC_I8 || f.saved, fold = !rows8 && h.groups <= kFoldGroups && h.groups * g.chunks <= kFoldParts &&
+                      (long)h.N * g.chunks * g.slabs <= kFoldBlocks;
     if (hold) run_held<TX, void, V>(h, held, f, stats, s);
-    else launch_stats<TX, V>(h, g, f, parts, stats, s);
+    else launch_stats<TX, V>(h, g, f, parts, stats, !fold, s);
     if (f.y_dtype == GSPC_I8) {
         *name = "norm_rows<i8>";
         if (f.saved) launch_rows<TX, int8_t, V, true>(h, f, stats, s);
@@ -467,12 +492,14 @@ static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream
         *name = "norm_apply";
         const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
         const TX *x = static_cast<const TX *>(f.x);
+        const auto run = [&](auto kern, auto *y) {
+            hipLaunchKernelGGL(kern, grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, f.eps, fold ? reinterpret_cast<float2 *>(f.stats) : stats,
+                               f.gamma, f.beta, y, f.ldy, f.past);
+        };
         if (f.y_dtype == GSPC_F32)
-            hipLaunchKernelGGL((norm_apply_kernel<TX, float, V>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, stats, f.gamma, f.beta,
-                               static_cast<float *>(f.y), f.ldy, f.past);
+            run(fold ? norm_apply_kernel<TX, float, V, true> : norm_apply_kernel<TX, float, V, false>, static_cast<float *>(f.y));
         else
-            hipLaunchKernelGGL((norm_apply_kernel<TX, uint16_t, V>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, stats, f.gamma, f.beta,
-                               static_cast<uint16_t *>(f.y), f.ldy, f.past);
+            run(fold ? norm_apply_kernel<TX, uint16_t, V, true> : norm_apply_kernel<TX, uint16_t, V, false>, static_cast<uint16_t *>(f.y));
     }
     return hipGetLastError();
 }

@@ -231,15 +231,17 @@ static PyObject *dequantize(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     CALL(g_calls.dequantize(q, scale, x.count / cols, cols, x.ptr, x.type, cols));
 }
 
-/* norm(x [N, ..., C], gamma, beta, groups, eps, act, out, stats, saved): a call that needs no workspace */
+static size_t bytes_of(const tensor_t *t) { return t->ptr ? (size_t)t->count * (t->type == 0 ? 4 : t->type == 1 ? 2 : 1) : 0; }
+
+/* norm(x [N, ..., C], gamma, beta, groups, eps, act, out, stats, saved, workspace) */
 static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
-    tensor_t x, y;
+    tensor_t x, y, ws = {0};
     void *gamma, *beta, *stats, *out, *scale = NULL, *saved = NULL, *saved_scale = NULL;
     int groups, act, kind;
-    if (n != 9 || !g_calls.norm || !tensor(a[0], &x) || x.type == 2 || x.dims < 3 || !fits(x.first) || !fits(x.last) || !small(a[3], &groups) ||
+    if (n != 10 || !g_calls.norm || !tensor(a[0], &x) || x.type == 2 || x.dims < 3 || !fits(x.first) || !fits(x.last) || !small(a[3], &groups) ||
         !PyFloat_CheckExact(a[4]) || !small(a[5], &act) || !fits(x.count / x.first / x.last) || !vector(a[1], 0, x.last, 1, &gamma) ||
-        !vector(a[2], 0, x.last, 1, &beta) || !vector(a[7], 0, x.first * groups * 2, 1, &stats))
+        !vector(a[2], 0, x.last, 1, &beta) || !vector(a[7], 0, x.first * groups * 2, 1, &stats) || (a[9] != Py_None && !tensor(a[9], &ws)))
         GENERAL;
     const int64_t rows = x.count / x.last;
     if (PyTuple_CheckExact(a[6])) {
@@ -253,7 +255,7 @@ static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (a[8] != Py_None && !rows8(a[8], rows, x.last, &saved, &saved_scale)) GENERAL;
     const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
     CALL(g_calls.norm(x.ptr, x.type, x.last, gamma, beta, (int)x.first, (int)(rows / x.first), (int)x.last, groups, eps, act, out, kind, x.last, scale,
-                      stats, saved, saved_scale, NULL, 0));
+                      stats, saved, saved_scale, ws.ptr, bytes_of(&ws)));
 }
 
 /* norm_backward(dy [N, ..., C], x, stats, gamma, beta, groups, act, dx, dgamma, dbeta, workspace) */
@@ -277,9 +279,8 @@ static PyObject *norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n)
         px = x.ptr;
         kind = x.type;
     }
-    const size_t bytes = ws.ptr ? (size_t)ws.count * (ws.type == 0 ? 4 : ws.type == 1 ? 2 : 1) : 0;
     CALL(g_calls.norm_backward(dy.ptr, dy.type, dy.last, px, kind, dy.last, scale, stats, gamma, beta, (int)dy.first, (int)(rows / dy.first),
-                               (int)dy.last, groups, act, dx.ptr, dy.last, dgamma, dbeta, ws.ptr, bytes));
+                               (int)dy.last, groups, act, dx.ptr, dy.last, dgamma, dbeta, ws.ptr, bytes_of(&ws)));
 }
 
 /* matmul((q, scale), (q, scale), bias, out [..., N]) */
