@@ -131,20 +131,20 @@ inline bool held_grid(const NormShape &h, int groups, int threads, int held, Hel
 
 // The grid that is taken, or false: segments of 64 bytes of a token at least (of `size` bytes a value; half a cache line: with 32
 // the same kernel took 71 instead of 53 us on 64 images of 56x56, 256 channels in bf16), of 128 where that leaves four blocks for
-// each compute unit; as few threads as hold them in `held` vectors each (512 at most), more where the launch does not fill the
+// each compute unit; as few threads as hold them in `held` vectors each (`most` at most), more where the launch does not fill the
 // chip with them (one image of 7x7, 512 channels in fp32: 3.8 us with 64 threads, 3.5 with 128).
-inline bool plan_held(const NormShape &h, int size, int held, HeldGrid *best) {
+inline bool plan_held(const NormShape &h, int size, int held, int most, HeldGrid *best) {
     bool found = false;
     for (int s = 1; s <= h.groups && s * (long)h.D <= 8 * kWave; ++s) {
         if (h.groups % s) continue;
         const int bytes = s * h.D * size;
         if (s < h.groups && bytes < 64) continue;
         if (found && (long)h.N * (h.groups / s) < 1024) break;
-        for (int t = 64; t <= 512; t *= 2) {
+        for (int t = 64; t <= most; t *= 2) {
             HeldGrid g;
             if (!held_grid(h, s, t, held, &g)) continue;
             const bool fills = (long)h.N * g.segs * g.threads >= 65536;
-            if (!fills && t < 512 && (h.P + g.slots - 1) / g.slots > 2) continue;
+            if (!fills && t < most && (h.P + g.slots - 1) / g.slots > 2) continue;
             *best = g;
             found = true;
             break;

@@ -25,11 +25,7 @@ __device__ __forceinline__ void load_grad_affine(const NormShape &h, const float
     for (int e = 0; e < V; ++e) f.a[e] *= f.rstd[e * E / V];
 }
 
-// x -> d, dy -> dz
-template <int V, int E> __device__ __forceinline__ void to_d(const GradAffine<V, E> &f, float (&x)[V]) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) x[e] -= f.mean[e * E / V];
-}
+// dy -> dz
 template <int V, int E> __device__ __forceinline__ void to_dz(const GradAffine<V, E> &f, int act, const float (&d)[V], float (&dy)[V]) {
     if (act == kActRelu) {
 #pragma unroll
@@ -52,12 +48,21 @@ __device__ __forceinline__ void to_dx(const GradAffine<V, E> &f, const GradGroup
 #pragma unroll
     for (int e = 0; e < V; ++e) dz[e] = fmaf(f.a[e], dz[e], fmaf(d[e], s.kappa[e * E / V], -s.lambda[e * E / V]));
 }
-// x of an 8-bit row is q * scale
-template <typename TX, int V> __device__ __forceinline__ void widen_x(const Raw<TX, V> &r, float scale, float (&x)[V]) {
-    widen(r, x);
-    if constexpr (sizeof(TX) == 1) {
+// x -> d.  x of an 8-bit row is q * scale: with u = q + 128 (an unsigned byte converts to fp32 in one instruction)
+// d = u scale - (128 scale + mean), off by less than 2^-17 of a step of the row's.
+template <typename TX, int V, int E>
+__device__ __forceinline__ void widen_d(const GradAffine<V, E> &f, const Raw<TX, V> &r, float scale, float (&d)[V]) {
+    if constexpr (sizeof(TX) == 1 && V == 8) {
+        float shift[E];
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[e] *= scale;
+        for (int e = 0; e < E; ++e) shift[e] = fmaf(-128.f, scale, -f.mean[e]);
+        const u32x2 u = r.a ^ 0x80808080u;
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = fmaf((float)(u[e / 4] >> (e % 4 * 8) & 0xffu), scale, shift[e * E / V]);
+    } else {
+        widen(r, d);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = (sizeof(TX) == 1 ? d[e] * scale : d[e]) - f.mean[e * E / V];
     }
 }
 
@@ -105,9 +110,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_sums_kernel(NormShape 
             for (int k = 0; k < Batch::DEEP; ++k)
                 if (r + k * g.TY < rows) {
                     float d[V], dz[V];
-                    widen_x<TX, V>(now.x[k], now.scale[k], d);
+                    widen_d<TX, V, E>(f, now.x[k], now.scale[k], d);
                     widen(now.g[k], dz);
-                    to_d<V, E>(f, d);
                     to_dz<V, E>(f, h.act, d, dz);
 #pragma unroll
                     for (int e = 0; e < V; ++e) sz[e] += dz[e], sx[e] = fmaf(dz[e], d[e], sx[e]);
@@ -246,9 +250,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape
         for (int k = 0; k < Batch::DEEP; ++k)
             if (r + k * g.TY < rows) {
                 float d[V], dz[V];
-                widen_x<TX, V>(now.x[k], now.scale[k], d);
+                widen_d<TX, V, E>(f, now.x[k], now.scale[k], d);
                 widen(now.g[k], dz);
-                to_d<V, E>(f, d);
                 to_dz<V, E>(f, h.act, d, dz);
                 to_dx<V, E>(f, s, d, dz);
                 store(pd + (size_t)(r + k * g.TY) * lddx, dz, past);
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape
 // 8-bit rows), and it is computed again from what was loaded.  sums: [n][2][C] for the parameters' gradients, or where there is
 // one image these themselves.
 template <typename TX, typename TG, int V, int E, int HELD>
-__global__ __launch_bounds__(512, 4) void norm_grad_held_kernel(NormShape h, HeldGrid g, const TG *__restrict__ dy, size_t lddy,
+__global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldGrid g, const TG *__restrict__ dy, size_t lddy,
                                                              const TX *__restrict__ x, size_t ldx, const float *__restrict__ x_scale,
                                                              const float2 *__restrict__ stats, const float *__restrict__ gamma,
                                                              const float *__restrict__ beta, float *__restrict__ sum_dz,
@@ -308,9 +311,8 @@ __global__ __launch_bounds__(512, 4) void norm_grad_held_kernel(NormShape h, Hel
                 hold(rx[k]);
                 hold(rg[k]);
                 if ((k + 1) * g.slots > h.P) keep_if(rg[k], slot + k * g.slots < h.P);
-                widen_x<TX, V>(rx[k], scale[k], d);
+                widen_d<TX, V, E>(f, rx[k], scale[k], d);
                 widen(rg[k], dz);
-                to_d<V, E>(f, d);
                 to_dz<V, E>(f, h.act, d, dz);
 #pragma unroll
                 for (int e = 0; e < V; ++e) sz[e] += dz[e], sx[e] = fmaf(dz[e], d[e], sx[e]);
@@ -361,8 +363,7 @@ __global__ __launch_bounds__(512, 4) void norm_grad_held_kernel(NormShape h, Hel
             float d[V];
             float (&dz)[V] = kept[KEEP ? k : 0];
             hold(rx[k]);
-            widen_x<TX, V>(rx[k], scale[k], d);
-            to_d<V, E>(f, d);
+            widen_d<TX, V, E>(f, rx[k], scale[k], d);
             if constexpr (!KEEP) {
                 hold(rg[k]);
                 widen(rg[k], dz);
@@ -378,10 +379,12 @@ __global__ __launch_bounds__(512, 4) void norm_grad_held_kernel(NormShape h, Hel
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 constexpr int kBackwardBlocks = 2048;
 
-// Four vectors a thread where that can be, else eight where x and dy take 64 registers then.
-template <typename TX, typename TG> constexpr int grad_held_most() { return sizeof(TX) == 4 || sizeof(TG) == 4 ? 4 : 8; }
+// Four vectors a thread where 512 threads will do.  Else eight from 8-bit rows and bf16 (48 registers; 256 images of 28x28, 128 channels:
+// 38 us, in 1024 threads 40), or 1024 threads (from bf16 45 us, 59 with eight vectors).
+template <typename TX, typename TG> constexpr int grad_held_most() { return sizeof(TX) == 1 && sizeof(TG) == 2 ? 8 : 4; }
 template <typename TX, typename TG> static bool plan_grad_held(const NormShape &h, HeldGrid *g) {
-    return plan_held(h, sizeof(TG), 4, g) || (grad_held_most<TX, TG>() > 4 && plan_held(h, sizeof(TG), 8, g));
+    return plan_held(h, sizeof(TG), 4, 512, g) || (grad_held_most<TX, TG>() > 4 && plan_held(h, sizeof(TG), 8, 512, g)) ||
+           plan_held(h, sizeof(TG), 4, 1024, g);
 }
 
 template <typename TX, typename TG> static size_t backward_bytes(const NormShape &h) {
@@ -400,7 +403,7 @@ size_t norm_backward_bytes(const NormShape &h, int dy_dtype, int x_dtype) {
 }
 
 template <typename TX, typename TG, int V, int E>
-static void launch_grad_held(const NormShape &h, HeldGrid g, const NormBackward &b, float *sums, hipStream_t s) {
+static hipError_t launch_grad_held(const NormShape &h, HeldGrid g, const NormBackward &b, float *sums, hipStream_t s) {
     constexpr int MOST = grad_held_most<TX, TG>();
     const int held = (h.P + g.slots - 1) / g.slots;
     const auto kern = held <= 1 ? norm_grad_held_kernel<TX, TG, V, E, 1> : held <= 2 ? norm_grad_held_kernel<TX, TG, V, E, 2>
@@ -409,9 +412,14 @@ static void launch_grad_held(const NormShape &h, HeldGrid g, const NormBackward 
     while ((1 << g.log_lanes) < g.slots && g.log_lanes < 6 && (4 * g.seg << g.log_lanes) <= g.threads) ++g.log_lanes;
     const size_t lds = (2 * (size_t)g.slots * (g.seg + 1) + 2 * g.seg + 2 * (g.seg / h.D) + 1) * sizeof(float);
     const bool one = h.N == 1;
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(kern, dim3((unsigned)((size_t)h.N * g.segs)), dim3(g.threads), lds, s, h, g, static_cast<const TG *>(b.dy), b.lddy,
                        static_cast<const TX *>(b.x), b.ldx, b.x_scale, reinterpret_cast<const float2 *>(b.stats), b.gamma, b.beta,
                        one ? b.dbeta : sums, one ? b.dgamma : sums + h.C, (size_t)2 * h.C, static_cast<TG *>(b.dx), b.lddx, b.past);
+    return hipSuccess;
 }
 
 template <typename TX, typename TG, int V, int E>
@@ -456,12 +464,15 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
     *name = hold ? "norm_grad_held" : "norm_grad_apply";
     const auto run = [&](auto e) {
         constexpr int E = decltype(e)::value;
-        if (hold) launch_grad_held<TX, TG, V, E>(h, held, b, sums, s);
-        else launch_grad<TX, TG, V, E>(h, g, b, parts, sums, ab, s);
+        if (hold) return launch_grad_held<TX, TG, V, E>(h, held, b, sums, s);
+        launch_grad<TX, TG, V, E>(h, g, b, parts, sums, ab, s);
+        return hipSuccess;
     };
-    if (V == 8 && h.D % 8 == 0) run(std::integral_constant<int, 1>{});
-    else if (V == 8 && h.D % 4 == 0) run(std::integral_constant<int, V == 8 ? 2 : 1>{});
-    else run(std::integral_constant<int, V>{});
+    hipError_t e;
+    if (V == 8 && h.D % 8 == 0) e = run(std::integral_constant<int, 1>{});
+    else if (V == 8 && h.D % 4 == 0) e = run(std::integral_constant<int, V == 8 ? 2 : 1>{});
+    else e = run(std::integral_constant<int, V>{});
+    if (e != hipSuccess) return e;
     if (params && hold && h.N > 1)
         hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h.C, h.N, sums, b.dgamma, b.dbeta);
     return hipGetLastError();

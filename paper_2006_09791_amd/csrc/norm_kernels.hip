@@ -454,7 +454,7 @@ static void launch_stats(const NormShape &h, const NormGrid &g, const NormForwar
 // Statistics of the caller's that it did not ask for, and the parts of two-launch ones.
 size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8) {
     HeldGrid held;
-    const bool hold = x_dtype == GSPC_F32 ? plan_held(h, 4, held_most<float>(), &held) : plan_held(h, 2, held_most<uint16_t>(), &held);
+    const bool hold = x_dtype == GSPC_F32 ? plan_held(h, 4, held_most<float>(), 512, &held) : plan_held(h, 2, held_most<uint16_t>(), 512, &held);
     if (hold && !rows8) return 0;
     const size_t stats = (size_t)h.N * h.groups * sizeof(float2);
     if (hold) return stats;
@@ -469,7 +469,7 @@ static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream
     float2 *parts = static_cast<float2 *>(ws) + (size_t)h.N * h.groups;
     f.past = (size_t)h.N * h.P * h.C * (f.y_dtype == GSPC_F32 ? 4 : 2) >= kPastCaches;
     HeldGrid held;
-    const bool hold = plan_held(h, sizeof(TX), held_most<TX>(), &held);
+    const bool hold = plan_held(h, sizeof(TX), held_most<TX>(), 512, &held);
     if (f.y_dtype != GSPC_I8 && !f.saved && hold) {
         *name = "norm_held";
         if (f.y_dtype == GSPC_F32) run_held<TX, float, V>(h, held, f, reinterpret_cast<float2 *>(f.stats), s);

@@ -13,7 +13,7 @@ constexpr int kTile = 64, kTilePitch = kTile + 1;
 // the other way) into 64 banks.  Bound by memory: each element is read and written once.
 template <typename TI, typename TO, int VI, int VO>
 __global__ __launch_bounds__(256) void transpose_kernel(const TI *__restrict__ in, TO *__restrict__ out, int R, int S, unsigned rtiles,
-                                                       unsigned tiles, unsigned m_rtiles, unsigned m_tiles) {
+                                                       unsigned tiles, unsigned m_rtiles, unsigned m_tiles, int past) {
     __shared__ float lds[kTile * kTilePitch];
     const unsigned n = fast_div_any(blockIdx.x, tiles, m_tiles), t = blockIdx.x - n * tiles;
     const unsigned st = fast_div_any(t, rtiles, m_rtiles), rt = t - st * rtiles;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void transpose_kernel(const TI *__restrict__ i
             float v[VO];
 #pragma unroll
             for (int e = 0; e < VO; ++e) v[e] = lds[s * kTilePitch + at + e];
-            store(op + (size_t)s * R + at, v);
+            store(op + (size_t)s * R + at, v, past);
         }
     }
 }
@@ -61,7 +61,8 @@ static hipError_t transpose(const void *in, int N, int R, int S, void *out, hipS
     for (int n = 0; n < N; n += step) {
         const int count = N - n < step ? N - n : step;
         hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * count)), dim3(256), 0, s, static_cast<const TI *>(in) + (size_t)n * R * S,
-                           static_cast<TO *>(out) + (size_t)n * R * S, R, S, rt, (unsigned)tiles, div_magic(rt), div_magic((unsigned)tiles));
+                           static_cast<TO *>(out) + (size_t)n * R * S, R, S, rt, (unsigned)tiles, div_magic(rt), div_magic((unsigned)tiles),
+                           R >= kTile && (size_t)N * R * S * sizeof(TO) >= kPastCaches);
     }
     return hipGetLastError();
 }

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict_
 
 template <typename T, int V>
 __global__ __launch_bounds__(256) void dequantize_rows_kernel(const int8_t *__restrict__ q, const float *__restrict__ scale,
-                                                              unsigned rows, int cols, int width, T *__restrict__ x, size_t ldx) {
+                                                              unsigned rows, int cols, int width, T *__restrict__ x, size_t ldx, int past) {
     const unsigned row = (blockIdx.x * 256 + threadIdx.x) / width;
     const int lane = threadIdx.x & (width - 1), nv = vectors_of<V>(cols);
     if (row >= rows) return;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const int8_t *__re
         widen(fetch<V>(q + at), v);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] *= s;
-        store(x + at, v);
+        store(x + at, v, past);
     }
 }
 
@@ -110,7 +110,8 @@ static hipError_t dequantize(const int8_t *q, const float *scale, size_t rows, i
     const auto kern = cols >= 8 ? dequantize_rows_kernel<T, 8> : dequantize_rows_kernel<T, 1>;
     const size_t pitch = rows8_pitch(cols);
     return in_pieces(rows, width, [&](size_t at, unsigned n, dim3 grid) {
-        hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, q + at * pitch, scale + at, n, cols, width, x + at * ldx, ldx);
+        hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, q + at * pitch, scale + at, n, cols, width, x + at * ldx, ldx,
+                           cols >= 32 && rows * cols * sizeof(T) >= kPastCaches);
     });
 }
 

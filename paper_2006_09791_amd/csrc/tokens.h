@@ -96,9 +96,10 @@ __device__ __forceinline__ void widen(const Raw8 &r, float (&v)[8]) {
 }
 template <typename T> __device__ __forceinline__ void widen(const T &r, float (&v)[1]) { v[0] = as_float(r); }
 
-// past: beyond the caches (a non-temporal store), for outputs of kPastCaches bytes and more, too large to be found there by whoever
-// reads them next.
-constexpr size_t kPastCaches = 32u << 20;
+// past: beyond the caches (a non-temporal store), for outputs of kPastCaches bytes and more.  Group norm in bf16, us alone and with a
+// reader of y behind it: 12.8 MB of y 10.6 and 15.6 through the caches, 9.4 and 14.9 past them; 25.7 MB 13.8, 22.4 and 12.2, 21.7; 51 MB
+// 29.5, 43.1 and 19.2, 46.0; below 8 MB level.  (Only whole pieces of 64 bytes and more: in pieces of 32 it took twice as long.)
+constexpr size_t kPastCaches = 8u << 20;
 __device__ __forceinline__ void store_vector(u32x4_any *p, u32x4 v, bool past) {
     if (past) {
         asm volatile("");           // (two stores that differ in their hint alone would be merged, without it)
