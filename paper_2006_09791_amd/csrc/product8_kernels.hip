@@ -20,6 +20,19 @@ template <int LEFT> __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
 }
 
+// Barriers around LDS that loads write directly and other lanes have written: nothing is to be moved across them.  (No fence: that
+// would wait for the loads that are to stay under way.)
+__device__ __forceinline__ void barrier_of_block() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void barrier_of_wave() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 struct ProductArgs {
     const int8_t *a, *w;
     const float *a_scale, *w_scale, *bias;
@@ -205,9 +218,12 @@ __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs
 #pragma unroll
     for (int t = 0; t < STAGES; ++t)
 #pragma unroll
-        for (int i = 0; i < (t + 1 < STAGES ? LOADS : FIRST); ++i) load_one(t * STAGE, t * kStep, i);
+        for (int i = 0; i < LOADS; ++i) {
+            if (t + 1 < STAGES || i < FIRST) load_one(t * STAGE, t * kStep, i);
+            __builtin_amdgcn_sched_barrier(0);      // loads are counted: in this order
+        }
     wait_loads<(STAGES - 2) * LOADS + FIRST>();
-    __builtin_amdgcn_s_barrier();
+    barrier_of_block();
 #pragma unroll
     for (int t = 0; t < READS; ++t) op[0][t] = read_one(0, 0, t);
     unsigned stage = 0, before = (STAGES - 1) * STAGE;      // of step k, and of the one before, where k + STAGES - 1 comes
@@ -220,7 +236,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs
             for (int t = 0; t < SLOTS; ++t) {
                 if (last && t == SKIP) {
                     wait_loads<(STAGES - 2) * LOADS>();
-                    __builtin_amdgcn_s_barrier();
+                    barrier_of_block();
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 const int s = last ? t - SKIP : t, slots = last ? SLOTS - SKIP : SLOTS;
@@ -279,7 +295,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs
                 if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(turn + r * PITCH + n * 4) = (f32x4){v[0], v[1], v[2], v[3]};
                 else *reinterpret_cast<u32x2 *>(turn + r * PITCH + n * 2) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
             }
-        __builtin_amdgcn_wave_barrier();            // (LDS operations of one wave are in order)
+        barrier_of_wave();            // (LDS operations of one wave are in order)
 #pragma unroll
         for (int t = 0; t < 32; t += kWave / LANES) {
             const int row = t + lane / LANES, n = lane % LANES * EACH;
@@ -299,7 +315,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs
                 }
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        barrier_of_wave();
     }
 }
 

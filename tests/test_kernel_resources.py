@@ -81,3 +81,20 @@ def test_bf16_strips_keep_their_waves():
     """bf16 depthwise at stride 2: left to the compiler it is two registers past the step of six waves."""
     k, = [v for n, v in kernels().items() if n.startswith("_ZN4gspc17conv_direct_smallILi1ELi1ELi2ELi2Et")]
     assert waves(k) >= 6 and k[".vgpr_spill_count"] == 0, k[".vgpr_count"]
+
+
+def test_held_norms_and_products_need_no_scratch():
+    """Kernels that hold an image or a tile in registers: a spilled value would go to memory in their inner loops."""
+    found = 0
+    for n, k in kernels().items():
+        if "norm_held_kernel" in n or "product8_" in n or "norm_rows_kernel" in n:
+            found += 1
+            assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, n
+    assert found > 40
+
+
+@pytest.mark.parametrize("held,least", [(8, 6), (16, 4)])
+def test_held_norm_keeps_its_waves(held, least):
+    """bf16, all of a vector in one group: waves per SIMD that the launches count on to load while others store."""
+    k, = [v for n, v in kernels().items() if n.startswith(f"_ZN4gspc16norm_held_kernelIttLi8ELi{held}ELb1E")]
+    assert waves(k) >= least, k[".vgpr_count"]
