@@ -8,7 +8,6 @@ namespace gspc {
 
 constexpr int kNormThreads = 512;
 constexpr int kSlab = 2048;             // channels of a block at most: 256 vectors
-constexpr int kMaxChunks = 128;
 
 // Blocks that keep their channels and walk down the rows of one image: thread (tx, ty) holds vector tx of the slab's channels
 // and the rows r0 + ty, r0 + ty + TY, ...
@@ -42,7 +41,7 @@ __device__ __forceinline__ NormBlock norm_block(const NormShape &h, const NormGr
     return b;
 }
 
-inline NormGrid norm_grid(const NormShape &h, int blocks_wanted) {
+inline NormGrid norm_grid(const NormShape &h, int blocks_wanted, int most_chunks) {
     NormGrid g;
     g.V = h.C >= 8 ? 8 : 1;
     g.slabs = (h.C + kSlab - 1) / kSlab;
@@ -51,11 +50,11 @@ inline NormGrid norm_grid(const NormShape &h, int blocks_wanted) {
     g.TY = kNormThreads / g.nvs;
     if (g.TY > h.P) g.TY = h.P;
     g.threads = round_up(g.TY * g.nvs, kWave);
-    // enough blocks to fill the chip, of at least four rows per thread
-    long want = blocks_wanted / ((long)h.N * g.slabs);
-    const long most = (h.P + 4L * g.TY - 1) / (4L * g.TY);
+    // enough blocks to fill the chip, of at least four rows per thread, or one where four leave compute units without a block
+    long want = blocks_wanted / ((long)h.N * g.slabs), most = (h.P + 4L * g.TY - 1) / (4L * g.TY);
+    if (most * h.N * g.slabs < 256) most = (h.P + g.TY - 1) / g.TY, want = 256 / ((long)h.N * g.slabs);
     if (want > most) want = most;
-    if (want > kMaxChunks) want = kMaxChunks;
+    if (want > most_chunks) want = most_chunks;
     if (want < 1) want = 1;
     g.rows = (int)((h.P + want - 1) / want);
     g.chunks = (h.P + g.rows - 1) / g.rows;

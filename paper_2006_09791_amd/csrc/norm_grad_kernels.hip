@@ -377,7 +377,7 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
-constexpr int kBackwardBlocks = 2048;
+constexpr int kBackwardBlocks = 2048, kBackwardChunks = 128;    // (the join takes an image's chunks one after another)
 
 // Four vectors a thread where 512 threads will do.  Else eight from 8-bit rows and bf16 (48 registers; 256 images of 28x28, 128 channels:
 // 38 us, in 1024 threads 40), or 1024 threads (from bf16 45 us, 59 with eight vectors).
@@ -393,7 +393,7 @@ template <typename TX, typename TG> static size_t backward_bytes(const NormShape
     if (hold && h.N == 1) return 0;
     const size_t sums = (size_t)h.N * 2 * h.C * sizeof(float);
     if (hold) return sums;
-    return sums + ((size_t)h.N * norm_grid(h, kBackwardBlocks).chunks * 2 * h.C + (size_t)h.N * h.groups * 2) * sizeof(float);
+    return sums + ((size_t)h.N * norm_grid(h, kBackwardBlocks, kBackwardChunks).chunks * 2 * h.C + (size_t)h.N * h.groups * 2) * sizeof(float);
 }
 
 size_t norm_backward_bytes(const NormShape &h, int dy_dtype, int x_dtype) {
@@ -454,7 +454,7 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
             hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h.C, 0, (const float *)nullptr, b.dgamma, b.dbeta);
         return hipGetLastError();
     }
-    const NormGrid g = norm_grid(h, kBackwardBlocks);
+    const NormGrid g = norm_grid(h, kBackwardBlocks, kBackwardChunks);
     float *sums = static_cast<float *>(ws);
     float2 *ab = reinterpret_cast<float2 *>(sums + (size_t)h.N * 2 * h.C);
     float *parts = reinterpret_cast<float *>(ab + (size_t)h.N * h.groups);

@@ -83,9 +83,12 @@ __global__ __launch_bounds__(kNormThreads) void norm_stats_kernel(NormShape h, N
     }
 }
 
-// The blocks' parts of group k of image n joined by `lanes` lanes: mean, 1 / sqrt(var + eps).
+// The blocks' parts of group k of image n joined by kJoinLanes lanes (always as many: the same statistics, whoever joins them): mean,
+// 1 / sqrt(var + eps).
+constexpr int kJoinLanes = kWave;
 __device__ __forceinline__ float2 join_parts(const NormShape &h, const NormGrid &g, const float2 *__restrict__ parts, int n, int k, float eps,
-                                             int lane, int lanes) {
+                                             int lane) {
+    constexpr int lanes = kJoinLanes;
     const int s0 = (k * h.D) / kSlab, s1 = ((k + 1) * h.D - 1) / kSlab, count = (s1 - s0 + 1) * g.chunks;
     const float2 *p = parts + (size_t)n * g.chunks * norm_parts(h, g) + k;
     const auto weight = [&](int s, int chunk) {
@@ -93,17 +96,33 @@ __device__ __forceinline__ float2 join_parts(const NormShape &h, const NormGrid 
         return (float)channels * (float)(min(h.P - chunk * g.rows, g.rows));
     };
     const float total = (float)h.P * (float)h.D;
-    float mean = 0.f, dev = 0.f;
-    for (int i = lane; i < count; i += lanes) {
+    const auto part = [&](int i, float &w) {
         const int s = fast_div_any(i, g.chunks, g.m_chunks), chunk = i - s * g.chunks;
-        mean += p[chunk * norm_parts(h, g) + s0 + s].x * weight(s0 + s, chunk);
+        w = weight(s0 + s, chunk);
+        return p[chunk * norm_parts(h, g) + s0 + s];
+    };
+    constexpr int HELD = 4;                         // parts that a lane loads once, all at the same time
+    float2 v[HELD];
+    float w[HELD], mean = 0.f, dev = 0.f;
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (lane + j * lanes < count) v[j] = part(lane + j * lanes, w[j]);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (lane + j * lanes < count) mean += v[j].x * w[j];
+    for (int i = lane + HELD * lanes; i < count; i += lanes) {
+        float wi;
+        const float2 vi = part(i, wi);
+        mean += vi.x * wi;
     }
     mean = lanes_sum(mean, lanes) / total;
-    for (int i = lane; i < count; i += lanes) {
-        const int s = fast_div_any(i, g.chunks, g.m_chunks), chunk = i - s * g.chunks;
-        const float2 v = p[chunk * norm_parts(h, g) + s0 + s];
-        const float d = v.x - mean;
-        dev += v.y + d * d * weight(s0 + s, chunk);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+        if (lane + j * lanes < count) dev += v[j].y + (v[j].x - mean) * (v[j].x - mean) * w[j];
+    for (int i = lane + HELD * lanes; i < count; i += lanes) {
+        float wi;
+        const float2 vi = part(i, wi);
+        dev += vi.y + (vi.x - mean) * (vi.x - mean) * wi;
     }
     dev = lanes_sum(dev, lanes);
     return make_float2(mean, 1.f / sqrtf(dev / total + eps));
@@ -111,9 +130,9 @@ __device__ __forceinline__ float2 join_parts(const NormShape &h, const NormGrid 
 
 __global__ __launch_bounds__(256) void norm_join_kernel(NormShape h, NormGrid g, const float2 *__restrict__ parts, float eps,
                                                         float2 *__restrict__ stats) {
-    const unsigned pair = (blockIdx.x * 256 + threadIdx.x) / 16, lane = threadIdx.x & 15;
+    const unsigned pair = (blockIdx.x * 256 + threadIdx.x) / kJoinLanes, lane = threadIdx.x % kJoinLanes;
     if (pair >= (unsigned)h.N * h.groups) return;
-    const float2 s = join_parts(h, g, parts, pair / h.groups, pair % h.groups, eps, lane, 16);
+    const float2 s = join_parts(h, g, parts, pair / h.groups, pair % h.groups, eps, lane);
     if (lane == 0) stats[pair] = s;
 }
 
@@ -167,9 +186,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_apply_kernel(NormShape h, N
     };
     if (b.active) load(b.ty, raw);
     if constexpr (FOLD) {
-        const int lane = threadIdx.x % kWave;
-        for (int k = threadIdx.x / kWave; k < h.groups; k += g.threads / kWave) {
-            const float2 s = join_parts(h, g, parts, b.n, k, eps, lane, kWave);
+        const int lane = threadIdx.x % kJoinLanes;
+        for (int k = threadIdx.x / kJoinLanes; k < h.groups; k += g.threads / kJoinLanes) {
+            const float2 s = join_parts(h, g, parts, b.n, k, eps, lane);
             if (lane == 0) {
                 s_stats[k] = s;
                 if (stats && b.chunk == 0 && b.c0 == 0) stats[(size_t)b.n * h.groups + k] = s;
@@ -393,7 +412,7 @@ __global__ __launch_bounds__(512) void norm_held_kernel(NormShape h, HeldGrid g,
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
-constexpr int kForwardBlocks = 2048;
+constexpr int kForwardBlocks = 2048, kForwardChunks = 256;
 
 template <typename TX, typename TY, int V, bool SAVE>
 static void launch_rows(const NormShape &h, const NormForward &f, const float2 *stats, hipStream_t s) {
@@ -448,7 +467,7 @@ static void launch_stats(const NormShape &h, const NormGrid &g, const NormForwar
         hipLaunchKernelGGL(kern, grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, lanes);
     } else
         hipLaunchKernelGGL((norm_stats_kernel<TX, V, false>), grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, lanes);
-    if (join) hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * 16 + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
+    if (join) hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * kJoinLanes + 255) / 256)), dim3(256), 0, s, h, g, parts, f.eps, stats);
 }
 
 // Statistics of the caller's that it did not ask for, and the parts of two-launch ones.
@@ -458,13 +477,13 @@ size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8) {
     if (hold && !rows8) return 0;
     const size_t stats = (size_t)h.N * h.groups * sizeof(float2);
     if (hold) return stats;
-    const NormGrid g = norm_grid(h, kForwardBlocks);
+    const NormGrid g = norm_grid(h, kForwardBlocks, kForwardChunks);
     return stats + (size_t)h.N * g.chunks * norm_parts(h, g) * sizeof(float2);
 }
 
 template <typename TX, int V>
 static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream_t s, const char **name) {
-    const NormGrid g = norm_grid(h, kForwardBlocks);
+    const NormGrid g = norm_grid(h, kForwardBlocks, kForwardChunks);
     float2 *stats = f.stats ? reinterpret_cast<float2 *>(f.stats) : static_cast<float2 *>(ws);
     float2 *parts = static_cast<float2 *>(ws) + (size_t)h.N * h.groups;
     f.past = (size_t)h.N * h.P * h.C * (f.y_dtype == GSPC_F32 ? 4 : 2) >= kPastCaches;

@@ -338,11 +338,12 @@ template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t
     //   128 x 128 from 256 tiles on: 2048 x 4096 x 2048 has 512, 22.4 against 29 in 64 x 128; 512 x 4096 x 4096 has 128, 18.3 against 15.8;
     //   64 x 128 where 32 x 32 without staging would be more than one block for each compute unit: 512 x 4096 x 4096, 15.8 against
     //   59; 200 x 1024 x 1024 (224 blocks without staging), 5.9 against 4.4.
-    // Up to 16 tokens: 1 x 4096 x 4096, 5.7 in blocks of 16 channels and eight waves, 7.2 in blocks of 32 x 32.
+    //   or where its steps are few: 133 x 3608 x 195, 3.7 without staging, 4.4 in 64 x 128.
+    // Up to 16 tokens: 1 x 4096 x 4096, 5.1 in blocks of 16 channels, 7.2 in blocks of 32 x 32.
     if (tiles(256, 256) >= 160) run(product8_tile_kernel<T, 2, 4, 4, 2, 2>, 256, 256, 512, "product8_tile<256,256>");
     else if (tiles(128, 128) >= 256) run(product8_tile_kernel<T, 2, 2, 2, 2, 2>, 128, 128, 256, "product8_tile<128,128>");
-    else if (in.M <= 16) run(product8_small_kernel<T, 1, 1, 8, 8>, 16, 16, 512, "product8_small<1,1>");
-    else if (tiles(32, 32) <= 256) run(product8_small_kernel<T, 2, 2, 8, 4>, 32, 32, 512, "product8_small<2,2>");
+    else if (in.M <= 16) run(product8_small_kernel<T, 1, 1, 8, 4>, 16, 16, 512, "product8_small<1,1>");
+    else if (tiles(32, 32) <= 256 || tiles(32, 32) * ((p.pitch + 63) / 64) <= 2560) run(product8_small_kernel<T, 2, 2, 8, 2>, 32, 32, 512, "product8_small<2,2>");
     else run(product8_tile_kernel<T, 2, 2, 1, 2, 3>, 64, 128, 256, "product8_tile<64,128>");
     return hipGetLastError();
 }
