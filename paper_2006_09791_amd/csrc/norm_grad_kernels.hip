@@ -135,25 +135,32 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_sums_kernel(NormShape 
     }
 }
 
-// The blocks' parts joined: sums[n][2][C] of an image, and A / m, B / m of each group.  `lanes` lanes for a group of an image.
-__global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape h, int chunks, int lanes, const float *__restrict__ parts,
+// The blocks' parts joined: sums[n][2][C] of an image, and A / m, B / m of each group.  A wave has a group of an image: 2^log_lanes
+// lanes its channels (in turn, where there are more), and as many times as these fit a wave the chunks between them.
+__global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape h, int chunks, int log_lanes, const float *__restrict__ parts,
                                                              const float *__restrict__ gamma, float *__restrict__ sums,
                                                              float2 *__restrict__ ab) {
-    const unsigned pair = (blockIdx.x * 256 + threadIdx.x) / lanes, lane = threadIdx.x & (lanes - 1);
+    const unsigned pair = (blockIdx.x * 256 + threadIdx.x) / kWave;
     if (pair >= (unsigned)h.N * h.groups) return;
+    const int lanes = 1 << log_lanes, lane = threadIdx.x % kWave, own = lane & (lanes - 1), share = lane >> log_lanes, shares = kWave >> log_lanes;
     const int n = pair / h.groups, k = pair - n * h.groups;
     float a = 0.f, b = 0.f;
-    for (int i = lane; i < h.D; i += lanes) {
-        const int c = k * h.D + i;
+    for (int i = own; i - own < h.D; i += lanes) {
+        const int c = k * h.D + min(i, h.D - 1);
         const float *p = parts + (size_t)n * chunks * 2 * h.C + c;
         float sz = 0.f, sx = 0.f;
-#pragma unroll 4
-        for (int j = 0; j < chunks; ++j) sz += p[(size_t)j * 2 * h.C], sx += p[((size_t)j * 2 + 1) * h.C];
-        sums[(size_t)n * 2 * h.C + c] = sz;
-        sums[((size_t)n * 2 + 1) * h.C + c] = sx;
-        const float w = gamma ? gamma[c] : 1.f;
-        a = fmaf(w, sz, a);
-        b = fmaf(w, sx, b);
+#pragma unroll 8
+        for (int j = share; j < chunks; j += shares) sz += p[(size_t)j * 2 * h.C], sx += p[((size_t)j * 2 + 1) * h.C];
+        for (int d = lanes; d < kWave; d *= 2) sz += __shfl_xor(sz, d), sx += __shfl_xor(sx, d);
+        if (i < h.D) {
+            if (share == 0) {
+                sums[(size_t)n * 2 * h.C + c] = sz;
+                sums[((size_t)n * 2 + 1) * h.C + c] = sx;
+            }
+            const float w = gamma ? gamma[c] : 1.f;
+            a = fmaf(w, sz, a);
+            b = fmaf(w, sx, b);
+        }
     }
     a = lanes_sum(a, lanes);
     b = lanes_sum(b, lanes);
@@ -377,7 +384,7 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------
-constexpr int kBackwardBlocks = 2048, kBackwardChunks = 128;    // (the join takes an image's chunks one after another)
+constexpr int kBackwardBlocks = 2048, kBackwardChunks = 256;
 
 // Four vectors a thread where 512 threads will do.  Else eight from 8-bit rows and bf16 (48 registers; 256 images of 28x28, 128 channels:
 // 38 us, in 1024 threads 40), or 1024 threads (from bf16 45 us, 59 with eight vectors).
@@ -438,9 +445,10 @@ static void launch_grad(const NormShape &h, const NormGrid &g, const NormBackwar
                            rows, from, b.dgamma, b.dbeta);
     };
     if (fold) return apply(norm_grad_apply_kernel<TX, TG, V, E, true>, h.N * g.chunks, parts);
-    const int lanes = group_lanes(h.D, (long)h.N * h.groups, 1L << 20);
-    hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * lanes + 255) / 256)), dim3(256), 0, s, h, g.chunks,
-                       lanes, parts, b.gamma, sums, ab);
+    int log_lanes = 0;
+    while ((1 << log_lanes) < h.D && log_lanes < 6) ++log_lanes;
+    hipLaunchKernelGGL(norm_grad_join_kernel, dim3((unsigned)(((size_t)h.N * h.groups * kWave + 255) / 256)), dim3(256), 0, s, h, g.chunks,
+                       log_lanes, parts, b.gamma, sums, ab);
     apply(norm_grad_apply_kernel<TX, TG, V, E, false>, h.N, sums);
 }
 
