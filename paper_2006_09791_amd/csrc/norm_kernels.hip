@@ -222,9 +222,9 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                                                         const TX *__restrict__ x, size_t ldx, const float2 *__restrict__ stats,
                                                         const float *__restrict__ gamma, const float *__restrict__ beta,
                                                         TY *__restrict__ y, size_t ldy, float *__restrict__ y_scale,
-                                                        int8_t *__restrict__ saved, float *__restrict__ saved_scale, int past) {
+                                                        int8_t *__restrict__ saved, float *__restrict__ saved_scale, int past, int past_saved) {
     constexpr bool CODES = sizeof(TY) == 1;
-    constexpr int H = HELD ? HELD : 1, DEEP = HELD == 0 ? 1 : 4 / HELD;
+    constexpr int H = HELD ? HELD : 1, DEEP = HELD == 1 ? 2 : 1;
     const int n = fast_div_any(blockIdx.x, blocks, m_blocks), width = 1 << log_width, lane = threadIdx.x & (width - 1);
     const int r0 = ((int)blockIdx.x - n * blocks) * rows, r1 = min(r0 + rows, h.P), slots = 256 >> log_width;
     const int nv = vectors_of<V>(h.C), pitch = rows8_pitch(h.C);
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                     for (int e = 0; e < V; ++e) top = max(top, magnitude(t[e]));
                 });
                 const RowCode c = row_code(lanes_umax(top, width));
-                each([&](int at, float (&t)[V], Affine<V> &) { store_codes(saved + row * pitch + at, t, c); });
+                each([&](int at, float (&t)[V], Affine<V> &) { store_codes(saved + row * pitch + at, t, c, past_saved); });
                 for (int i = h.C + lane; i < pitch; i += width) saved[row * pitch + i] = 0;
                 if (lane == 0) saved_scale[row] = c.scale;
             }
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                 const RowCode c = row_code(lanes_umax(top, width));
                 each([&](int at, float (&t)[V], Affine<V> &fk) {
                     if constexpr (HELD == 0) apply_affine<V>(fk, h.act, t);
-                    store_codes(reinterpret_cast<int8_t *>(y) + row * pitch + at, t, c);
+                    store_codes(reinterpret_cast<int8_t *>(y) + row * pitch + at, t, c, false);
                 });
                 for (int i = h.C + lane; i < pitch; i += width) reinterpret_cast<int8_t *>(y)[row * pitch + i] = 0;
                 if (lane == 0) y_scale[row] = c.scale;
@@ -424,14 +424,15 @@ static void launch_rows(const NormShape &h, const NormForward &f, const float2 *
                     : each <= 2 ? norm_rows_kernel<TX, TY, V, 2, SAVE>
                     : each <= 4 ? norm_rows_kernel<TX, TY, V, 4, SAVE> : norm_rows_kernel<TX, TY, V, 0, SAVE>;
     const int at_once = 256 / width;
-    long blocks = 2048 / h.N + 1;
-    const long most = (h.P + 4L * at_once - 1) / (4L * at_once);
+    // (blocks of two rows a lane: with four and a quarter as many blocks 64 images of 14x14, 512 channels took 9.8 us instead of 8.8)
+    long blocks = 8192 / h.N + 1;
+    const long most = (h.P + 2L * at_once - 1) / (2L * at_once);
     if (blocks > most) blocks = most;
     const int rows = (int)((h.P + blocks - 1) / blocks);
     blocks = (h.P + rows - 1) / rows;
     hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * h.N)), dim3(256), 0, s, h, log_width, (int)blocks, rows, div_magic((unsigned)blocks),
                        static_cast<const TX *>(f.x), f.ldx, stats, f.gamma, f.beta, static_cast<TY *>(f.y), f.ldy, f.y_scale, f.saved,
-                       f.saved_scale, f.past);
+                       f.saved_scale, f.past, h.C >= 64 && (size_t)h.N * h.P * h.C >= kPastCaches);
 }
 
 // Vectors that a thread of norm_held_kernel holds at most: 64 registers of raw values.

@@ -100,10 +100,19 @@ template <typename T> __device__ __forceinline__ void widen(const T &r, float (&
 // reader of y behind it: 12.8 MB of y 10.6 and 15.6 through the caches, 9.4 and 14.9 past them; 25.7 MB 13.8, 22.4 and 12.2, 21.7; 51 MB
 // 29.5, 43.1 and 19.2, 46.0; below 8 MB level.  (Only whole pieces of 64 bytes and more: in pieces of 32 it took twice as long.)
 constexpr size_t kPastCaches = 8u << 20;
+// (two stores that differ in their hint alone would be merged, without the empty statements)
 __device__ __forceinline__ void store_vector(u32x4_any *p, u32x4 v, bool past) {
     if (past) {
-        asm volatile("");           // (two stores that differ in their hint alone would be merged, without it)
+        asm volatile("");
         __builtin_nontemporal_store((u32x4_any)v, p);
+        asm volatile("");
+    } else
+        *p = v;
+}
+__device__ __forceinline__ void store_vector(u32x2_any *p, u32x2 v, bool past) {
+    if (past) {
+        asm volatile("");
+        __builtin_nontemporal_store((u32x2_any)v, p);
         asm volatile("");
     } else
         *p = v;
@@ -187,10 +196,10 @@ __device__ __forceinline__ unsigned code_word(float v0, float v1, float v2, floa
     const unsigned hi = __builtin_amdgcn_perm(code_bits(v3, c), code_bits(v2, c), 0x04000c0cu);
     return (lo | hi) & c.keep;
 }
-__device__ __forceinline__ void store_codes(int8_t *p, const float (&v)[8], const RowCode &c) {
-    *reinterpret_cast<u32x2_any *>(p) = (u32x2){code_word(v[0], v[1], v[2], v[3], c), code_word(v[4], v[5], v[6], v[7], c)};
+__device__ __forceinline__ void store_codes(int8_t *p, const float (&v)[8], const RowCode &c, bool past) {
+    store_vector(reinterpret_cast<u32x2_any *>(p), (u32x2){code_word(v[0], v[1], v[2], v[3], c), code_word(v[4], v[5], v[6], v[7], c)}, past);
 }
-__device__ __forceinline__ void store_codes(int8_t *p, const float (&v)[1], const RowCode &c) {
+__device__ __forceinline__ void store_codes(int8_t *p, const float (&v)[1], const RowCode &c, bool) {
     *p = (int8_t)(code_bits(v[0], c) & c.keep);
 }
 
