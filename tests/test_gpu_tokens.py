@@ -254,10 +254,11 @@ def test_norm_without_spread_or_parameters(gpu):
         assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("pixels", [40, 9001])      # an image that a block holds, and one in two passes
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_norm_keeps_what_is_not_finite_in_its_group(gpu, bad):
+def test_norm_keeps_what_is_not_finite_in_its_group(gpu, bad, pixels):
     torch, b = gpu
-    x, gamma, beta = norm_inputs(3, 40, 48, 4)
+    x, gamma, beta = norm_inputs(3, pixels, 48, 4)
     x = dev(torch, x)
     clean = b.gspc_group_norm(x, dev(torch, gamma), dev(torch, beta), 6, act=b.ACT_RELU)
     x[1, 13, 17] = bad
