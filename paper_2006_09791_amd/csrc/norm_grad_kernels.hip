@@ -267,11 +267,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape
     }
 }
 
-// All but the sum over images in one launch, x and dy read once: a block holds its channels of an image.  Up to four vectors a
-// thread dz stays in fp32, so that the activation's slope is computed once (256 images of 14x14, 512 channels in bf16 with SiLU:
-// 36 us, 44 with it computed twice); eight leave no room for that (they spill: 69 us instead of 39 on 28x28, 128 channels from
-// 8-bit rows), and it is computed again from what was loaded.  sums: [n][2][C] for the parameters' gradients, or where there is
-// one image these themselves.
+// All but the sum over images in one launch, x and dy read once: a block holds its channels of an image, x as it came and dz in fp32,
+// so that the activation's slope is computed once (256 images of 14x14, 512 channels in bf16 with SiLU: 36 us; with x and dy held as
+// they came and it computed twice 44).  Four vectors a thread: with eight dz spills (69 us on 28x28, 128 channels from 8-bit rows; four in
+// 1024 threads 40).  sums: [n][2][C] for the parameters' gradients, or where there is one image these themselves.
 template <typename TX, typename TG, int V, int E, int HELD>
 __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldGrid g, const TG *__restrict__ dy, size_t lddy,
                                                              const TX *__restrict__ x, size_t ldx, const float *__restrict__ x_scale,
@@ -279,7 +278,6 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
                                                              const float *__restrict__ beta, float *__restrict__ sum_dz,
                                                              float *__restrict__ sum_dx, size_t ld_sums, TG *__restrict__ dx, size_t lddx,
                                                              int past) {
-    constexpr bool KEEP = HELD <= 4;
     extern __shared__ float part[];                 // [2][slots][row], then [2][seg] of the channels, [groups][2] of the groups
     const unsigned block = held_block(g, blockIdx.x), n = fast_div_any(block, g.segs, g.m_segs);
     const int c0 = (block - n * g.segs) * g.seg, row = g.seg + 1;      // (an odd pitch: sums over slots read one column)
@@ -307,22 +305,21 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
         }
     GradAffine<V, E> f;
     load_grad_affine<V, E>(h, stats, gamma, beta, n, c0 + at, f);
-    float kept[KEEP ? HELD : 1][V];
+    float dz[HELD][V];
     {
         float sz[V] = {}, sx[V] = {};
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
             if (k * g.slots < h.P) {
                 float d[V];
-                float (&dz)[V] = kept[KEEP ? k : 0];
                 hold(rx[k]);
                 hold(rg[k]);
                 if ((k + 1) * g.slots > h.P) keep_if(rg[k], slot + k * g.slots < h.P);
                 widen_d<TX, V, E>(f, rx[k], scale[k], d);
-                widen(rg[k], dz);
-                to_dz<V, E>(f, h.act, d, dz);
+                widen(rg[k], dz[k]);
+                to_dz<V, E>(f, h.act, d, dz[k]);
 #pragma unroll
-                for (int e = 0; e < V; ++e) sz[e] += dz[e], sx[e] = fmaf(dz[e], d[e], sx[e]);
+                for (int e = 0; e < V; ++e) sz[e] += dz[k][e], sx[e] = fmaf(dz[k][e], d[e], sx[e]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -368,16 +365,10 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
         if (k * g.slots < h.P) {
             const int p = slot + k * g.slots;
             float d[V];
-            float (&dz)[V] = kept[KEEP ? k : 0];
             hold(rx[k]);
             widen_d<TX, V, E>(f, rx[k], scale[k], d);
-            if constexpr (!KEEP) {
-                hold(rg[k]);
-                widen(rg[k], dz);
-                to_dz<V, E>(f, h.act, d, dz);
-            }
-            to_dx<V, E>(f, s, d, dz);
-            if (on && p < h.P) store(dx + (token0 + p) * lddx + c0 + at, dz, past);
+            to_dx<V, E>(f, s, d, dz[k]);
+            if (on && p < h.P) store(dx + (token0 + p) * lddx + c0 + at, dz[k], past);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -386,35 +377,22 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 constexpr int kBackwardBlocks = 2048, kBackwardChunks = 256;
 
-// Four vectors a thread where 512 threads will do.  Else eight from 8-bit rows and bf16 (48 registers; 256 images of 28x28, 128 channels:
-// 38 us, in 1024 threads 40), or 1024 threads (from bf16 45 us, 59 with eight vectors).
-template <typename TX, typename TG> constexpr int grad_held_most() { return sizeof(TX) == 1 && sizeof(TG) == 2 ? 8 : 4; }
-template <typename TX, typename TG> static bool plan_grad_held(const NormShape &h, HeldGrid *g) {
-    return plan_held(h, sizeof(TG), 4, 512, g) || (grad_held_most<TX, TG>() > 4 && plan_held(h, sizeof(TG), 8, 512, g)) ||
-           plan_held(h, sizeof(TG), 4, 1024, g);
-}
+static bool plan_grad_held(const NormShape &h, int size, HeldGrid *g) { return plan_held(h, size, 4, 512, g) || plan_held(h, size, 4, 1024, g); }
 
-template <typename TX, typename TG> static size_t backward_bytes(const NormShape &h) {
+size_t norm_backward_bytes(const NormShape &h, int dy_dtype) {
     HeldGrid held;
-    const bool hold = plan_grad_held<TX, TG>(h, &held);
+    const bool hold = plan_grad_held(h, dy_dtype == GSPC_F32 ? 4 : 2, &held);
     if (hold && h.N == 1) return 0;
     const size_t sums = (size_t)h.N * 2 * h.C * sizeof(float);
     if (hold) return sums;
     return sums + ((size_t)h.N * norm_grid(h, kBackwardBlocks, kBackwardChunks).chunks * 2 * h.C + (size_t)h.N * h.groups * 2) * sizeof(float);
 }
 
-size_t norm_backward_bytes(const NormShape &h, int dy_dtype, int x_dtype) {
-    if (dy_dtype == GSPC_F32)
-        return x_dtype == GSPC_F32 ? backward_bytes<float, float>(h) : x_dtype == GSPC_BF16 ? backward_bytes<uint16_t, float>(h) : backward_bytes<int8_t, float>(h);
-    return x_dtype == GSPC_F32 ? backward_bytes<float, uint16_t>(h) : x_dtype == GSPC_BF16 ? backward_bytes<uint16_t, uint16_t>(h) : backward_bytes<int8_t, uint16_t>(h);
-}
-
 template <typename TX, typename TG, int V, int E>
 static hipError_t launch_grad_held(const NormShape &h, HeldGrid g, const NormBackward &b, float *sums, hipStream_t s) {
-    constexpr int MOST = grad_held_most<TX, TG>();
     const int held = (h.P + g.slots - 1) / g.slots;
     const auto kern = held <= 1 ? norm_grad_held_kernel<TX, TG, V, E, 1> : held <= 2 ? norm_grad_held_kernel<TX, TG, V, E, 2>
-                    : held <= 4 ? norm_grad_held_kernel<TX, TG, V, E, 4> : norm_grad_held_kernel<TX, TG, V, E, MOST>;
+                                                                          : norm_grad_held_kernel<TX, TG, V, E, 4>;
     g.log_lanes = 0;
     while ((1 << g.log_lanes) < g.slots && g.log_lanes < 6 && (4 * g.seg << g.log_lanes) <= g.threads) ++g.log_lanes;
     const size_t lds = (2 * (size_t)g.slots * (g.seg + 1) + 2 * g.seg + 2 * (g.seg / h.D) + 1) * sizeof(float);
@@ -468,7 +446,7 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
     float *parts = reinterpret_cast<float *>(ab + (size_t)h.N * h.groups);
     b.past = (size_t)h.N * h.P * h.C * sizeof(TG) >= kPastCaches;
     HeldGrid held;
-    const bool hold = plan_grad_held<TX, TG>(h, &held);
+    const bool hold = plan_grad_held(h, sizeof(TG), &held);
     *name = hold ? "norm_grad_held" : "norm_grad_apply";
     const auto run = [&](auto e) {
         constexpr int E = decltype(e)::value;

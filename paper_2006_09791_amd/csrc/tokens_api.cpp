@@ -122,7 +122,7 @@ size_t gspc_group_norm_backward_workspace_bytes(int N, int P, int C, int groups,
     gspc::NormShape h;
     if (check_norm(N, P, C, groups, GSPC_ACT_NONE, &h) || (int64_t)N * P == 0) return 0;
     if (!dense(dy_dtype) || (!dense(x_dtype) && x_dtype != GSPC_I8)) return fail(GSPC_ERR_DTYPE, "unknown dtype (%d, %d)", dy_dtype, x_dtype), 0;
-    return gspc::norm_backward_bytes(h, dy_dtype, x_dtype);
+    return gspc::norm_backward_bytes(h, dy_dtype);
 }
 
 int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma, const float *beta, int N, int P, int C, int groups,
@@ -161,7 +161,7 @@ int gspc_group_norm_backward(const void *dy, int dy_dtype, int64_t lddy, const v
     if (misaligned(stats, 8)) return fail(GSPC_ERR_ARG, "stats must be 8-byte aligned");
     if ((int64_t)N * P > 0) {
         if (!dy || !x || !dx || !stats || (codes && !x_scale)) return fail(GSPC_ERR_NULL, "null pointer argument");
-        if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_backward_bytes(h, dy_dtype, x_dtype)))) return rc;
+        if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_backward_bytes(h, dy_dtype)))) return rc;
     }
     if (codes) ldx = gspc_rows8_pitch(C);
     const gspc::NormBackward b = {dy, dy_dtype, (size_t)lddy, x, x_dtype, (size_t)ldx, x_scale, stats, gamma, beta,

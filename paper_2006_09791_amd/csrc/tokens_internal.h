@@ -53,7 +53,7 @@ struct NormBackward {
 };
 // Workspace of a call; rows8: one that writes 8-bit rows.
 size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8);
-size_t norm_backward_bytes(const NormShape &h, int dy_dtype, int x_dtype);
+size_t norm_backward_bytes(const NormShape &h, int dy_dtype);
 hipError_t launch_norm_forward(const NormShape &h, const NormForward &f, void *ws, hipStream_t s, const char **name);
 hipError_t launch_norm_backward(const NormShape &h, const NormBackward &b, void *ws, hipStream_t s, const char **name);
 
