@@ -91,7 +91,7 @@ __device__ __forceinline__ unsigned held_block(const HeldGrid &g, unsigned b) {
 }
 
 // Sums over the tokens of an image and the channels of a group.  `part` holds [slots][row] values, row = seg / unit; one wave
-// takes a group, and leaves f(sum) in out[group].
+// takes a group, and one of its lanes calls f(group, sum).
 template <typename F>
 __device__ __forceinline__ void held_group_sums(const HeldGrid &g, const float *part, int row, int groups, F f) {
     const int lane = threadIdx.x % kWave, waves = (g.threads + kWave - 1) / kWave;
@@ -128,8 +128,8 @@ inline bool held_grid(const NormShape &h, int groups, int threads, int held, Hel
     return blocks < 0x7fffffffu / 1024;
 }
 
-// The grid that is taken, or false: segments of 64 bytes of a token at least (of `size` bytes a value; half a cache line: with 32
-// the same kernel took 71 instead of 53 us on 64 images of 56x56, 256 channels in bf16), of 128 where that leaves four blocks for
+// The grid that is taken, or false: segments of 64 bytes of a token at least (of `size` bytes a value; half a cache line: in pieces of
+// 32 group norm of 64 images of 56x56, 256 channels in bf16 took 71 us, and 114 past the caches), of 128 where that leaves four blocks for
 // each compute unit; as few threads as hold them in `held` vectors each (`most` at most), more where the launch does not fill the
 // chip with them (one image of 7x7, 512 channels in fp32: 3.8 us with 64 threads, 3.5 with 128).
 inline bool plan_held(const NormShape &h, int size, int held, int most, HeldGrid *best) {
