@@ -380,6 +380,7 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
 // ---- launches ---------------------------------------------------------------------------------------------------------------
 constexpr int kBackwardBlocks = 2048, kBackwardChunks = 256;
 
+// Up to 512 threads where four vectors each hold the channels; 1024 leave one block a compute unit and are taken where 512 do not.
 static bool plan_grad_held(const NormShape &h, int size, HeldGrid *g) { return plan_held(h, size, 4, 512, g) || plan_held(h, size, 4, 1024, g); }
 
 size_t norm_backward_bytes(const NormShape &h, int dy_dtype) {

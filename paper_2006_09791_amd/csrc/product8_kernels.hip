@@ -164,7 +164,7 @@ constexpr int kStep = 128;              // bytes of a row that one stage holds: 
 // LDS directly (16 bytes a lane, eight rows a wave), STAGES - 1 ahead of the products.  Within a row the 16-byte pieces are permuted by the row's number, so that the
 // lanes that read one column of pieces spread over all banks; a load's lanes fetch from the addresses that this asks for.
 // 8192 x 4096 x 8192 to bf16: 217 to 239 us, 2.3 to 2.5 POP/s.  A copy of the loop without its loads took 210, and whole products of zeros a
-// quarter less than of random values: the chip's power sets the clock.  12544 x 512 x 1024 (196 tiles, one round): 12.9 us.  Stages of
+// quarter less than of random values: the chip's power sets the clock.  12544 x 1024 x 512 (196 tiles, one round): 12.9 us.  Stages of
 // 64 bytes, four of them, took 285 us instead of 255 (two requests for a cache line).  Four waves of 128 x 128 products each instead of eight
 // of 128 x 64 were level where K is long and behind where it is short.
 template <typename T, int WM, int WN, int TM, int TN, int STAGES>
