@@ -512,3 +512,76 @@ def test_rows_past_32_bits(gpu):
     w = (torch.randint(-127, 128, (C, 48), dtype=torch.int8, device="cuda"), torch.rand(C, device="cuda"))
     b.gspc_matmul_i8(a, w, out=y)
     assert torch.equal(y, b.gspc_matmul_i8(a, w))
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_workspace_is_as_large_as_said(gpu, shape, kind):
+    """What a workspace held before does not matter, and a call given as many bytes as it asks for leaves what lies behind them."""
+    torch, b = gpu
+    N, P, C, groups = shape
+    x, gamma, beta = norm_inputs(N, P, C, 11)
+    x, gamma, beta = dev(torch, x, getattr(torch, kind)), dev(torch, gamma), dev(torch, beta)
+    dtype = b.GSPC_F32 if kind == "float32" else b.GSPC_BF16
+
+    def scratch(need):
+        whole = torch.full((need // 4 + 64,), float("nan"), device="cuda")
+        whole[need // 4:] = 7.0
+        return whole, whole[:need // 4]
+
+    def run(forward, rows8, backward, backward8):
+        st = torch.empty(N, groups, 2, device="cuda")
+        y = b.gspc_group_norm(x, gamma, beta, groups, act=b.ACT_SILU, stats=st, workspace=forward)
+        q = b.gspc_group_norm(x, gamma, beta, groups, act=b.ACT_SILU, dtype=b.GSPC_I8, workspace=rows8)
+        kept = b.gspc_quantize_rows(x)
+        return (y, st, *q, *b.gspc_group_norm_backward(y, x, st, gamma, beta, groups, b.ACT_SILU, workspace=backward),
+                *b.gspc_group_norm_backward(y, kept, st, gamma, beta, groups, b.ACT_SILU, workspace=backward8))
+
+    needs = [b.gspc_group_norm_workspace_bytes(N, P, C, groups, dtype), b.gspc_group_norm_workspace_bytes(N, P, C, groups, dtype, True),
+             b.gspc_group_norm_backward_workspace_bytes(N, P, C, groups, dtype, dtype),
+             b.gspc_group_norm_backward_workspace_bytes(N, P, C, groups, dtype, b.GSPC_I8)]
+    assert all(n % 4 == 0 for n in needs)
+    spaces = [scratch(n) for n in needs]
+    got = run(*(view for _, view in spaces))
+    assert all(bool((whole[n // 4:] == 7.0).all()) for (whole, _), n in zip(spaces, needs))
+    assert all(bool(t.isfinite().all()) for t in got)
+    assert all(torch.equal(p, q) for p, q in zip(got, run(None, None, None, None)))
+
+
+def test_tensors_past_32_bits(gpu):
+    """Contiguous tensors of more than 2^32 elements: the same few images over and over.  The last ones get what the first ones get,
+    bit by bit, and those what a small call gives: sums may be in another order there, so that a value may be rounded to the
+    bf16 beside it (2^-8 of it), and 2^-12 stands for what sums of values around 1 leave."""
+    torch, b = gpu
+    P, C, few = 64, 128, 8
+    N = (1 << 32) // (P * C) + few                              # 2^32 and eight images more
+    small = torch.randn(few, P, C, device="cuda").bfloat16()
+    x = small.repeat(N // few, 1, 1)
+    assert x.numel() > 1 << 32
+
+    def check(big, want):
+        n = want.shape[0]
+        assert torch.equal(big[:n], big[-n:])
+        assert bool(((big[:n].float() - want.float()).abs() <= B * want.float().abs() + 2.0 ** -12).all())
+
+    out = torch.empty_like(x)
+    b.gspc_pack_channels_last(x, out=out.view(N, C, P))         # (planes of 64 channels as tokens)
+    check(out.view(N, C, P), b.gspc_pack_channels_last(small))
+    gamma, beta = 1 + 0.1 * torch.randn(C, device="cuda"), 0.1 * torch.randn(C, device="cuda")
+    st, few_st = torch.empty(N, 8, 2, device="cuda"), torch.empty(few, 8, 2, device="cuda")
+    b.gspc_group_norm(x, gamma, beta, 8, act=b.ACT_SILU, out=out, stats=st)
+    check(out, b.gspc_group_norm(small, gamma, beta, 8, act=b.ACT_SILU, stats=few_st))
+    check(st, few_st)
+    b.gspc_group_norm_backward(x, x, st, gamma, beta, 8, b.ACT_SILU, dx=out)
+    check(out, b.gspc_group_norm_backward(small, small, few_st, gamma, beta, 8, b.ACT_SILU)[0])
+    q = b.gspc_group_norm(x, gamma, beta, 8, act=b.ACT_SILU, dtype=b.GSPC_I8)
+    first = tuple(t[:few * P] for t in q)
+    assert all(torch.equal(t[-few * P:], f) for t, f in zip(q, first))
+    check(q[1], b.gspc_group_norm(small, gamma, beta, 8, act=b.ACT_SILU, dtype=b.GSPC_I8)[1])
+    w = b.gspc_quantize_rows(torch.randn(C, C, device="cuda"))
+    b.gspc_matmul_i8(q, w, out=out)
+    check(out.view(N * P, C), b.gspc_matmul_i8(first, w))
+    b.gspc_dequantize_rows(q, C, out=out)
+    check(out.view(N * P, C), b.gspc_dequantize_rows(first, C, dtype=b.GSPC_BF16))
+    again = b.gspc_quantize_rows(out)
+    assert all(torch.equal(t[-few * P:], t[:few * P]) for t in again)
