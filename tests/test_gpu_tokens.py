@@ -1,7 +1,7 @@
 """Channels-last operators on the GPU against their definitions in 64 bits (numpy): layout passes, 8-bit rows, group norm with an
 activation and its gradient, products of 8-bit rows.
 
-Tolerances, with u = 2^-24 (fp32) and 2^-8 for a value rounded to bf16 (half of its last place is 2^-9 of it):
+Tolerances, with u = 2^-24 (fp32) and 2^-8 for a value rounded to bf16 (half of its last place is 2^-9 to 2^-8 of it):
   group norm: x - mean is rounded and so is the mean, u (|x| + |mean|) rstd <= 2 u (|xh| + |mean| rstd) of xh; the mean's and the
   variance's own sums, of differences and in tree order, stay below 64 u of the group's spread (chains of at most 32 terms behind
   one another, joined in trees).  SiLU's slope is below 1.1 and its own rounding a few u.  Together 256 u (1 + |xh| + |mean| rstd)
@@ -549,39 +549,38 @@ def test_workspace_is_as_large_as_said(gpu, shape, kind):
 
 
 def test_tensors_past_32_bits(gpu):
-    """Contiguous tensors of more than 2^32 elements: the same few images over and over.  The last ones get what the first ones get,
-    bit by bit, and those what a small call gives: sums may be in another order there, so that a value may be rounded to the
-    bf16 beside it (2^-8 of it), and 2^-12 stands for what sums of values around 1 leave."""
+    """Contiguous tensors of more than 2^32 elements: the same 2048 images over and over.  The first and the last ones get, bit by
+    bit, what these images get by themselves (2048 fill the chip, so that sums are taken in the same order)."""
     torch, b = gpu
-    P, C, few = 64, 128, 8
-    N = (1 << 32) // (P * C) + few                              # 2^32 and eight images more
-    small = torch.randn(few, P, C, device="cuda").bfloat16()
-    x = small.repeat(N // few, 1, 1)
-    assert x.numel() > 1 << 32
+    P, C, some = 64, 128, 2048
+    N = (1 << 32) // (P * C) + some                             # 2^32 and 2048 images more
+    small = torch.randn(some, P, C, device="cuda").bfloat16()
+    x = small.repeat(N // some, 1, 1)
+    assert N % some == 0 and x.numel() > 1 << 32
 
     def check(big, want):
         n = want.shape[0]
-        assert torch.equal(big[:n], big[-n:])
-        assert bool(((big[:n].float() - want.float()).abs() <= B * want.float().abs() + 2.0 ** -12).all())
+        assert torch.equal(big[:n], want) and torch.equal(big[-n:], want)
 
     out = torch.empty_like(x)
     b.gspc_pack_channels_last(x, out=out.view(N, C, P))         # (planes of 64 channels as tokens)
     check(out.view(N, C, P), b.gspc_pack_channels_last(small))
     gamma, beta = 1 + 0.1 * torch.randn(C, device="cuda"), 0.1 * torch.randn(C, device="cuda")
-    st, few_st = torch.empty(N, 8, 2, device="cuda"), torch.empty(few, 8, 2, device="cuda")
+    st, some_st = torch.empty(N, 8, 2, device="cuda"), torch.empty(some, 8, 2, device="cuda")
     b.gspc_group_norm(x, gamma, beta, 8, act=b.ACT_SILU, out=out, stats=st)
-    check(out, b.gspc_group_norm(small, gamma, beta, 8, act=b.ACT_SILU, stats=few_st))
-    check(st, few_st)
+    check(out, b.gspc_group_norm(small, gamma, beta, 8, act=b.ACT_SILU, stats=some_st))
+    check(st, some_st)
     b.gspc_group_norm_backward(x, x, st, gamma, beta, 8, b.ACT_SILU, dx=out)
-    check(out, b.gspc_group_norm_backward(small, small, few_st, gamma, beta, 8, b.ACT_SILU)[0])
+    check(out, b.gspc_group_norm_backward(small, small, some_st, gamma, beta, 8, b.ACT_SILU)[0])
     q = b.gspc_group_norm(x, gamma, beta, 8, act=b.ACT_SILU, dtype=b.GSPC_I8)
-    first = tuple(t[:few * P] for t in q)
-    assert all(torch.equal(t[-few * P:], f) for t, f in zip(q, first))
-    check(q[1], b.gspc_group_norm(small, gamma, beta, 8, act=b.ACT_SILU, dtype=b.GSPC_I8)[1])
+    some_q = b.gspc_group_norm(small, gamma, beta, 8, act=b.ACT_SILU, dtype=b.GSPC_I8)
+    for t, want in zip(q, some_q):
+        check(t, want)
     w = b.gspc_quantize_rows(torch.randn(C, C, device="cuda"))
     b.gspc_matmul_i8(q, w, out=out)
-    check(out.view(N * P, C), b.gspc_matmul_i8(first, w))
+    check(out.view(N * P, C), b.gspc_matmul_i8(some_q, w))
     b.gspc_dequantize_rows(q, C, out=out)
-    check(out.view(N * P, C), b.gspc_dequantize_rows(first, C, dtype=b.GSPC_BF16))
-    again = b.gspc_quantize_rows(out)
-    assert all(torch.equal(t[-few * P:], t[:few * P]) for t in again)
+    tokens = b.gspc_dequantize_rows(some_q, C, dtype=b.GSPC_BF16)
+    check(out.view(N * P, C), tokens)
+    for t, want in zip(b.gspc_quantize_rows(out), b.gspc_quantize_rows(tokens)):
+        check(t, want)
