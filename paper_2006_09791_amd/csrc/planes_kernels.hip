@@ -14,9 +14,9 @@ constexpr int kTile = 64, kTilePitch = kTile + 1;
 // 128 x 784 from fp32 to bf16 27.8 us, 5.5 TB/s, what a large copy reaches.
 template <typename TI, typename TO, int VI, int VO>
 __global__ __launch_bounds__(256) void transpose_kernel(const TI *__restrict__ in, TO *__restrict__ out, int R, int S, unsigned rtiles,
-                                                       unsigned tiles, unsigned m_rtiles, unsigned m_tiles, int past) {
+                                                       unsigned tiles, unsigned m_rtiles, unsigned m_tiles, int past, unsigned first) {
     __shared__ float lds[kTile * kTilePitch];
-    const unsigned n = fast_div_any(blockIdx.x, tiles, m_tiles), t = blockIdx.x - n * tiles;
+    const unsigned b = first + blockIdx.x, n = fast_div_any(b, tiles, m_tiles), t = b - n * tiles;
     const unsigned st = fast_div_any(t, rtiles, m_rtiles), rt = t - st * rtiles;
     const int wr = min(R, kTile), ws = min(S, kTile);
     const int r0 = min((int)rt * kTile, R - wr), s0 = min((int)st * kTile, S - ws);
@@ -107,32 +107,36 @@ __global__ __launch_bounds__(256) void transpose_thin_kernel(const TI *__restric
     }
 }
 
+// Launches for N images of `tiles` blocks each: f(first image, first tile, blocks).
+template <typename F> static void in_launches(int N, unsigned tiles, unsigned threads, const F &f) {
+    const unsigned most = most_blocks(threads);
+    const long step = tiles > most ? 1 : most / tiles;
+    for (long n = 0; n < N; n += step) {
+        const unsigned all = tiles * (unsigned)(N - n < step ? N - n : step);      // more than a launch may have: of one image
+        for (unsigned first = 0; first < all; first += most) f((size_t)n, first, all - first < most ? all - first : most);
+    }
+}
+
 template <typename TI, typename TO>
 static hipError_t transpose(const void *in, int N, int R, int S, void *out, hipStream_t s) {
     const int past = (size_t)N * R * S * sizeof(TO) >= kPastCaches;
     if ((R < 8) != (S < 8)) {                       // 152 images of 6 x 10954 in bf16: 17.8 us in tiles of 64 x 64
         const int thin = R < S ? R : S, wide = R < S ? S : R;
-        const unsigned tiles = (wide + kLong - 1) / kLong;
+        const unsigned tiles = (wide - 1) / kLong + 1;
         const auto kern = S < R ? transpose_thin_kernel<TI, TO, true> : transpose_thin_kernel<TI, TO, false>;
-        const int step = N < (int)(0x7fffffffu / tiles) ? N : (int)(0x7fffffffu / tiles);
-        for (int n = 0; n < N; n += step) {
-            const int count = N - n < step ? N - n : step;
-            hipLaunchKernelGGL(kern, dim3(tiles * count), dim3(256), 0, s, static_cast<const TI *>(in) + (size_t)n * R * S,
-                               static_cast<TO *>(out) + (size_t)n * R * S, thin, wide, tiles, div_magic(tiles), div_magic(thin), past);
-        }
+        in_launches(N, tiles, 256, [&](size_t n, unsigned, unsigned blocks) {      // (an image is at most 2^21 tiles)
+            hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, static_cast<const TI *>(in) + n * R * S,
+                               static_cast<TO *>(out) + n * R * S, thin, wide, tiles, div_magic(tiles), div_magic(thin), past);
+        });
         return hipGetLastError();
     }
-    const unsigned rt = (R + kTile - 1) / kTile, st = (S + kTile - 1) / kTile;
-    const unsigned long long tiles = (unsigned long long)rt * st;
+    const unsigned rt = (R - 1) / kTile + 1, st = (S - 1) / kTile + 1;
+    const unsigned tiles = rt * st;
     const auto kern = R >= 8 ? transpose_kernel<TI, TO, 8, 8> : transpose_kernel<TI, TO, 1, 1>;
-    // images of one launch: blocks are numbered in 31 bits
-    const int step = (int)(tiles * N < 0x7fffffffull ? N : 0x7fffffffull / tiles);
-    for (int n = 0; n < N; n += step) {
-        const int count = N - n < step ? N - n : step;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * count)), dim3(256), 0, s, static_cast<const TI *>(in) + (size_t)n * R * S,
-                           static_cast<TO *>(out) + (size_t)n * R * S, R, S, rt, (unsigned)tiles, div_magic(rt), div_magic((unsigned)tiles),
-                           R >= kTile && past);
-    }
+    in_launches(N, tiles, 256, [&](size_t n, unsigned first, unsigned blocks) {
+        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, static_cast<const TI *>(in) + n * R * S,
+                           static_cast<TO *>(out) + n * R * S, R, S, rt, tiles, div_magic(rt), div_magic(tiles), R >= kTile && past, first);
+    });
     return hipGetLastError();
 }
 

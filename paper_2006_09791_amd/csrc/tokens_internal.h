@@ -10,6 +10,9 @@ hipStream_t current_stream();
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 void set_last_kernel(const char *name);
 
+// Blocks of one launch at most: HIP numbers a dimension's threads, not its blocks, in 32 bits.
+constexpr unsigned most_blocks(unsigned threads) { return 0xffffffffu / threads; }
+
 // in [N][R][S] -> out [N][S][R]
 hipError_t launch_transpose(const void *in, int in_dtype, int N, int R, int S, void *out, int out_dtype, hipStream_t s);
 
