@@ -64,6 +64,11 @@ inline NormGrid norm_grid(const NormShape &h, int blocks_wanted, int most_chunks
     return g;
 }
 
+// Images of one launch at most of a grid's kernels, and of those with a block of 256 threads an image.
+inline long norm_images(const NormGrid &g) {
+    return most_blocks(g.threads > 256 ? g.threads : 256) / ((unsigned)g.chunks * (unsigned)g.slabs);
+}
+
 // Lanes that share a sum of `count` values, where `sums` of them are taken by `threads` threads: a power of two up to a wave.
 inline int group_lanes(int count, long sums, long threads) {
     int w = 1;

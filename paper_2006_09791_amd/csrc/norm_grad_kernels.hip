@@ -170,34 +170,39 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape h, int ch
     if (lane == 0) ab[pair] = make_float2(a / m, b / m);
 }
 
-// dgamma and dbeta: 64 channels a block, its waves (MOST at most) take the rows of sums ([rows][2][C]: of images, or of their parts)
-// in turn.
+// dgamma and dbeta: `blocks` blocks take 64 channels at a time, in turn, and their waves (MOST at most) the rows of sums ([rows][2][C]: of
+// images, or of their parts).
 template <int MOST>
-__device__ __forceinline__ void sum_params(int C, int block, int rows, const float *__restrict__ sums, float *__restrict__ dgamma,
-                                           float *__restrict__ dbeta) {
+__device__ __forceinline__ void sum_params(int C, unsigned block, unsigned blocks, int rows, const float *__restrict__ sums,
+                                           float *__restrict__ dgamma, float *__restrict__ dbeta) {
     __shared__ float s_sum[2][MOST][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave, c = block * kWave + lane;
-    float sz = 0.f, sx = 0.f;
-    if (c < C) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    for (unsigned c = block * kWave + lane; c - lane < (unsigned)C; c += blocks * kWave) {
+        float sz = 0.f, sx = 0.f;
+        if (c < (unsigned)C) {
 #pragma unroll 8
-        for (int n = wave; n < rows; n += waves) sz += sums[(size_t)n * 2 * C + c], sx += sums[((size_t)n * 2 + 1) * C + c];
-    }
-    s_sum[0][wave][lane] = sz;
-    s_sum[1][wave][lane] = sx;
-    __syncthreads();
-    for (int which = wave; which < 2; which += waves) {
-        if (c >= C) continue;
-        float sum = 0.f;
-        for (int w = 0; w < waves; ++w) sum += s_sum[which][w][lane];
-        if (which == 0 && dbeta) dbeta[c] = sum;
-        if (which == 1 && dgamma) dgamma[c] = sum;
+            for (int n = wave; n < rows; n += waves) sz += sums[(size_t)n * 2 * C + c], sx += sums[((size_t)n * 2 + 1) * C + c];
+        }
+        s_sum[0][wave][lane] = sz;
+        s_sum[1][wave][lane] = sx;
+        __syncthreads();
+        for (int which = wave; which < 2; which += waves) {
+            if (c >= (unsigned)C) continue;
+            float sum = 0.f;
+            for (int w = 0; w < waves; ++w) sum += s_sum[which][w][lane];
+            if (which == 0 && dbeta) dbeta[c] = sum;
+            if (which == 1 && dgamma) dgamma[c] = sum;
+        }
+        __syncthreads();
     }
 }
 
 constexpr int kParamWaves = 16;
+constexpr int kParamBlocks = 1 << 16;
+static unsigned param_blocks(int C) { return C > kParamBlocks * kWave ? kParamBlocks : (C + kWave - 1) / kWave; }
 __global__ __launch_bounds__(kParamWaves * kWave) void norm_grad_params_kernel(int C, int rows, const float *__restrict__ sums,
                                                                                float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    sum_params<kParamWaves>(C, blockIdx.x, rows, sums, dgamma, dbeta);
+    sum_params<kParamWaves>(C, blockIdx.x, gridDim.x, rows, sums, dgamma, dbeta);
 }
 
 // An image's groups whose A and B a block of norm_grad_apply_kernel takes from the parts itself, and the channels' sums behind them: in
@@ -217,7 +222,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape
                                                                        float *__restrict__ dbeta) {
     typedef GradBatch<TX, TG, V> Batch;
     __shared__ float2 s_ab[FOLD ? kFoldGroups : 1];
-    if ((int)blockIdx.x < param_blocks) return sum_params<kNormThreads / kWave>(h.C, blockIdx.x, param_rows, sums, dgamma, dbeta);
+    if ((int)blockIdx.x < param_blocks) return sum_params<kNormThreads / kWave>(h.C, blockIdx.x, param_blocks, param_rows, sums, dgamma, dbeta);
     const NormBlock b = norm_block(h, g, blockIdx.x - param_blocks);
     const size_t row0 = (size_t)b.n * h.P + b.r0;
     const TX *px = x + row0 * ldx + b.at;
@@ -411,20 +416,42 @@ static hipError_t launch_grad_held(const NormShape &h, HeldGrid g, const NormBac
     return hipSuccess;
 }
 
+// The call's tensors from image n on.
+template <typename TX, typename TG> static NormBackward from_image(const NormShape &h, NormBackward b, size_t n) {
+    const size_t row = n * h.P;
+    b.dy = static_cast<const TG *>(b.dy) + row * b.lddy;
+    b.x = static_cast<const TX *>(b.x) + row * b.ldx;
+    if (b.x_scale) b.x_scale += row;
+    b.stats += n * h.groups * 2;
+    b.dx = static_cast<TG *>(b.dx) + row * b.lddx;
+    return b;
+}
+
 template <typename TX, typename TG, int V, int E>
 static void launch_grad(const NormShape &h, const NormGrid &g, const NormBackward &b, float *parts, float *sums, float2 *ab, hipStream_t s) {
-    const TX *x = static_cast<const TX *>(b.x);
-    const TG *dy = static_cast<const TG *>(b.dy);
-    const float2 *stats = reinterpret_cast<const float2 *>(b.stats);
-    const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
-    hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TG, V, E>), grid, dim3(g.threads), 0, s, h, g, dy, b.lddy, x, b.ldx, b.x_scale, stats,
-                       b.gamma, b.beta, parts);
-    const bool fold = h.groups <= kFoldGroups && (long)g.chunks * 2 * h.C <= kFoldSums && grid.x <= kFoldBlocks;
-    const unsigned param_blocks = b.dgamma || b.dbeta ? (h.C + kWave - 1) / kWave : 0;
+    const unsigned params = b.dgamma || b.dbeta ? param_blocks(h.C) : 0;
+    const bool fold = h.groups <= kFoldGroups && (long)g.chunks * 2 * h.C <= kFoldSums && (long)h.N * g.chunks * g.slabs <= kFoldBlocks;
+    // f(images, their shape, tensors, blocks) for the images of each launch
+    const auto launches = [&](const auto &f) {
+        const long step = norm_images(g) - kParamBlocks / (g.chunks * g.slabs) - 1;
+        for (long n = 0; n < h.N; n += step) {
+            NormShape some = h;
+            some.N = (int)(h.N - n < step ? h.N - n : step);
+            f((size_t)n, some, from_image<TX, TG>(h, b, n), (unsigned)((size_t)some.N * g.chunks * g.slabs));
+        }
+    };
+    launches([&](size_t n, const NormShape &some, const NormBackward &p, unsigned blocks) {
+        hipLaunchKernelGGL((norm_grad_sums_kernel<TX, TG, V, E>), dim3(blocks), dim3(g.threads), 0, s, some, g, static_cast<const TG *>(p.dy), p.lddy,
+                           static_cast<const TX *>(p.x), p.ldx, p.x_scale, reinterpret_cast<const float2 *>(p.stats), p.gamma, p.beta,
+                           parts + n * g.chunks * 2 * h.C);
+    });
     const auto apply = [&](auto kern, int rows, const float *from) {
-        hipLaunchKernelGGL(kern, dim3(grid.x + param_blocks), dim3(g.threads), 0, s, h, g, dy,
-                           b.lddy, x, b.ldx, b.x_scale, stats, b.gamma, b.beta, ab, static_cast<TG *>(b.dx), b.lddx, b.past, (int)param_blocks,
-                           rows, from, b.dgamma, b.dbeta);
+        launches([&](size_t n, const NormShape &some, const NormBackward &p, unsigned blocks) {
+            const unsigned own = n == 0 ? params : 0;
+            hipLaunchKernelGGL(kern, dim3(blocks + own), dim3(g.threads), 0, s, some, g, static_cast<const TG *>(p.dy), p.lddy,
+                               static_cast<const TX *>(p.x), p.ldx, p.x_scale, reinterpret_cast<const float2 *>(p.stats), p.gamma, p.beta,
+                               ab + n * h.groups, static_cast<TG *>(p.dx), p.lddx, p.past, (int)own, rows, from, p.dgamma, p.dbeta);
+        });
     };
     if (fold) return apply(norm_grad_apply_kernel<TX, TG, V, E, true>, h.N * g.chunks, parts);
     int log_lanes = 0;
@@ -436,12 +463,12 @@ static void launch_grad(const NormShape &h, const NormGrid &g, const NormBackwar
 
 template <typename TX, typename TG, int V>
 static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStream_t s, const char **name) {
-    const dim3 param_blocks((h.C + kWave - 1) / kWave);
+    const dim3 params_grid(param_blocks(h.C));
     const bool params = b.dgamma || b.dbeta;
     if ((long)h.N * h.P == 0) {                     // no tokens: zeros
         *name = "norm_grad_params";
         if (params)
-            hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h.C, 0, (const float *)nullptr, b.dgamma, b.dbeta);
+            hipLaunchKernelGGL(norm_grad_params_kernel, params_grid, dim3(kParamWaves * kWave), 0, s, h.C, 0, (const float *)nullptr, b.dgamma, b.dbeta);
         return hipGetLastError();
     }
     const NormGrid g = norm_grid(h, kBackwardBlocks, kBackwardChunks);
@@ -464,7 +491,7 @@ static hipError_t backward(const NormShape &h, NormBackward b, void *ws, hipStre
     else e = run(std::integral_constant<int, V>{});
     if (e != hipSuccess) return e;
     if (params && hold && h.N > 1)
-        hipLaunchKernelGGL(norm_grad_params_kernel, param_blocks, dim3(kParamWaves * kWave), 0, s, h.C, h.N, sums, b.dgamma, b.dbeta);
+        hipLaunchKernelGGL(norm_grad_params_kernel, params_grid, dim3(kParamWaves * kWave), 0, s, h.C, h.N, sums, b.dgamma, b.dbeta);
     return hipGetLastError();
 }
 

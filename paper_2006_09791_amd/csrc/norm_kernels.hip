@@ -487,6 +487,18 @@ size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8) {
     return stats + (size_t)h.N * g.chunks * norm_parts(h, g) * sizeof(float2);
 }
 
+// The call's tensors from image n on.
+static NormForward from_image(const NormShape &h, NormForward f, size_t n) {
+    const size_t row = n * h.P, pitch = rows8_pitch(h.C);
+    const auto size = [](int dtype) { return dtype == GSPC_F32 ? 4u : 2u; };
+    f.x = static_cast<const char *>(f.x) + row * f.ldx * size(f.x_dtype);
+    f.y = static_cast<char *>(f.y) + row * (f.y_dtype == GSPC_I8 ? pitch : f.ldy * size(f.y_dtype));
+    if (f.y_scale) f.y_scale += row;
+    if (f.stats) f.stats += n * h.groups * 2;
+    if (f.saved) f.saved += row * pitch, f.saved_scale += row;
+    return f;
+}
+
 template <typename TX, int V>
 static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream_t s, const char **name) {
     const NormGrid g = norm_grid(h, kForwardBlocks, kForwardChunks);
@@ -503,28 +515,32 @@ static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream
     }
     const bool rows8 = f.y_dtype == GSPC_I8 || f.saved, fold = !rows8 && h.groups <= kFoldGroups && h.groups * g.chunks <= kFoldParts &&
                       (long)h.N * g.chunks * g.slabs <= kFoldBlocks;
+    *name = f.y_dtype == GSPC_I8 ? "norm_rows<i8>" : f.saved ? "norm_rows<saved>" : "norm_apply";
     if (hold) run_held<TX, void, V>(h, held, f, stats, s);
-    else launch_stats<TX, V>(h, g, f, parts, stats, !fold, s);
-    if (f.y_dtype == GSPC_I8) {
-        *name = "norm_rows<i8>";
-        if (f.saved) launch_rows<TX, int8_t, V, true>(h, f, stats, s);
-        else launch_rows<TX, int8_t, V, false>(h, f, stats, s);
-    } else if (f.saved) {
-        *name = "norm_rows<saved>";
-        if (f.y_dtype == GSPC_F32) launch_rows<TX, float, V, true>(h, f, stats, s);
-        else launch_rows<TX, uint16_t, V, true>(h, f, stats, s);
-    } else {
-        *name = "norm_apply";
-        const dim3 grid((unsigned)((size_t)h.N * g.chunks * g.slabs));
-        const TX *x = static_cast<const TX *>(f.x);
-        const auto run = [&](auto kern, auto *y) {
-            hipLaunchKernelGGL(kern, grid, dim3(g.threads), 0, s, h, g, x, f.ldx, parts, f.eps, fold ? reinterpret_cast<float2 *>(f.stats) : stats,
-                               f.gamma, f.beta, y, f.ldy, f.past);
-        };
-        if (f.y_dtype == GSPC_F32)
-            run(fold ? norm_apply_kernel<TX, float, V, true> : norm_apply_kernel<TX, float, V, false>, static_cast<float *>(f.y));
-        else
-            run(fold ? norm_apply_kernel<TX, uint16_t, V, true> : norm_apply_kernel<TX, uint16_t, V, false>, static_cast<uint16_t *>(f.y));
+    const long step = norm_images(g);
+    for (long n = 0; n < h.N; n += step) {          // (an image that is held has fewer companions than that)
+        NormShape some = h;
+        some.N = (int)(h.N - n < step ? h.N - n : step);
+        const NormForward p = from_image(h, f, n);
+        float2 *const st = stats + n * h.groups, *const pt = parts + n * g.chunks * norm_parts(h, g);
+        if (!hold) launch_stats<TX, V>(some, g, p, pt, st, !fold, s);
+        if (f.y_dtype == GSPC_I8) {
+            if (f.saved) launch_rows<TX, int8_t, V, true>(some, p, st, s);
+            else launch_rows<TX, int8_t, V, false>(some, p, st, s);
+        } else if (f.saved) {
+            if (f.y_dtype == GSPC_F32) launch_rows<TX, float, V, true>(some, p, st, s);
+            else launch_rows<TX, uint16_t, V, true>(some, p, st, s);
+        } else {
+            const dim3 grid((unsigned)((size_t)some.N * g.chunks * g.slabs));
+            const auto run = [&](auto kern, auto *y) {
+                hipLaunchKernelGGL(kern, grid, dim3(g.threads), 0, s, some, g, static_cast<const TX *>(p.x), p.ldx, pt, p.eps,
+                                   fold ? reinterpret_cast<float2 *>(p.stats) : st, p.gamma, p.beta, y, p.ldy, p.past);
+            };
+            if (f.y_dtype == GSPC_F32)
+                run(fold ? norm_apply_kernel<TX, float, V, true> : norm_apply_kernel<TX, float, V, false>, static_cast<float *>(p.y));
+            else
+                run(fold ? norm_apply_kernel<TX, uint16_t, V, true> : norm_apply_kernel<TX, uint16_t, V, false>, static_cast<uint16_t *>(p.y));
+        }
     }
     return hipGetLastError();
 }

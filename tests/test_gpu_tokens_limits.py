@@ -30,3 +30,38 @@ def test_layout_of_one_large_plane(gpu):
     for c in range(C):
         for at in range(0, P, piece):
             assert torch.equal(y[0, at:at + piece, c], number(c, at)), (c, at)
+
+
+def pieces(call, *tensors):
+    """What `call` gives for four million images at a time (the last of them end with the tensors): too many for a block to hold each,
+    as all of them are, so that sums are taken in the same order."""
+    N, step = tensors[0].shape[0], 4_000_000
+    for at in range(0, N, step):
+        at = min(at, N - step)
+        yield slice(at, at + step), call(*(t[at:at + step] for t in tensors))
+
+
+@pytest.mark.parametrize("N,P,C", [(MANY, 1, 16), (9_600_000, 64, 7)])
+def test_norm_of_many_images(gpu, N, P, C):
+    """Every image gets, bit by bit, what it gets among fewer."""
+    torch, b = gpu
+    x = torch.randn(N, P, C, device="cuda", dtype=torch.bfloat16)
+    gamma, beta = 1 + 0.1 * torch.randn(C, device="cuda"), 0.1 * torch.randn(C, device="cuda")
+    norm = lambda t, **k: b.gspc_group_norm(t, gamma, beta, 1, act=b.ACT_SILU, **k)  # noqa: E731
+    st = torch.empty(N, 1, 2, device="cuda")
+    y = norm(x, stats=st)
+    for at, want in pieces(norm, x):
+        assert torch.equal(y[at], want)
+    back = lambda d, t, s: b.gspc_group_norm_backward(d, t, s, gamma, beta, 1, b.ACT_SILU)  # noqa: E731
+    dx = back(x, x, st)[0]
+    for at, want in pieces(back, x, x, st):
+        assert torch.equal(dx[at], want[0])
+    del dx, y, want
+    saved = lambda n: (torch.empty(n, 16, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda"))  # noqa: E731
+    kept = saved(N * P)
+    q = norm(x, dtype=b.GSPC_I8, saved=kept)
+    for at, want in pieces(lambda t: norm(t, dtype=b.GSPC_I8), x):
+        rows = slice(at.start * P, at.stop * P)
+        assert torch.equal(q[0][rows], want[0]) and torch.equal(q[1][rows], want[1])
+        for got, codes in zip(kept, b.gspc_quantize_rows(x[at])):
+            assert torch.equal(got[rows], codes)

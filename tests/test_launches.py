@@ -52,3 +52,82 @@ def test_layout_launches_of_one_large_plane(runtime):
         assert struct.unpack("<I", args[2])[0] == first and first + blocks <= tiles
         at += blocks
     assert at == N * tiles
+
+
+# What the norm's kernels are given: NormShape (N first), and the pointers that go from image to image.
+NORM = {"norm_stats_kernel": [(0, 4), (2, 8), (4, 8)], "norm_join_kernel": [(0, 4), (2, 8), (4, 8)],
+        "norm_apply_kernel": [(0, 4), (2, 8), (6, 8), (9, 8)], "norm_rows_kernel": [(0, 4), (5, 8), (7, 8), (10, 8), (12, 8), (13, 8), (14, 8)],
+        "norm_held_kernel": [(0, 4)],
+        "norm_grad_sums_kernel": [(0, 4), (2, 8), (4, 8), (6, 8), (7, 8), (10, 8)], "norm_grad_join_kernel": [(0, 4), (3, 8), (5, 8), (6, 8)],
+        "norm_grad_apply_kernel": [(0, 4), (2, 8), (4, 8), (6, 8), (7, 8), (10, 8), (11, 8), (14, 4), (15, 4)], "norm_grad_params_kernel": [(0, 4), (1, 4)]}
+X, Y, YS, ST, SV, SS, DX, DG, DB, WS = (BASE + (k << 41) for k in range(10))       # (tensors are below 2^41 bytes)
+
+
+def number(raw):
+    return int.from_bytes(raw, "little")
+
+
+def consecutive(found, kernel, N, per_image):
+    """The launches of `kernel` take the N images in turn, and its pointers go `per_image` bytes (first address, step) with them."""
+    at, some = 0, [f for f in found if f[0] == kernel]
+    for _, blocks, threads, args in some:
+        assert blocks * threads < 1 << 32
+        for raw, (base, step) in zip(args[1:], per_image):
+            assert number(raw) == (base + at * step if base else 0), kernel
+        at += number(args[0])
+    assert at == N, kernel
+    return some
+
+
+# N, P, C, groups: blocks of one row for each image; 448 threads for images of seven channels; 256 threads and two slabs
+MANY_IMAGES = [(17_000_000, 1, 16, 1), (9_600_000, 64, 7, 1), (5_000_000, 1, 2056, 1)]
+
+
+@pytest.mark.parametrize("N,P,C,groups", MANY_IMAGES)
+@pytest.mark.parametrize("kind", ["dense", "rows8", "saved"])
+def test_norm_launches_reach_every_image(runtime, N, P, C, groups, kind):
+    pitch, rows = (C + 15) // 16 * 16, kind == "rows8"
+    need = fake_runtime.b.gspc_group_norm_workspace_bytes(N, P, C, groups, 1, kind != "dense")
+    saved = (SV, SS) if kind == "saved" else (None, None)
+    (rc, found), = fake_runtime.launches(runtime, [("gspc_group_norm", [X, 1, C, None, None, N, P, C, groups, 1e-5, 2, Y, 2 if rows else 1, C,
+                                                                        YS if rows else None, ST, *saved, WS, need])], NORM)
+    assert rc == 0
+    x, st = (X, 2 * P * C), (ST, 8 * groups)
+    slabs = (C + 2047) // 2048
+    first = WS + 8 * N * groups                                 # the parts lie behind the statistics that a caller does not ask for
+    consecutive(found, "norm_stats_kernel", N, [x, (first, 8 * (groups + slabs - 1))])
+    consecutive(found, "norm_join_kernel", N, [(first, 8 * (groups + slabs - 1)), st])
+    if kind == "dense":
+        consecutive(found, "norm_apply_kernel", N, [x, st, (Y, 2 * P * C)])
+    else:
+        y = (Y, P * pitch) if rows else (Y, 2 * P * C)
+        some = consecutive(found, "norm_rows_kernel", N, [x, st, y, (YS if rows else 0, 4 * P), (saved[0] or 0, P * pitch), (saved[1] or 0, 4 * P)])
+        assert all(blocks == number(args[0]) for _, blocks, _, args in some)
+
+
+@pytest.mark.parametrize("N,P,C,groups", MANY_IMAGES + [(1, 1, 1 << 28, 1 << 20), (2, 3, (1 << 30) + 8, 1)])
+@pytest.mark.parametrize("rows8", [False, True])
+def test_gradient_launches_reach_every_image(runtime, N, P, C, groups, rows8):
+    pitch = (C + 15) // 16 * 16
+    need = fake_runtime.b.gspc_group_norm_backward_workspace_bytes(N, P, C, groups, 1, 2 if rows8 else 1)
+    (rc, found), = fake_runtime.launches(runtime, [("gspc_group_norm_backward", [Y, 1, C, X, 2 if rows8 else 1, C, YS if rows8 else None, ST, None, None,
+                                                                                 N, P, C, groups, 2, DX, C, DG, DB, WS, need])], NORM)
+    assert rc == 0
+    for _, blocks, threads, _ in found:
+        assert blocks * threads < 1 << 32
+    if any(k == "norm_grad_held_kernel" for k, *_ in found):
+        return
+    x, dy, scale, st = (X, P * pitch if rows8 else 2 * P * C), (Y, 2 * P * C), (YS if rows8 else 0, 4 * P), (ST, 8 * groups)
+    sums, ab, parts = (WS, 8 * C), (WS + 8 * C * N, 8 * groups), (WS + 8 * C * N + 8 * groups * N, 8 * C)
+    assert found[-1][0] == "norm_grad_apply_kernel" and parts[0] + parts[1] * N <= WS + need
+    consecutive(found, "norm_grad_sums_kernel", N, [dy, x, scale, st, parts])
+    consecutive(found, "norm_grad_join_kernel", N, [parts, sums, ab])
+    some = consecutive(found, "norm_grad_apply_kernel", N, [dy, x, scale, st, ab, (DX, 2 * P * C)])
+    with_params = [args for *_, args in some if number(args[7])]
+    assert len(with_params) == 1 and number(with_params[0][8]) == N
+
+
+def test_gradients_of_many_parameters_without_tokens(runtime):
+    (rc, found), = fake_runtime.launches(runtime, [("gspc_group_norm_backward", [None, 1, 1 << 30, None, 1, 1 << 30, None, None, None, None,
+                                                                                 0, 3, 1 << 30, 1, 2, None, 1 << 30, DG, DB, None, 0])], NORM)
+    assert rc == 0 and len(found) == 1 and found[0][1] * found[0][2] < 1 << 32
