@@ -171,14 +171,15 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormShape h, int ch
 }
 
 // dgamma and dbeta: `blocks` blocks take 64 channels at a time, in turn, and their waves (MOST at most) the rows of sums ([rows][2][C]: of
-// images, or of their parts).
+// images, or of their parts).  In 64 bits: millions of images added up in 32 lose what is small against their sum (17 million of one
+// pixel each: 5 % of dgamma).
 template <int MOST>
 __device__ __forceinline__ void sum_params(int C, unsigned block, unsigned blocks, int rows, const float *__restrict__ sums,
                                            float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    __shared__ float s_sum[2][MOST][kWave];
+    __shared__ double s_sum[2][MOST][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
     for (unsigned c = block * kWave + lane; c - lane < (unsigned)C; c += blocks * kWave) {
-        float sz = 0.f, sx = 0.f;
+        double sz = 0., sx = 0.;
         if (c < (unsigned)C) {
 #pragma unroll 8
             for (int n = wave; n < rows; n += waves) sz += sums[(size_t)n * 2 * C + c], sx += sums[((size_t)n * 2 + 1) * C + c];
@@ -188,10 +189,10 @@ __device__ __forceinline__ void sum_params(int C, unsigned block, unsigned block
         __syncthreads();
         for (int which = wave; which < 2; which += waves) {
             if (c >= (unsigned)C) continue;
-            float sum = 0.f;
+            double sum = 0.;
             for (int w = 0; w < waves; ++w) sum += s_sum[which][w][lane];
-            if (which == 0 && dbeta) dbeta[c] = sum;
-            if (which == 1 && dgamma) dgamma[c] = sum;
+            if (which == 0 && dbeta) dbeta[c] = (float)sum;
+            if (which == 1 && dgamma) dgamma[c] = (float)sum;
         }
         __syncthreads();
     }

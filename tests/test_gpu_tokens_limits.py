@@ -65,3 +65,26 @@ def test_norm_of_many_images(gpu, N, P, C):
         assert torch.equal(q[0][rows], want[0]) and torch.equal(q[1][rows], want[1])
         for got, codes in zip(kept, b.gspc_quantize_rows(x[at])):
             assert torch.equal(got[rows], codes)
+
+
+@pytest.mark.parametrize("N,P,C", [(MANY, 1, 16), (3_000_000, 1, 9), (200_000, 65, 24)])
+def test_parameter_gradients_of_many_images(gpu, N, P, C):
+    """Against sums in 64 bits, which images' own sums enter without another rounding: 256 u of the sum of magnitudes, as for one image."""
+    torch, b = gpu
+    x = torch.randn(N, P, C, device="cuda", dtype=torch.bfloat16)
+    gamma, beta = 1 + 0.1 * torch.randn(C, device="cuda"), 0.1 * torch.randn(C, device="cuda")
+    st = torch.empty(N, 1, 2, device="cuda")
+    b.gspc_group_norm(x, gamma, beta, 1, stats=st)
+    _, dgamma, dbeta = b.gspc_group_norm_backward(x, x, st, gamma, beta, 1, b.ACT_SILU)
+    sums, sizes = torch.zeros(2, C, dtype=torch.float64, device="cuda"), torch.zeros(2, C, dtype=torch.float64, device="cuda")
+    for at in range(0, N, 1_000_000):
+        at = slice(at, at + 1_000_000)
+        xh = (x[at].double() - st[at][..., :1]) * st[at][..., 1:]
+        z = xh * gamma + beta
+        dz = x[at].double() * (torch.sigmoid(z) * (1 + z * (1 - torch.sigmoid(z))))
+        for k, t in enumerate((dz * xh, dz)):
+            sums[k] += t.sum((0, 1))
+            sizes[k] += t.abs().sum((0, 1))
+    shift = float((st[..., 0] * st[..., 1]).abs().max())
+    off = (torch.stack((dgamma, dbeta)) - sums).abs() / (256 * 2.0 ** -24 * (1 + shift) * sizes)
+    assert bool((off <= 1).all()), off.max()
