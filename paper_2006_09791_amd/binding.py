@@ -594,15 +594,21 @@ def gspc_group_norm_backward(dy, x, stats, gamma, beta, groups, act=ACT_NONE, dx
     return dx, dgamma, dbeta
 
 
-def gspc_matmul_i8(a, w, bias=None, out=None, dtype=GSPC_BF16):
-    """8-bit rows a (M tokens) and w (N filters) of the same length -> [M, N]; `out`: a tensor [..., N] to write into."""
-    if out is not None and _fast is not None and _done(_fast.matmul(a, w, bias, out)):
+def gspc_matmul_i8(a, w, bias=None, out=None, dtype=GSPC_BF16, cols=None):
+    """8-bit rows a (M tokens) and w (N filters) of the same length -> [M, N]; `out`: a tensor [..., N] to write into.  cols: that
+    length, checked against both; without it all of the rows' pitch is summed, whose padding is zero (rows of 133137 to 133144 values,
+    the longest there are, have a longer pitch than may be summed, and need it)."""
+    if out is not None and _fast is not None and _done(_fast.matmul(a, w, bias, out, cols)):
         return out
     import torch
     lib = load()
     K, M, N = a[0].shape[-1], a[1].numel(), w[1].numel()
     if w[0].shape[-1] != K:
         raise GspcError(-5, f"tokens of {K} values, filters of {w[0].shape[-1]}")
+    if cols is not None:
+        if gspc_rows8_pitch(cols) != K:
+            raise GspcError(-5, f"rows of {cols} values have a pitch of {gspc_rows8_pitch(cols)}, these of {K}")
+        K = cols
     qa, sa = _rows8(a, M, K, "a")
     qw, sw = _rows8(w, N, K, "w")
     if out is None:

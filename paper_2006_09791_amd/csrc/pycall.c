@@ -283,18 +283,19 @@ static PyObject *norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n)
                                (int)dy.last, groups, act, dx.ptr, dy.last, dgamma, dbeta, ws.ptr, bytes_of(&ws)));
 }
 
-/* matmul((q, scale), (q, scale), bias, out [..., N]) */
+/* matmul((q, scale), (q, scale), bias, out [..., N], cols = None: all of the pitch) */
 static PyObject *matmul(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
     tensor_t x, w, out;
     void *sa, *sw, *bias;
-    if (n != 4 || !g_calls.matmul || !PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 2 || !PyTuple_CheckExact(a[1]) ||
+    int cols = 0;
+    if (n < 4 || n > 5 || (n == 5 && a[4] != Py_None && (!small(a[4], &cols) || cols <= 0)) || !g_calls.matmul || !PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 2 || !PyTuple_CheckExact(a[1]) ||
         PyTuple_GET_SIZE(a[1]) != 2 || !tensor(PyTuple_GET_ITEM(a[0], 0), &x) || !tensor(PyTuple_GET_ITEM(a[1], 0), &w) || x.type != 2 ||
-        w.type != 2 || x.dims != 2 || w.dims != 2 || x.last != w.last || x.last % 16 || !fits(x.last) || !fits(w.first) ||
+        w.type != 2 || x.dims != 2 || w.dims != 2 || x.last != w.last || x.last % 16 || !fits(x.last) || (cols && (cols + (int64_t)15) / 16 * 16 != x.last) || !fits(w.first) ||
         !vector(PyTuple_GET_ITEM(a[0], 1), 0, x.first, 0, &sa) || !vector(PyTuple_GET_ITEM(a[1], 1), 0, w.first, 0, &sw) ||
         !vector(a[2], 0, w.first, 1, &bias) || !tensor(a[3], &out) || out.type == 2 || out.last != w.first || out.count != x.first * w.first)
         GENERAL;
-    CALL(g_calls.matmul(x.ptr, sa, w.ptr, sw, bias, x.first, (int)w.first, (int)x.last, out.ptr, out.type, w.first));
+    CALL(g_calls.matmul(x.ptr, sa, w.ptr, sw, bias, x.first, (int)w.first, cols ? cols : (int)x.last, out.ptr, out.type, w.first));
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}

@@ -88,3 +88,17 @@ def test_parameter_gradients_of_many_images(gpu, N, P, C):
     shift = float((st[..., 0] * st[..., 1]).abs().max())
     off = (torch.stack((dgamma, dbeta)) - sums).abs() / (256 * 2.0 ** -24 * (1 + shift) * sizes)
     assert bool((off <= 1).all()), off.max()
+
+
+@pytest.mark.parametrize("M,N", [(1, 20), (40, 40)])
+@pytest.mark.parametrize("given", [False, True])
+def test_longest_rows_through_the_binding(gpu, M, N, given):
+    torch, b = gpu
+    K = 133144
+    a, w = b.gspc_quantize_rows(torch.ones(M, K, device="cuda")), b.gspc_quantize_rows(-torch.ones(N, K, device="cuda"))
+    a[1].fill_(1.0)
+    w[1].fill_(1.0)
+    out = b.gspc_matmul_i8(a, w, out=torch.empty(M, N, device="cuda") if given else None, dtype=b.GSPC_F32, cols=K)
+    assert bool((out == float(torch.tensor(-127.0 * 127 * K))).all())
+    with pytest.raises(b.GspcError, match="133144"):
+        b.gspc_matmul_i8(a, w, dtype=b.GSPC_F32)
