@@ -336,17 +336,21 @@ template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t
         *name = n;
         hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), 0, s, p);
     };
-    // The largest tile that still gives most compute units one (M x N x K, us; both sides):
-    //   256 x 256 from 160 tiles on: 12544 x 1024 x 512 has 196, 15.0 against 17.1 in tiles of 128; 2048 x 4096 x 2048 has 128, 27.8
-    //   against 22.4;
-    //   128 x 128 from 256 tiles on: 2048 x 4096 x 2048 has 512, 22.4 against 29 in 64 x 128; 512 x 4096 x 4096 has 128, 18.3 against 15.8;
+    // The largest tile that is more than half full and still gives most compute units one (M x K x N, us; both sides):
+    //   256 x 256 from 160 tiles on: 12544 x 512 x 1024 has 196, 15.0 against 17.1 in tiles of 128; 2048 x 2048 x 4096 has 128, 27.8
+    //   against 22.4.  Not for 128 tokens or filters and fewer: 128 x 4096 x 50257, 44.4 against 34.0 in tiles of 128 (129 tokens 43.7
+    //   against 53); 50000 x 512 x 128, 12.3 against 7.9 (129 filters 13.4 against 14.7);
+    //   128 x 128 from 256 tiles on: 2048 x 2048 x 4096 has 512, 22.4 against 29 in 64 x 128; 512 x 4096 x 4096 has 128, 18.3 against 15.8.
+    //   Not for 64 tokens and fewer: 64 x 4096 x 32768, 25.3 against 22.1 in 64 x 128 (96 tokens 25.8 against 24.2, 128 x 4096 x 50257 34.0
+    //   against 44);
     //   64 x 128 where 32 x 32 without staging would be more than one block for each compute unit: 512 x 4096 x 4096, 15.8 against
     //   59; 200 x 1024 x 1024 (224 blocks without staging), 5.9 against 4.4.
-    //   or where its steps are few: 133 x 3608 x 195, 3.7 without staging, 4.4 in 64 x 128.
-    // Up to 16 tokens: 1 x 4096 x 4096, 5.1 in blocks of 16 channels, 7.2 in blocks of 32 x 32.
-    if (tiles(256, 256) >= 160) run(product8_tile_kernel<T, 2, 4, 4, 2, 2>, 256, 256, 512, "product8_tile<256,256>");
-    else if (tiles(128, 128) >= 256) run(product8_tile_kernel<T, 2, 2, 2, 2, 2>, 128, 128, 256, "product8_tile<128,128>");
-    else if (in.M <= 16) run(product8_small_kernel<T, 1, 1, 8, 4>, 16, 16, 512, "product8_small<1,1>");
+    //   or where its steps are few: 133 x 195 x 3608, 3.7 without staging, 4.4 in 64 x 128.
+    // Up to 16 tokens: 1 x 4096 x 4096, 5.1 in blocks of 16 channels, 7.2 in blocks of 32 x 32; unless tiles of 64 x 128 give every compute
+    // unit one: 16 x 4096 x 32768, 30.9 against 21.0 (1 token 24.8 against 20.4; 1 x 4096 x 16384 has 128 tiles, 13.8 against 12.9).
+    if (in.M > 128 && in.N > 128 && tiles(256, 256) >= 160) run(product8_tile_kernel<T, 2, 4, 4, 2, 2>, 256, 256, 512, "product8_tile<256,256>");
+    else if (in.M > 64 && tiles(128, 128) >= 256) run(product8_tile_kernel<T, 2, 2, 2, 2, 2>, 128, 128, 256, "product8_tile<128,128>");
+    else if (in.M <= 16 && tiles(64, 128) < 256) run(product8_small_kernel<T, 1, 1, 8, 4>, 16, 16, 512, "product8_small<1,1>");
     else if (tiles(32, 32) <= 256 || tiles(32, 32) * ((p.pitch + 63) / 64) <= 2560) run(product8_small_kernel<T, 2, 2, 8, 2>, 32, 32, 512, "product8_small<2,2>");
     else run(product8_tile_kernel<T, 2, 2, 1, 2, 3>, 64, 128, 256, "product8_tile<64,128>");
     return hipGetLastError();

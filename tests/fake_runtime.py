@@ -52,7 +52,7 @@ launches, decode = [], {}
 def take_down(name, blocks, threads, args):
     short = re.match(r"_ZN4gspc(\d+)(\w+)", name.decode())
     short = short[2][:int(short[1])]
-    values = [bytes((ctypes.c_char * size).from_address(args[i])).hex() for i, size in decode.get(short, [])]
+    values = [(name if i < 0 else bytes((ctypes.c_char * size).from_address(args[i]))).hex() for i, size in decode.get(short, [])]
     launches.append([short, blocks, threads, values])
 kind = ctypes.CFUNCTYPE(None, ctypes.c_char_p, ctypes.c_uint, ctypes.c_uint, ctypes.POINTER(ctypes.c_void_p))
 keep = kind(take_down)
@@ -80,7 +80,7 @@ def build(folder):
 
 def launches(runtime, calls, decode):
     """[(result, [(kernel, blocks, threads of a block, arguments)])] for calls [(entry point, arguments)]: of each kernel those arguments
-    that `decode` names as (number, bytes), raw."""
+    that `decode` names as (number, bytes), raw; number -1 is the kernel's whole name."""
     lib = b.load()
     work = [(name, [t._type_ for t in getattr(lib, name).argtypes], getattr(lib, name).restype._type_, args) for name, args in calls]
     r = subprocess.run([sys.executable, "-c", CHILD, runtime, b.LIB_PATH], input=json.dumps({"calls": work, "decode": decode}), capture_output=True,

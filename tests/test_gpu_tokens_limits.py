@@ -102,3 +102,17 @@ def test_longest_rows_through_the_binding(gpu, M, N, given):
     assert bool((out == float(torch.tensor(-127.0 * 127 * K))).all())
     with pytest.raises(b.GspcError, match="133144"):
         b.gspc_matmul_i8(a, w, dtype=b.GSPC_F32)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 50257, 272), (16, 41000, 128), (1, 128256, 80), (40, 33000, 272), (100, 50257, 144), (50000, 10, 80), (50000, 100, 272)])
+def test_products_long_in_one_direction(gpu, M, N, K):
+    """Few tokens and many filters, or the reverse: the integer sums, exact in fp32 (127 * 127 * 272 < 2^24)."""
+    torch, b = gpu
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    q = lambda rows: torch.randint(-127, 128, (rows, K), dtype=torch.int8, device="cuda", generator=g)  # noqa: E731
+    a, w = (q(M), torch.ones(M, device="cuda")), (q(N), torch.ones(N, device="cuda"))
+    out = torch.full((M + 2, N + 5), 7.0, device="cuda")
+    b.gspc_matmul_i8(a, w, out=out[1:-1, 2:-3])
+    want = a[0].float() @ w[0].float().t().contiguous()         # (sums of whole numbers below 2^24: exact in any order)
+    assert torch.equal(out[1:-1, 2:-3], want), b.gspc_last_kernel()
+    assert bool((out[0] == 7).all() and (out[-1] == 7).all() and (out[:, :2] == 7).all() and (out[:, -3:] == 7).all())

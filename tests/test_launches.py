@@ -1,5 +1,6 @@
 """How the channels-last operators are cut into launches: no launch has 2^32 threads or more, which the HIP runtime refuses, and the
 launches of a call together reach every image once."""
+import re
 import struct
 
 import pytest
@@ -131,3 +132,25 @@ def test_gradients_of_many_parameters_without_tokens(runtime):
     (rc, found), = fake_runtime.launches(runtime, [("gspc_group_norm_backward", [None, 1, 1 << 30, None, 1, 1 << 30, None, None, None, None,
                                                                                  0, 3, 1 << 30, 1, 2, None, 1 << 30, DG, DB, None, 0])], NORM)
     assert rc == 0 and len(found) == 1 and found[0][1] * found[0][2] < 1 << 32
+
+
+PRODUCT = {k: [(-1, 0), (0, 88)] for k in ("product8_small_kernel", "product8_tile_kernel")}
+
+
+def product_tile(raw):
+    """(tokens, filters) of a block, from the kernel's name."""
+    n = [int(v) for v in re.findall(r"Li(\d+)E", raw.decode())]
+    return (32 * n[0] * n[2], 32 * n[1] * n[3]) if b"tile_kernel" in raw else (16 * n[1], 16 * n[0])
+
+
+@pytest.mark.parametrize("M,N", [(1, 50257), (16, 128256), (17, 50257), (64, 33000), (64, 1 << 20), (65, 33000), (100, 50257), (128, 128256), (50000, 1),
+                                 (50000, 10), (200000, 64), (50000, 100), (1 << 20, 128), (129, 50257), (50000, 129), (8192, 8192), (12544, 1024)])
+@pytest.mark.parametrize("K", [128, 4096])
+def test_large_tiles_are_at_least_half_full(runtime, M, N, K):
+    """A tile of 128 tokens and more, or of 256 filters, is taken where the product fills more than half of it."""
+    (rc, found), = fake_runtime.launches(runtime, [("gspc_matmul_i8", [X, SV, Y, YS, None, M, N, K, DX, 1, N])], PRODUCT)
+    assert rc == 0
+    for _, _, _, (name, _) in found:
+        tokens, filters = product_tile(name)
+        assert tokens < 128 or 2 * M > tokens, (tokens, filters)
+        assert filters < 256 or 2 * N > filters, (tokens, filters)
