@@ -325,16 +325,21 @@ __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------------
 template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t s, const char **name) {
-    ProductArgs p{in.a, in.w, in.a_scale, in.w_scale, in.bias, in.out, in.M, in.ldo, in.N, rows8_pitch(in.K), 0, 0, in.M * in.N * sizeof(T) >= kPastCaches};
-    const auto tiles = [&](int bm, int bn) {
-        p.mtiles = (unsigned)((in.M + bm - 1) / bm);
-        p.ntiles = (in.N + bn - 1) / bn;
-        return (unsigned long long)p.mtiles * p.ntiles;
-    };
-    const auto run = [&](auto kern, int bm, int bn, int threads, const char *n) {
-        const unsigned blocks = (unsigned)tiles(bm, bn);
-        *name = n;
-        hipLaunchKernelGGL(kern, dim3(blocks), dim3(threads), 0, s, p);
+    const unsigned pitch = rows8_pitch(in.K);
+    const auto count = [](size_t all, unsigned of) { return (unsigned)((all - 1) / of + 1); };
+    const auto tiles = [&](int bm, int bn) { return (unsigned long long)count(in.M, bm) * count(in.N, bn); };
+    const auto run = [&](auto kern, unsigned bm, unsigned bn, unsigned threads, const char *name_of) {
+        *name = name_of;
+        const unsigned most = most_blocks(threads), nt = count(in.N, bn) < most ? count(in.N, bn) : most;
+        const size_t m_step = (size_t)(most / nt) * bm, n_step = (size_t)nt * bn;       // of one launch at most
+        for (size_t m = 0; m < in.M; m += m_step)
+            for (size_t n = 0; n < (size_t)in.N; n += n_step) {
+                const size_t rows = in.M - m < m_step ? in.M - m : m_step, cols = in.N - n < n_step ? in.N - n : n_step;
+                const ProductArgs p{in.a + m * pitch, in.w + n * pitch, in.a_scale + m, in.w_scale + n, in.bias ? in.bias + n : nullptr,
+                                    static_cast<T *>(in.out) + m * in.ldo + n, rows, in.ldo, (int)cols, (int)pitch, count(rows, bm), count(cols, bn),
+                                    in.M * in.N * sizeof(T) >= kPastCaches};
+                hipLaunchKernelGGL(kern, dim3(p.mtiles * p.ntiles), dim3(threads), 0, s, p);
+            }
     };
     // The largest tile that is more than half full and still gives most compute units one (M x K x N, us; both sides):
     //   256 x 256 from 160 tiles on: 12544 x 512 x 1024 has 196, 15.0 against 17.1 in tiles of 128; 2048 x 2048 x 4096 has 128, 27.8
@@ -351,7 +356,7 @@ template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t
     if (in.M > 128 && in.N > 128 && tiles(256, 256) >= 160) run(product8_tile_kernel<T, 2, 4, 4, 2, 2>, 256, 256, 512, "product8_tile<256,256>");
     else if (in.M > 64 && tiles(128, 128) >= 256) run(product8_tile_kernel<T, 2, 2, 2, 2, 2>, 128, 128, 256, "product8_tile<128,128>");
     else if (in.M <= 16 && tiles(64, 128) < 256) run(product8_small_kernel<T, 1, 1, 8, 4>, 16, 16, 512, "product8_small<1,1>");
-    else if (tiles(32, 32) <= 256 || tiles(32, 32) * ((p.pitch + 63) / 64) <= 2560) run(product8_small_kernel<T, 2, 2, 8, 2>, 32, 32, 512, "product8_small<2,2>");
+    else if (tiles(32, 32) <= 256 || tiles(32, 32) * ((pitch + 63) / 64) <= 2560) run(product8_small_kernel<T, 2, 2, 8, 2>, 32, 32, 512, "product8_small<2,2>");
     else run(product8_tile_kernel<T, 2, 2, 1, 2, 3>, 64, 128, 256, "product8_tile<64,128>");
     return hipGetLastError();
 }

@@ -116,3 +116,14 @@ def test_products_long_in_one_direction(gpu, M, N, K):
     want = a[0].float() @ w[0].float().t().contiguous()         # (sums of whole numbers below 2^24: exact in any order)
     assert torch.equal(out[1:-1, 2:-3], want), b.gspc_last_kernel()
     assert bool((out[0] == 7).all() and (out[-1] == 7).all() and (out[:, :2] == 7).all() and (out[:, -3:] == 7).all())
+
+
+def test_product_of_as_many_tokens_as_there_are(gpu):
+    """2^31 - 1 tokens: more blocks than one launch may have.  Whole numbers, exact."""
+    torch, b = gpu
+    M, N, K, step = 0x7fffffff, 2, 16, 1 << 26
+    a = (torch.randint(-127, 128, (M, K), dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda"))
+    w = (torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda"), torch.ones(N, device="cuda"))
+    out = b.gspc_matmul_i8(a, w, dtype=b.GSPC_F32)
+    for at in range(0, M, step):
+        assert torch.equal(out[at:at + step], a[0][at:at + step].float() @ w[0].float().t().contiguous()), at

@@ -154,3 +154,24 @@ def test_large_tiles_are_at_least_half_full(runtime, M, N, K):
         tokens, filters = product_tile(name)
         assert tokens < 128 or 2 * M > tokens, (tokens, filters)
         assert filters < 256 or 2 * N > filters, (tokens, filters)
+
+
+@pytest.mark.parametrize("M,N", [(0x7fffffff, 100), (0x7fffffff, 130), (0x7fffffff, 200), (1 << 30, 1), (1, 0x7ffffff0), (16, 140_000_000), (64, 0x7ffffff0),
+                                 (100, 0x7ffffff0), (3, 5), (8192, 8192)])
+@pytest.mark.parametrize("bias", [None, SS])
+def test_product_launches_cover_the_output(runtime, M, N, bias):
+    K, ld = 16, N + 3
+    (rc, found), = fake_runtime.launches(runtime, [("gspc_matmul_i8", [X, SV, Y, YS, bias, M, N, K, DX, 1, ld])], PRODUCT)
+    assert rc == 0
+    seen = set()
+    for _, blocks, threads, (name, raw) in found:
+        assert blocks * threads < 1 << 32
+        a, w, sa, sw, sb, out, m, ldo, n, pitch, mtiles, ntiles, _ = struct.unpack("<8Q2i2Ii", raw[:84])
+        m0, n0 = (a - X) // pitch, (w - Y) // pitch
+        assert (a, w, sa, sw, out) == (X + m0 * pitch, Y + n0 * pitch, SV + 4 * m0, YS + 4 * n0, DX + 2 * (m0 * ld + n0))
+        assert sb == (bias + 4 * n0 if bias else 0) and ldo == ld and pitch == K
+        tokens, filters = product_tile(name)
+        assert (mtiles, ntiles) == (-(-m // tokens), -(-n // filters)) and blocks == mtiles * ntiles
+        assert m0 + m <= M and n0 + n <= N and m0 % tokens == 0 and n0 % filters == 0
+        seen.add((m0, n0, m * n))
+    assert len(seen) == len(found) and sum(s for *_, s in seen) == M * N
