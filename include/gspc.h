@@ -271,7 +271,8 @@ size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int x_dt
 size_t gspc_group_norm_backward_workspace_bytes(int N, int P, int C, int groups, int dy_dtype, int x_dtype);
 
 /* y = act(gamma * (x - mean) / sqrt(var + eps) + beta) over N images of P tokens of C channels; mean and (biased) variance
- * are those of the P * C / groups values of a group of one image.  N * groups is at most 2^25.
+ * are those of the P * C / groups values of a group of one image.  N * groups is at most 2^25,
+ * C below 2^31 - 4096.
  *   gamma, beta : dev fp32 [C], or NULL for 1 and 0
  *   y           : dense rows, fp32 or bf16 (y_dtype, ldy), or 8-bit rows (GSPC_I8; ldy ignored) with y_scale
  *   stats       : dev fp32 [N][groups][2], receives mean and 1 / sqrt(var + eps) for the gradient, or NULL

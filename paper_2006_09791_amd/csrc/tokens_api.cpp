@@ -10,6 +10,7 @@ using gspc::fail;
 
 constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int kMaxCols = 0x7ffffff0;        // whose pitch is an int
+constexpr int kMaxNormCols = 0x7fffffff - 4096;     // whose slabs of channels end within an int
 constexpr int kMaxK = 133144;               // 2^31 / 127^2: sums of products fit 32 bits
 
 int done(hipError_t e, const char *what) {
@@ -41,7 +42,7 @@ int check_count(int64_t rows, int cols) {
 }
 
 int check_norm(int N, int P, int C, int groups, int act, gspc::NormShape *h) {
-    if (N < 0 || P < 0 || C <= 0 || C > kMaxCols) return fail(GSPC_ERR_DIM, "invalid dimension (N=%d P=%d C=%d)", N, P, C);
+    if (N < 0 || P < 0 || C <= 0 || C > kMaxNormCols) return fail(GSPC_ERR_DIM, "invalid dimension (N=%d P=%d C=%d)", N, P, C);
     if ((int64_t)N * P > kMaxRows) return fail(GSPC_ERR_DIM, "%lld tokens", (long long)N * P);
     if (groups <= 0 || C % groups) return fail(GSPC_ERR_GROUPS, "C=%d must be divisible by groups=%d", C, groups);
     if (act != GSPC_ACT_NONE && act != GSPC_ACT_RELU && act != GSPC_ACT_SILU) return fail(GSPC_ERR_ARG, "unknown activation %d", act);
