@@ -441,21 +441,23 @@ def _change_layout(call, x, out, dtype, pack):
     shape = (N, P, C) if pack else (N, C, P)
     if out is None:
         out = _empty(shape, _torch_dtype(dtype), x.device)
-    elif out.numel() != x.numel() or not _on_gpu(out, "out").is_contiguous():
-        raise GspcError(-8, f"out: a contiguous tensor of {x.numel()} elements is needed")
+    elif out.dim() < 3 or out.shape[0] != N or out.shape[-1 if pack else 1] != C or out.numel() != x.numel():
+        raise GspcError(-2, f"out has shape {tuple(out.shape)}, expected {shape}, with its pixels in one dimension or more")
+    elif not _on_gpu(out, "out").is_contiguous():
+        raise GspcError(-8, "out must be contiguous")
     _check(call(x.data_ptr(), _dtype(x, "x"), N, C, P, out.data_ptr(), _dtype(out, "out")))
     return out
 
 
 def gspc_pack_channels_last(x, out=None, dtype=GSPC_BF16):
-    """x [N, C, ...] (planes) -> [N, P, C] (tokens), P the pixels of a plane."""
+    """x [N, C, ...] (planes) -> [N, P, C] (tokens), P the pixels of a plane; `out`: a tensor [N, ..., C] to write into."""
     if out is not None and _fast is not None and _done(_fast.pack(x, out)):
         return out
     return _change_layout(load().gspc_pack_channels_last, x, out, dtype, True)
 
 
 def gspc_unpack_channels_last(x, out=None, dtype=GSPC_F32):
-    """x [N, ..., C] (tokens) -> [N, C, P] (planes)."""
+    """x [N, ..., C] (tokens) -> [N, C, P] (planes); `out`: a tensor [N, C, ...] to write into."""
     if out is not None and _fast is not None and _done(_fast.unpack(x, out)):
         return out
     return _change_layout(load().gspc_unpack_channels_last, x, out, dtype, False)

@@ -121,7 +121,7 @@ static PyObject *bind_tokens(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 typedef struct {
     void *ptr;
     int type, dims;
-    int64_t first, last, count;            /* first and last dimension, elements */
+    int64_t first, second, last, count;    /* first, second and last dimension, elements */
 } tensor_t;
 
 static int is_true(PyObject *v) {
@@ -145,10 +145,11 @@ static int tensor(PyObject *t, tensor_t *o) {
     }
     o->dims = (int)PyTuple_GET_SIZE(v);
     o->count = 1;
-    o->first = o->last = 1;
+    o->first = o->second = o->last = 1;
     for (int i = 0; i < o->dims; ++i) {
         o->last = PyLong_AsLongLong(PyTuple_GET_ITEM(v, i));
         if (i == 0) o->first = o->last;
+        if (i == 1) o->second = o->last;
         o->count *= o->last;
     }
     Py_DECREF(v);
@@ -192,13 +193,13 @@ static int fits(int64_t v) { return v > 0 && v < 0x7ffffff0; }
     Py_END_ALLOW_THREADS             \
     return PyLong_FromLong(rc)
 
-/* pack(x [N, C, ...], out), unpack(x [N, ..., C], out) */
+/* pack(x [N, C, P], out [N, ..., C]), unpack(x [N, P, C], out [N, C, ...]) */
 static PyObject *layout(PyObject *const *a, Py_ssize_t n, int pack) {
     tensor_t x, out;
     if (n != 2 || !g_calls.pack || !tensor(a[0], &x) || x.dims != 3 || !fits(x.count) || x.type == 2 || !tensor(a[1], &out) || out.type == 2 ||
-        out.count != x.count)
+        out.count != x.count || out.dims < 3 || out.first != x.first || (pack ? out.last != x.second : out.second != x.last))
         GENERAL;
-    const int N = (int)x.first, middle = (int)(x.count / x.first / x.last), C = pack ? middle : (int)x.last;
+    const int N = (int)x.first, C = (int)(pack ? x.second : x.last);
     CALL((pack ? g_calls.pack : g_calls.unpack)(x.ptr, x.type, N, C, (int)(x.count / N / C), out.ptr, out.type));
 }
 static PyObject *pack(PyObject *self, PyObject *const *a, Py_ssize_t n) {

@@ -1,0 +1,31 @@
+"""Outputs of the channels-last operators have the shape of what is written into them, by either route of a call."""
+import pytest
+
+from paper_2006_09791_amd import binding as b
+from test_tokens_call import call, fake  # noqa: F401  (fixture)
+
+torch = pytest.importorskip("torch")
+
+
+class Fake(torch.Tensor):
+    """A host tensor that says it is on the GPU: what is refused for its shape never gets to be read."""
+    is_cuda = True
+
+
+def test_layout_outputs(call):  # noqa: F811
+    c, seen = call
+    for out in ((2, 5, 3), (2, 1, 5, 3), (2, 5, 1, 3)):
+        assert c.pack(fake(16, (2, 3, 5)), fake(32, out)) == -100
+    for out in ((2, 3, 5), (2, 3, 5, 1), (2, 3, 1, 5)):
+        assert c.unpack(fake(16, (2, 5, 3)), fake(32, out)) == -101
+    assert [a[2:5] for _, a in seen] == [(2, 3, 5)] * 6
+    del seen[:]
+    for out in ((2, 3, 5), (5, 2, 3), (3, 10), (30,), (10, 3), (1, 10, 3)):
+        assert c.pack(fake(16, (2, 3, 5)), fake(32, out)) is NotImplemented
+        with pytest.raises(b.GspcError, match="out has shape"):
+            b.gspc_pack_channels_last(torch.zeros(2, 3, 5).as_subclass(Fake), out=torch.zeros(out).as_subclass(Fake))
+    for out in ((2, 5, 3), (5, 3, 2), (2, 15), (30,), (1, 3, 10)):
+        assert c.unpack(fake(16, (2, 5, 3)), fake(32, out)) is NotImplemented
+        with pytest.raises(b.GspcError, match="out has shape"):
+            b.gspc_unpack_channels_last(torch.zeros(2, 5, 3).as_subclass(Fake), out=torch.zeros(out).as_subclass(Fake))
+    assert not seen
