@@ -234,6 +234,11 @@ static PyObject *dequantize(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 
 static size_t bytes_of(const tensor_t *t) { return t->ptr ? (size_t)t->count * (t->type == 0 ? 4 : t->type == 1 ? 2 : 1) : 0; }
 
+/* Whether two tensors of up to four dimensions (more: no) have the same shape. */
+static int same_shape(const tensor_t *a, const tensor_t *b) {
+    return a->dims == b->dims && a->dims <= 4 && a->first == b->first && a->second == b->second && a->last == b->last && a->count == b->count;
+}
+
 /* norm(x [N, ..., C], gamma, beta, groups, eps, act, out, stats, saved, workspace) */
 static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
@@ -249,7 +254,7 @@ static PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
         if (!rows8(a[6], rows, x.last, &out, &scale)) GENERAL;
         kind = 2;
     } else {
-        if (!tensor(a[6], &y) || y.type == 2 || y.dims != x.dims || y.first != x.first || y.last != x.last || y.count != x.count) GENERAL;
+        if (!tensor(a[6], &y) || y.type == 2 || !same_shape(&y, &x)) GENERAL;
         out = y.ptr;
         kind = y.type;
     }
@@ -268,15 +273,15 @@ static PyObject *norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n)
     if (n != 11 || !g_calls.norm_backward || !tensor(a[0], &dy) || dy.type == 2 || dy.dims < 3 || !fits(dy.first) || !fits(dy.last) ||
         !fits(dy.count / dy.first / dy.last) || !small(a[5], &groups) || !small(a[6], &act) || !vector(a[2], 0, dy.first * groups * 2, 0, &stats) ||
         !vector(a[3], 0, dy.last, 1, &gamma) || !vector(a[4], 0, dy.last, 1, &beta) || !vector(a[8], 0, dy.last, 0, &dgamma) ||
-        !vector(a[9], 0, dy.last, 0, &dbeta) || !tensor(a[7], &dx) || dx.type != dy.type || dx.dims != dy.dims || dx.first != dy.first ||
-        dx.last != dy.last || dx.count != dy.count || (a[10] != Py_None && !tensor(a[10], &ws)))
+        !vector(a[9], 0, dy.last, 0, &dbeta) || !tensor(a[7], &dx) || dx.type != dy.type || !same_shape(&dx, &dy) ||
+        (a[10] != Py_None && !tensor(a[10], &ws)))
         GENERAL;
     const int64_t rows = dy.count / dy.last;
     if (PyTuple_CheckExact(a[1])) {
         if (!rows8(a[1], rows, dy.last, &px, &scale)) GENERAL;
         kind = 2;
     } else {
-        if (!tensor(a[1], &x) || x.type == 2 || x.dims != dy.dims || x.first != dy.first || x.last != dy.last || x.count != dy.count) GENERAL;
+        if (!tensor(a[1], &x) || x.type == 2 || !same_shape(&x, &dy)) GENERAL;
         px = x.ptr;
         kind = x.type;
     }

@@ -29,3 +29,16 @@ def test_layout_outputs(call):  # noqa: F811
         with pytest.raises(b.GspcError, match="out has shape"):
             b.gspc_unpack_channels_last(torch.zeros(2, 5, 3).as_subclass(Fake), out=torch.zeros(out).as_subclass(Fake))
     assert not seen
+
+
+def test_norm_tensors_of_another_shape_are_left_to_the_general_route(call):  # noqa: F811
+    """Which refuses them: pixels in another order are another image."""
+    c, seen = call
+    x, stats, v = fake(16, (2, 3, 4, 24)), fake(80, (2, 3, 2)), fake(48, (24,))
+    same, turned, flat = fake(96, (2, 3, 4, 24)), fake(96, (2, 4, 3, 24)), fake(96, (2, 12, 24))
+    norm = lambda x, y: c.norm(x, v, v, 3, 1e-5, 0, y, None, None, None)  # noqa: E731
+    back = lambda dy, x, dx: c.norm_backward(dy, x, stats, v, v, 3, 0, dx, v, v, None)  # noqa: E731
+    assert norm(x, same) == -104 and back(x, same, same) == -105 and len(seen) == 2
+    for other in (turned, flat, fake(96, (2, 3, 2, 2, 24))):
+        assert norm(x, other) is back(x, other, same) is back(x, same, other) is NotImplemented
+    assert len(seen) == 2
