@@ -226,7 +226,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                                                         const TX *__restrict__ x, size_t ldx, const float2 *__restrict__ stats,
                                                         const float *__restrict__ gamma, const float *__restrict__ beta,
                                                         TY *__restrict__ y, size_t ldy, float *__restrict__ y_scale,
-                                                        int8_t *__restrict__ saved, float *__restrict__ saved_scale, int past, int past_saved) {
+                                                        int8_t *__restrict__ saved, float *__restrict__ saved_scale, int past) {
     constexpr bool CODES = sizeof(TY) == 1;
     constexpr int H = HELD ? HELD : 1, DEEP = HELD == 1 ? 2 : 1;
     const int n = fast_div_any(blockIdx.x, blocks, m_blocks), width = 1 << log_width, lane = threadIdx.x & (width - 1);
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                     for (int e = 0; e < V; ++e) top = max(top, magnitude(t[e]));
                 });
                 const RowCode c = row_code(lanes_umax(top, width));
-                each([&](int at, float (&t)[V], Affine<V> &) { store_codes(saved + row * pitch + at, t, c, past_saved); });
+                each([&](int at, float (&t)[V], Affine<V> &) { store_codes(saved + row * pitch + at, t, c); });
                 for (int i = h.C + lane; i < pitch; i += width) saved[row * pitch + i] = 0;
                 if (lane == 0) saved_scale[row] = c.scale;
             }
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
                 const RowCode c = row_code(lanes_umax(top, width));
                 each([&](int at, float (&t)[V], Affine<V> &fk) {
                     if constexpr (HELD == 0) apply_affine<V>(fk, h.act, t);
-                    store_codes(reinterpret_cast<int8_t *>(y) + row * pitch + at, t, c, false);
+                    store_codes(reinterpret_cast<int8_t *>(y) + row * pitch + at, t, c);
                 });
                 for (int i = h.C + lane; i < pitch; i += width) reinterpret_cast<int8_t *>(y)[row * pitch + i] = 0;
                 if (lane == 0) y_scale[row] = c.scale;
@@ -437,7 +437,7 @@ static void launch_rows(const NormShape &h, const NormForward &f, const float2 *
     blocks = (h.P + rows - 1) / rows;
     hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * h.N)), dim3(256), 0, s, h, log_width, (int)blocks, rows, div_magic((unsigned)blocks),
                        static_cast<const TX *>(f.x), f.ldx, stats, f.gamma, f.beta, static_cast<TY *>(f.y), f.ldy, f.y_scale, f.saved,
-                       f.saved_scale, f.past, h.C >= 64 && (size_t)h.N * h.P * h.C >= kPastCaches);
+                       f.saved_scale, f.past);
 }
 
 // Vectors that a thread of norm_held_kernel holds at most: 64 registers of raw values.
@@ -504,7 +504,8 @@ static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream
     const NormGrid g = norm_grid(h, kForwardBlocks, kForwardChunks);
     float2 *stats = f.stats ? reinterpret_cast<float2 *>(f.stats) : static_cast<float2 *>(ws);
     float2 *parts = static_cast<float2 *>(ws) + (size_t)h.N * h.groups;
-    f.past = (size_t)h.N * h.P * h.C * (f.y_dtype == GSPC_F32 ? 4 : 2) >= kPastCaches;
+    f.past = f.y_dtype == GSPC_BF16 && (size_t)h.N * h.P * h.C * 2 >= kPastCaches &&
+             (f.ldy == (size_t)h.C || whole_pieces(f.y, (size_t)h.C * 2, f.ldy * 2));
     HeldGrid held;
     const bool hold = plan_held(h, sizeof(TX), held_most<TX>(), 512, &held);
     if (f.y_dtype != GSPC_I8 && !f.saved && hold) {

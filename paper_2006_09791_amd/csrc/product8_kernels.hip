@@ -328,6 +328,11 @@ template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t
     const unsigned pitch = rows8_pitch(in.K);
     const auto count = [](size_t all, unsigned of) { return (unsigned)((all - 1) / of + 1); };
     const auto tiles = [&](int bm, int bn) { return (unsigned long long)count(in.M, bm) * count(in.N, bn); };
+    // Past the caches (M x K x N, us through them and past): 8192 x 4096 x 8192, 255 and 240; 16384 x 256 x 1024, 12.1 and 10.2.  From 16 MB on only
+    // rows of whole pieces: 16384 x 256 x 1001, 13.6 and 17.3, 100000 x 64 x 1001 55.8 and 109 (below, 8582 x 64 x 501 7.1 and 7.8, 11976 x 1024 x
+    // 501 14.4 and 13.5).
+    const size_t bytes = in.M * in.N * sizeof(T);
+    const int past = bytes >= kPastCaches && (bytes < 2 * kPastCaches || whole_pieces(in.out, in.N * sizeof(T), in.ldo * sizeof(T)));
     const auto run = [&](auto kern, unsigned bm, unsigned bn, unsigned threads, const char *name_of) {
         *name = name_of;
         const unsigned most = most_blocks(threads), nt = count(in.N, bn) < most ? count(in.N, bn) : most;
@@ -337,7 +342,7 @@ template <typename T> static hipError_t product(const ProductI8 &in, hipStream_t
                 const size_t rows = in.M - m < m_step ? in.M - m : m_step, cols = in.N - n < n_step ? in.N - n : n_step;
                 const ProductArgs p{in.a + m * pitch, in.w + n * pitch, in.a_scale + m, in.w_scale + n, in.bias ? in.bias + n : nullptr,
                                     static_cast<T *>(in.out) + m * in.ldo + n, rows, in.ldo, (int)cols, (int)pitch, count(rows, bm), count(cols, bn),
-                                    in.M * in.N * sizeof(T) >= kPastCaches};
+                                    past};
                 hipLaunchKernelGGL(kern, dim3(p.mtiles * p.ntiles), dim3(threads), 0, s, p);
             }
     };

@@ -6,8 +6,8 @@ namespace gspc {
 
 // `width` lanes (a power of two up to a wave) hold one row, lane l the vectors l, l + width, ...  HELD of them per lane stay in
 // registers between the maximum and the rounding; HELD = 0: rows of any length, read a second time.  Bound by memory: 2 or 4
-// bytes of a value in, one out; 50176 rows of 512 in bf16 16.9 us, 4.6 TB/s.  (Through the caches, whatever the size: written past
-// them, these took 5 us longer to write and read back.)
+// bytes of a value in, one out; 50176 rows of 512 in bf16 16.9 us, 4.6 TB/s.  (Written past the caches, these took 5 us longer to write
+// and read back.)
 template <typename T, int V, int HELD>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict__ x, size_t ldx, unsigned rows, int cols, int width,
                                                             int8_t *__restrict__ q, float *__restrict__ scale) {
@@ -45,13 +45,13 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict_
             if (lane + k * width < nv) {
                 float v[V];
                 widen(raw[k], v);
-                store_codes(q + vector_start<V>(lane + k * width, cols), v, c, false);
+                store_codes(q + vector_start<V>(lane + k * width, cols), v, c);
             }
     } else {
         for (int i = lane; i < nv; i += width) {
             float v[V];
             widen(fetch<V>(x + vector_start<V>(i, cols)), v);
-            store_codes(q + vector_start<V>(i, cols), v, c, false);
+            store_codes(q + vector_start<V>(i, cols), v, c);
         }
     }
     for (int i = cols + lane; i < pitch; i += width) q[i] = 0;
@@ -113,7 +113,7 @@ static hipError_t dequantize(const int8_t *q, const float *scale, size_t rows, i
     const size_t pitch = rows8_pitch(cols);
     return in_pieces(rows, width, [&](size_t at, unsigned n, dim3 grid) {
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, q + at * pitch, scale + at, n, cols, width, x + at * ldx, ldx,
-                           cols >= 32 && rows * cols * sizeof(T) >= kPastCaches);
+                           sizeof(T) == 2 && cols >= 32 && rows * cols * 2 >= kPastCaches);
     });
 }
 

@@ -175,3 +175,56 @@ def test_product_launches_cover_the_output(runtime, M, N, bias):
         assert m0 + m <= M and n0 + n <= N and m0 % tokens == 0 and n0 % filters == 0
         seen.add((m0, n0, m * n))
     assert len(seen) == len(found) and sum(s for *_, s in seen) == M * N
+
+
+PAST = {"transpose_kernel": [(8, 4)], "transpose_thin_kernel": [(7, 4)], "norm_apply_kernel": [(11, 4)], "norm_held_kernel": [(10, 4)],
+        "norm_rows_kernel": [(15, 4)], "norm_grad_held_kernel": [(15, 4)], "norm_grad_apply_kernel": [(13, 4)], "dequantize_rows_kernel": [(7, 4)]}
+
+
+def goes_past(runtime, name, args):
+    """Whether the kernel that writes the call's output is told to write past the caches."""
+    (rc, found), = fake_runtime.launches(runtime, [(name, args)], {**PAST, **PRODUCT})
+    assert rc == 0
+    if name == "gspc_matmul_i8":
+        return bool(struct.unpack("<i", found[-1][3][1][80:84])[0])
+    return bool(number([args for k, _, _, args in found if k in PAST][-1][0]))
+
+
+@pytest.mark.parametrize("N,P,C,groups", [(64, 3136, 96, 8), (256, 784, 64, 8), (128, 3136, 24, 4)])
+def test_norms_write_whole_pieces_past_the_caches(runtime, N, P, C, groups):
+    """bf16 side by side, or in rows of whole pieces of 64 bytes; never fp32, whose vectors are two stores with a gap."""
+    def forward(ld, kind=1, saved=None, at=0):
+        need = fake_runtime.b.gspc_group_norm_workspace_bytes(N, P, C, groups, kind, saved is not None)
+        return goes_past(runtime, "gspc_group_norm", [X, kind, C, None, None, N, P, C, groups, 1e-5, 2, Y + at, kind, ld, None, ST, saved, SS, WS, need])
+
+    def backward(ld, kind=1, at=0):
+        need = fake_runtime.b.gspc_group_norm_backward_workspace_bytes(N, P, C, groups, kind, kind)
+        return goes_past(runtime, "gspc_group_norm_backward", [Y, kind, C, X, kind, C, None, ST, None, None, N, P, C, groups, 2, DX + at, ld, DG, DB, WS, need])
+
+    whole = C % 32 == 0
+    for call in (forward, backward, lambda *a, **k: forward(*a, saved=SV, **k)):
+        assert call(C) and call(C, at=2) and call(2 * C) == call(C + 32) == whole
+        assert not (call(C + 2) or call(C + 16) or call(2 * C, at=32) or call(C, kind=0) or call(2 * C, kind=0))
+
+
+def test_gradients_of_wide_rows_go_past_the_caches(runtime):
+    need = fake_runtime.b.gspc_group_norm_backward_workspace_bytes(64, 3136, 256, 32, 1, 1)
+    assert goes_past(runtime, "gspc_group_norm_backward", [Y, 1, 256, X, 1, 256, None, ST, None, None, 64, 3136, 256, 32, 2, DX, 258, DG, DB, WS, need])
+
+
+@pytest.mark.parametrize("M,N,K", [(100000, 128, 64), (16384, 1024, 256), (8192, 8192, 4096), (100000, 256, 64)])
+def test_products_write_whole_pieces_past_the_caches(runtime, M, N, K):
+    call = lambda N, ld, kind, at=0: goes_past(runtime, "gspc_matmul_i8", [X, SV, Y, YS, None, M, N, K, DX + at, kind, ld])  # noqa: E731
+    for kind, line in ((1, 32), (0, 16)):
+        assert call(N, N, kind) and call(N, N + line, kind) and call(N - line, N, kind)
+        assert not (call(N, N + 1, kind) or call(N, N + 8, kind) or call(N - 1, N - 1, kind) or call(N - 4, N, kind) or call(N, N, kind, 16))
+
+
+@pytest.mark.parametrize("name,C,P,past", [("gspc_pack_channels_last", 128, 784, True), ("gspc_pack_channels_last", 100, 1073, False),
+                                           ("gspc_pack_channels_last", 32, 3136, False), ("gspc_unpack_channels_last", 128, 784, False),
+                                           ("gspc_unpack_channels_last", 128, 3136, True), ("gspc_pack_channels_last", 6, 12545, True),
+                                           ("gspc_unpack_channels_last", 6, 12544, True), ("gspc_unpack_channels_last", 6, 12545, False)])
+def test_layout_passes_write_whole_pieces_past_the_caches(runtime, name, C, P, past):
+    assert goes_past(runtime, name, [X, 0, 256, C, P, Y, 1]) == past
+    assert not goes_past(runtime, name, [X, 1, 256, C, P, Y, 0])         # fp32
+    assert not goes_past(runtime, name, [X, 0, 1, C, P, Y, 1])           # small
