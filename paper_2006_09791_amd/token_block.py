@@ -12,7 +12,8 @@ from . import binding as b
 
 
 class TokenBlock:
-    """weight [C, C/groups, 3, 3], gamma and beta [C], pointwise [filters, C]: fp32 tensors on the GPU."""
+    """weight [C, C/groups, 3, 3], gamma and beta [C], pointwise [filters, C]: fp32 tensors on the GPU.  What a pass makes for itself and drops
+    at its end belongs to the library's stream (binding._empty): torch gives it to no other stream's work before that stream is done."""
 
     def __init__(self, weight, gamma, beta, pointwise, conv_groups, norm_groups, eps=1e-5):
         self.C, self.conv_groups, self.norm_groups, self.eps = weight.shape[0], conv_groups, norm_groups, eps
@@ -23,8 +24,10 @@ class TokenBlock:
 
     def tokens(self, x):
         """x [N, C, H, W] fp32 -> what the convolution leaves, as bf16 tokens [N, H * W, C]."""
+        import torch
         N, C, H, W = x.shape
-        y = b.gspc_conv2d_grouped(x, self.packed, N, C, H, W, C, 3, 3, 1, 1, self.conv_groups)
+        y = b._empty((N, C, H, W), torch.float32, x.device)
+        b.gspc_conv2d_grouped(x, self.packed, N, C, H, W, C, 3, 3, 1, 1, self.conv_groups, output=y)
         return b.gspc_pack_channels_last(y)
 
     def answer(self, x):
@@ -39,9 +42,8 @@ class TokenBlock:
         two numbers for each group are kept."""
         import torch
         N, P, C = tokens.shape
-        stats = torch.empty((N, self.norm_groups, 2), dtype=torch.float32, device=tokens.device)
-        saved = (torch.empty((N * P, b.gspc_rows8_pitch(C)), dtype=torch.int8, device=tokens.device),
-                 torch.empty((N * P,), dtype=torch.float32, device=tokens.device))
+        stats = b._empty((N, self.norm_groups, 2), torch.float32, tokens.device)
+        saved = b._new_rows8(N * P, C, tokens.device)
         y = b.gspc_group_norm(tokens, self.gamma, self.beta, self.norm_groups, self.eps, b.ACT_SILU, stats=stats, saved=saved)
         return (y, *b.gspc_group_norm_backward(dy, saved, stats, self.gamma, self.beta, self.norm_groups, b.ACT_SILU))
 
