@@ -314,6 +314,19 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
         }
     GradAffine<V, E> f;
     load_grad_affine<V, E>(h, stats, gamma, beta, n, c0 + at, f);
+    // Eight groups a vector and four vectors of fp32: d takes the place of x at once, and 1 / deviation is fetched where sums are complete, so that
+    // neither has registers during the passes below (kept as for the others, they spilled).
+    constexpr bool CENTRED = E == 8 && HELD == 4 && sizeof(TX) == 4;
+    if constexpr (CENTRED) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rx[k].a[e] -= f.mean[e], rx[k].b[e] -= f.mean[4 + e];
+    }
+    const auto to_d = [&](int k, float (&d)[V]) {
+        if constexpr (CENTRED) widen(rx[k], d);
+        else widen_d<TX, V, E>(f, rx[k], scale[k], d);
+    };
     float dz[HELD][V];
     {
         float sz[V] = {}, sx[V] = {};
@@ -324,7 +337,7 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
                 hold(rx[k]);
                 hold(rg[k]);
                 if ((k + 1) * g.slots > h.P) keep_if(rg[k], slot + k * g.slots < h.P);
-                widen_d<TX, V, E>(f, rx[k], scale[k], d);
+                to_d(k, d);
                 widen(rg[k], dz[k]);
                 to_dz<V, E>(f, h.act, d, dz[k]);
 #pragma unroll
@@ -334,7 +347,7 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
         }
         if (on) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) part[slot * row + at + e] = sz[e], part[(g.slots + slot) * row + at + e] = sx[e] * f.rstd[e * E / V];
+            for (int e = 0; e < V; ++e) part[slot * row + at + e] = sz[e], part[(g.slots + slot) * row + at + e] = CENTRED ? sx[e] : sx[e] * f.rstd[e * E / V];
         }
     }
     __syncthreads();
@@ -346,6 +359,7 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
         for (int j = threadIdx.x & (lanes - 1); j < g.slots; j += lanes) sum += part[(which * g.slots + j) * row + c];
         sum = lanes_sum(sum, lanes);
         if ((threadIdx.x & (lanes - 1)) == 0) {
+            if (CENTRED && which) sum *= stats[(size_t)n * h.groups + group_of(h, c0 + c)].y;
             channel[i] = sum;
             float *to = which ? sum_dx : sum_dz;
             if (to) to[n * ld_sums + c0 + c] = sum;
@@ -363,19 +377,29 @@ __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldG
         }
         a = lanes_sum(a, kWave);
         b = lanes_sum(b, kWave);
-        if (wave_lane == 0) group_ab[k] = make_float2(a / m, b / m);
+        if (wave_lane == 0) {
+            group_ab[k] = make_float2(a / m, b / m);
+            if constexpr (CENTRED) {
+                const float r = stats[(size_t)n * h.groups + group_of(h, c0) + k].y;
+                group_ab[k] = make_float2(r * (a / m), -r * r * (b / m));
+            }
+        }
     }
     __syncthreads();
     GradGroups<E> s;
 #pragma unroll
-    for (int e = 0; e < E; ++e) set_group(f, e, group_ab[group_of(h, at + e * (V / E))], s);
+    for (int e = 0; e < E; ++e) {
+        const float2 ab = group_ab[group_of(h, at + e * (V / E))];
+        if constexpr (CENTRED) s.lambda[e] = ab.x, s.kappa[e] = ab.y;
+        else set_group(f, e, ab, s);
+    }
 #pragma unroll
     for (int k = 0; k < HELD; ++k) {
         if (k * g.slots < h.P) {
             const int p = slot + k * g.slots;
             float d[V];
             hold(rx[k]);
-            widen_d<TX, V, E>(f, rx[k], scale[k], d);
+            to_d(k, d);
             to_dx<V, E>(f, s, d, dz[k]);
             if (on && p < h.P) store(dx + (token0 + p) * lddx + c0 + at, dz[k], past);
         }

@@ -127,3 +127,23 @@ def test_product_of_as_many_tokens_as_there_are(gpu):
     out = b.gspc_matmul_i8(a, w, dtype=b.GSPC_F32)
     for at in range(0, M, step):
         assert torch.equal(out[at:at + step], a[0][at:at + step].float() @ w[0].float().t().contiguous()), at
+
+
+@pytest.mark.parametrize("N,P,C,groups", [(3, 196, 48, 8), (2, 100, 60, 12), (5, 49, 96, 16), (1, 784, 24, 4), (2, 160, 35, 7)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_gradient_of_odd_groups_held(gpu, N, P, C, groups, dtype):
+    """Groups of channels that are no multiple of four, x in fp32, three and four vectors a thread: as test_norm_backward, its tolerance."""
+    import numpy as np
+    from test_gpu_tokens import B, U, dev, grad64, host, norm_inputs
+    torch, b = gpu
+    x, gamma, beta = norm_inputs(N, P, C, N + 2 * P + C, offset=3.0)
+    dy = dev(torch, np.random.default_rng(P).standard_normal((N, P, C)).astype(np.float32), getattr(torch, dtype))
+    xd, gd, bd, st = dev(torch, x), dev(torch, gamma), dev(torch, beta), torch.empty(N, groups, 2, device="cuda")
+    b.gspc_group_norm(xd, gd, bd, groups, act=b.ACT_SILU, stats=st)
+    dx, dgamma, dbeta, size, size_g, size_b, xh, shift = grad64(host(dy), host(xd), host(st), gamma.astype(float), beta.astype(float), groups, 2)
+    got = b.gspc_group_norm_backward(dy, xd, st, gd, bd, groups, b.ACT_SILU)
+    tol = 256 * U * size * (1 + np.abs(xh) + np.abs(shift)) + (B * np.abs(dx) if dtype == "bfloat16" else 0) + 1e-30
+    rel = 1 + np.abs(shift).max()
+    assert (np.abs(host(got[0]) - dx) <= tol).all(), np.max(np.abs(host(got[0]) - dx) / tol)
+    assert (np.abs(host(got[1]) - dgamma) <= 256 * U * rel * size_g + 1e-30).all()
+    assert (np.abs(host(got[2]) - dbeta) <= 256 * U * rel * size_b + 1e-30).all()
