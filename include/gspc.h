@@ -279,7 +279,7 @@ size_t gspc_group_norm_backward_workspace_bytes(int N, int P, int C, int groups,
  *   saved       : receives x as 8-bit rows, with saved_scale, in the same pass: what a training step keeps
  *                 of x for the gradient; or NULL
  *   workspace   : dev, 16-byte aligned, as large as said above (GSPC_ERR_SPACE if it is too small; a call that is
- *                 given stats needs none of it for these); not initialised */
+ *                 given stats needs none of it for these, 8 * N * groups bytes less where it is not 0); not initialised */
 int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma, const float *beta, int N, int P, int C,
                     int groups, float eps, int act, void *y, int y_dtype, int64_t ldy, float *y_scale, float *stats,
                     void *saved, float *saved_scale, void *workspace, size_t workspace_bytes);

@@ -477,11 +477,11 @@ static void launch_stats(const NormShape &h, const NormGrid &g, const NormForwar
 }
 
 // Statistics of the caller's that it did not ask for, and the parts of two-launch ones.
-size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8) {
+size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8, bool given) {
     HeldGrid held;
     const bool hold = x_dtype == GSPC_F32 ? plan_held(h, 4, held_most<float>(), 512, &held) : plan_held(h, 2, held_most<uint16_t>(), 512, &held);
     if (hold && !rows8) return 0;
-    const size_t stats = (size_t)h.N * h.groups * sizeof(float2);
+    const size_t stats = given ? 0 : (size_t)h.N * h.groups * sizeof(float2);
     if (hold) return stats;
     const NormGrid g = norm_grid(h, kForwardBlocks, kForwardChunks);
     return stats + (size_t)h.N * g.chunks * norm_parts(h, g) * sizeof(float2);
@@ -503,7 +503,7 @@ template <typename TX, int V>
 static hipError_t forward(const NormShape &h, NormForward f, void *ws, hipStream_t s, const char **name) {
     const NormGrid g = norm_grid(h, kForwardBlocks, kForwardChunks);
     float2 *stats = f.stats ? reinterpret_cast<float2 *>(f.stats) : static_cast<float2 *>(ws);
-    float2 *parts = static_cast<float2 *>(ws) + (size_t)h.N * h.groups;
+    float2 *parts = static_cast<float2 *>(ws) + (f.stats ? 0 : (size_t)h.N * h.groups);
     f.past = f.y_dtype == GSPC_BF16 && (size_t)h.N * h.P * h.C * 2 >= kPastCaches &&
              (f.ldy == (size_t)h.C || whole_pieces(f.y, (size_t)h.C * 2, f.ldy * 2));
     HeldGrid held;

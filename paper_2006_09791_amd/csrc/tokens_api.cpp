@@ -116,7 +116,7 @@ size_t gspc_group_norm_workspace_bytes(int N, int P, int C, int groups, int x_dt
     gspc::NormShape h;
     if (check_norm(N, P, C, groups, GSPC_ACT_NONE, &h) || (int64_t)N * P == 0) return 0;
     if (!dense(x_dtype)) return fail(GSPC_ERR_DTYPE, "unknown dtype %d", x_dtype), 0;
-    return gspc::norm_forward_bytes(h, x_dtype, rows8 != 0);
+    return gspc::norm_forward_bytes(h, x_dtype, rows8 != 0, false);
 }
 
 size_t gspc_group_norm_backward_workspace_bytes(int N, int P, int C, int groups, int dy_dtype, int x_dtype) {
@@ -140,7 +140,7 @@ int gspc_group_norm(const void *x, int x_dtype, int64_t ldx, const float *gamma,
     if (misaligned(stats, 8)) return fail(GSPC_ERR_ARG, "stats must be 8-byte aligned");
     if ((int64_t)N * P == 0) return GSPC_OK;
     if (!x || !y || (codes && !y_scale) || (saved && !saved_scale)) return fail(GSPC_ERR_NULL, "null pointer argument");
-    if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_forward_bytes(h, x_dtype, (codes || saved) && !stats)))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, gspc::norm_forward_bytes(h, x_dtype, codes || saved, stats != nullptr)))) return rc;
     const gspc::NormForward f = {x, x_dtype, (size_t)ldx, gamma, beta, eps, y, y_dtype, (size_t)ldy, y_scale, stats,
                                  static_cast<int8_t *>(saved), saved_scale, 0};
     const char *name = "";

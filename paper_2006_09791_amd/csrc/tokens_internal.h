@@ -54,8 +54,8 @@ struct NormBackward {
     float *dgamma, *dbeta;          // either may be nullptr
     int past;                       // dx is stored past the caches (set by the launch)
 };
-// Workspace of a call; rows8: one that writes 8-bit rows.
-size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8);
+// Workspace of a call; rows8: one that writes 8-bit rows; given: one that has the caller's memory for the statistics.
+size_t norm_forward_bytes(const NormShape &h, int x_dtype, bool rows8, bool given);
 size_t norm_backward_bytes(const NormShape &h, int dy_dtype);
 hipError_t launch_norm_forward(const NormShape &h, const NormForward &f, void *ws, hipStream_t s, const char **name);
 hipError_t launch_norm_backward(const NormShape &h, const NormBackward &b, void *ws, hipStream_t s, const char **name);

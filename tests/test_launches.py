@@ -95,7 +95,7 @@ def test_norm_launches_reach_every_image(runtime, N, P, C, groups, kind):
     assert rc == 0
     x, st = (X, 2 * P * C), (ST, 8 * groups)
     slabs = (C + 2047) // 2048
-    first = WS + 8 * N * groups                                 # the parts lie behind the statistics that a caller does not ask for
+    first = WS                                                  # of the parts: the statistics are the caller's
     consecutive(found, "norm_stats_kernel", N, [x, (first, 8 * (groups + slabs - 1))])
     consecutive(found, "norm_join_kernel", N, [(first, 8 * (groups + slabs - 1)), st])
     if kind == "dense":
@@ -228,3 +228,15 @@ def test_layout_passes_write_whole_pieces_past_the_caches(runtime, name, C, P, p
     assert goes_past(runtime, name, [X, 0, 256, C, P, Y, 1]) == past
     assert not goes_past(runtime, name, [X, 1, 256, C, P, Y, 0])         # fp32
     assert not goes_past(runtime, name, [X, 0, 1, C, P, Y, 1])           # small
+
+
+def test_norm_given_statistics_needs_no_workspace_for_them(runtime):
+    """In two passes: the parts' bytes alone, from the workspace's start on."""
+    N, P, C, groups = 3, 70000, 8, 2
+    need, own = fake_runtime.b.gspc_group_norm_workspace_bytes(N, P, C, groups, 0), 8 * N * groups
+    call = lambda stats, given: ("gspc_group_norm", [X, 0, C, None, None, N, P, C, groups, 1e-5, 0, Y, 0, C, None, stats, None, None, WS, given])  # noqa: E731
+    results = fake_runtime.launches(runtime, [call(None, need - 1), call(ST, need - own - 1), call(None, need), call(ST, need - own)], NORM)
+    assert [rc for rc, _ in results] == [-6, -6, 0, 0]
+    for (_, found), first in zip(results[2:], (WS + own, WS)):
+        assert number([args for k, _, _, args in found if k == "norm_stats_kernel"][0][2]) == first
+        assert number([args for k, _, _, args in found if k == "norm_apply_kernel"][0][3]) == Y
