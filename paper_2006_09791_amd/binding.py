@@ -503,7 +503,7 @@ def gspc_group_norm_backward_workspace_bytes(N, P, C, groups, dy_dtype, x_dtype)
 
 
 def _tokens(x, what):
-    if x.dim() < 3:
+    if _on_gpu(x, what).dim() < 3:
         raise GspcError(-2, f"{what}: [images, pixels, channels] is needed")
     N, C, P = x.shape[0], x.shape[-1], 1
     for n in x.shape[1:-1]:
@@ -534,7 +534,7 @@ def gspc_group_norm(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, out=None, dt
         rc = _fast.norm(x, gamma, beta, groups, eps, act, out, stats, saved, workspace)
         if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
             N, P, C = _tokens(x, "x")
-            need = gspc_group_norm_workspace_bytes(N, P, C, groups, _dtype(x, "x"), isinstance(out, tuple) or saved is not None)
+            need = gspc_group_norm_workspace_bytes(N, P, C, groups, _dtype(x, "x"), isinstance(out, (tuple, list)) or saved is not None)
             rc = _fast.norm(x, gamma, beta, groups, eps, act, out, stats, saved, _scratch(need, x.device))
         if _done(rc):
             return out
@@ -543,7 +543,7 @@ def gspc_group_norm(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, out=None, dt
     N, P, C = _tokens(x, "x")
     if out is None:
         out = _new_rows8(N * P, C, x.device) if dtype == GSPC_I8 else _empty(x.shape, x.dtype if dtype is None else _torch_dtype(dtype), x.device)
-    if isinstance(out, tuple):
+    if isinstance(out, (tuple, list)):
         (y, y_scale), kind, ldy = _rows8(out, N * P, C, "out"), GSPC_I8, 0
     else:
         _same_shape(out, x.shape, "out")
@@ -564,14 +564,14 @@ def gspc_group_norm_backward(dy, x, stats, gamma, beta, groups, act=ACT_NONE, dx
         rc = _fast.norm_backward(dy, x, stats, gamma, beta, groups, act, dx, dgamma, dbeta, workspace)
         if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
             N, P, C = _tokens(dy, "dy")
-            need = gspc_group_norm_backward_workspace_bytes(N, P, C, groups, _dtype(dy, "dy"), GSPC_I8 if isinstance(x, tuple) else _dtype(x, "x"))
+            need = gspc_group_norm_backward_workspace_bytes(N, P, C, groups, _dtype(dy, "dy"), GSPC_I8 if isinstance(x, (tuple, list)) else _dtype(x, "x"))
             rc = _fast.norm_backward(dy, x, stats, gamma, beta, groups, act, dx, dgamma, dbeta, _scratch(need, dy.device))
         if _done(rc):
             return dx, dgamma, dbeta
     import torch
     lib = load()
     N, P, C = _tokens(dy, "dy")
-    if isinstance(x, tuple):
+    if isinstance(x, (tuple, list)):
         (px, x_scale), kind, ldx = _rows8(x, N * P, C, "x"), GSPC_I8, 0
     else:
         _same_shape(x, dy.shape, "x")

@@ -147,3 +147,15 @@ def test_gradient_of_odd_groups_held(gpu, N, P, C, groups, dtype):
     assert (np.abs(host(got[0]) - dx) <= tol).all(), np.max(np.abs(host(got[0]) - dx) / tol)
     assert (np.abs(host(got[1]) - dgamma) <= 256 * U * rel * size_g + 1e-30).all()
     assert (np.abs(host(got[2]) - dbeta) <= 256 * U * rel * size_b + 1e-30).all()
+
+
+def test_pairs_as_lists(gpu):
+    torch, b = gpu
+    x = torch.randn(2, 9, 24, device="cuda")
+    pair = lambda: [torch.empty(18, 32, dtype=torch.int8, device="cuda"), torch.empty(18, device="cuda")]  # noqa: E731
+    st, out, kept = torch.empty(2, 3, 2, device="cuda"), pair(), pair()
+    assert b.gspc_group_norm(x, None, None, 3, out=out, stats=st, saved=kept) is out
+    want = b.gspc_group_norm(x, None, None, 3, dtype=b.GSPC_I8)
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+    for p, q in zip(b.gspc_group_norm_backward(x, kept, st, None, None, 3), b.gspc_group_norm_backward(x, tuple(kept), st, None, None, 3)):
+        assert torch.equal(p, q)

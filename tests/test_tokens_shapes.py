@@ -42,3 +42,13 @@ def test_norm_tensors_of_another_shape_are_left_to_the_general_route(call):  # n
     for other in (turned, flat, fake(96, (2, 3, 2, 2, 24))):
         assert norm(x, other) is back(x, other, same) is back(x, same, other) is NotImplemented
     assert len(seen) == 2
+
+
+def test_pairs_may_be_lists():
+    """8-bit rows as a list of two, outputs given or not: what is wrong with host tensors is that they are not on the GPU."""
+    x, pair = torch.zeros(2, 3, 16), [torch.zeros(6, 16, dtype=torch.int8), torch.zeros(6)]
+    for c in (lambda: b.gspc_group_norm(x, None, None, 4, out=pair), lambda: b.gspc_group_norm(x, None, None, 4, saved=pair),
+              lambda: b.gspc_group_norm_backward(x, pair, torch.zeros(2, 4, 2), None, None, 4),
+              lambda: b.gspc_quantize_rows(x, out=pair), lambda: b.gspc_dequantize_rows(pair, 16), lambda: b.gspc_matmul_i8(pair, pair)):
+        with pytest.raises(b.GspcError, match="GPU"):
+            c()
