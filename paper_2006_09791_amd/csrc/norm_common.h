@@ -32,7 +32,7 @@ __device__ __forceinline__ NormBlock norm_block(const NormShape &h, const NormGr
     b.c0 = (q - n * g.slabs) * kSlab;
     b.c1 = min(b.c0 + kSlab, h.C);
     b.r0 = b.chunk * g.rows;
-    b.r1 = min(b.r0 + g.rows, h.P);
+    b.r1 = b.r0 + min(g.rows, h.P - b.r0);
     b.ty = fast_div(threadIdx.x, g.m_nvs);
     b.tx = threadIdx.x - b.ty * g.nvs;
     b.nv = g.V == 1 ? b.c1 - b.c0 : (b.c1 - b.c0 + 7) / 8;
@@ -52,12 +52,12 @@ inline NormGrid norm_grid(const NormShape &h, int blocks_wanted, int most_chunks
     g.threads = round_up(g.TY * g.nvs, kWave);
     // enough blocks to fill the chip, of at least four rows per thread, or one where four leave compute units without a block
     long want = blocks_wanted / ((long)h.N * g.slabs), most = (h.P + 4L * g.TY - 1) / (4L * g.TY);
-    if (most * h.N * g.slabs < 256) most = (h.P + g.TY - 1) / g.TY, want = 256 / ((long)h.N * g.slabs);
+    if (most * h.N * g.slabs < 256) most = (h.P - 1) / g.TY + 1, want = 256 / ((long)h.N * g.slabs);
     if (want > most) want = most;
     if (want > most_chunks) want = most_chunks;
     if (want < 1) want = 1;
     g.rows = (int)((h.P + want - 1) / want);
-    g.chunks = (h.P + g.rows - 1) / g.rows;
+    g.chunks = (h.P - 1) / g.rows + 1;
     g.m_nvs = div_magic(g.nvs);
     g.m_chunks = div_magic(g.chunks);
     g.m_slabs = div_magic(g.slabs);
@@ -122,7 +122,7 @@ inline bool held_grid(const NormShape &h, int groups, int threads, int held, Hel
     const long wanted = (long)h.P << g->log_width;          // no more threads than there are vectors
     g->threads = wanted < threads ? round_up((int)wanted, kWave) : threads;
     g->slots = g->threads >> g->log_width;
-    if ((h.P + g->slots - 1) / g->slots > held) return false;
+    if ((h.P - 1) / g->slots >= held) return false;
     g->unit = h.D % 8 == 0 ? 8 : 1;
     g->units = h.D / g->unit;
     g->m_segs = div_magic(g->segs);
@@ -148,7 +148,7 @@ inline bool plan_held(const NormShape &h, int size, int held, int most, HeldGrid
             HeldGrid g;
             if (!held_grid(h, s, t, held, &g)) continue;
             const bool fills = (long)h.N * g.segs * g.threads >= 65536;
-            if (!fills && t < most && (h.P + g.slots - 1) / g.slots > 2) continue;
+            if (!fills && t < most && (h.P - 1) / g.slots >= 2) continue;
             *best = g;
             found = true;
             break;

@@ -424,7 +424,7 @@ size_t norm_backward_bytes(const NormShape &h, int dy_dtype) {
 
 template <typename TX, typename TG, int V, int E>
 static hipError_t launch_grad_held(const NormShape &h, HeldGrid g, const NormBackward &b, float *sums, hipStream_t s) {
-    const int held = (h.P + g.slots - 1) / g.slots;
+    const int held = (h.P - 1) / g.slots + 1;
     const auto kern = held <= 1 ? norm_grad_held_kernel<TX, TG, V, E, 1> : held <= 2 ? norm_grad_held_kernel<TX, TG, V, E, 2>
                                                                           : norm_grad_held_kernel<TX, TG, V, E, 4>;
     g.log_lanes = 0;

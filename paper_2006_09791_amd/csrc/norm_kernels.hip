@@ -230,8 +230,9 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
     constexpr bool CODES = sizeof(TY) == 1;
     constexpr int H = HELD ? HELD : 1, DEEP = HELD == 1 ? 2 : 1;
     const int n = fast_div_any(blockIdx.x, blocks, m_blocks), width = 1 << log_width, lane = threadIdx.x & (width - 1);
-    const int r0 = ((int)blockIdx.x - n * blocks) * rows, r1 = min(r0 + rows, h.P), slots = 256 >> log_width;
+    const int r0 = ((int)blockIdx.x - n * blocks) * rows, count = min(rows, h.P - r0), slots = 256 >> log_width;
     const int nv = vectors_of<V>(h.C), pitch = rows8_pitch(h.C);
+    const size_t row0 = (size_t)n * h.P + r0;
     stats += (size_t)n * h.groups;
     Raw<TX, V> raw[DEEP][H], next[DEEP][H];
     const auto load = [&](int r, Raw<TX, V> (&to)[DEEP][H]) {
@@ -240,23 +241,23 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_wid
             for (int d = 0; d < DEEP; ++d)
 #pragma unroll
                 for (int k = 0; k < HELD; ++k)
-                    if (r + d * slots < r1 && lane + k * width < nv)
-                        to[d][k] = fetch<V>(x + ((size_t)n * h.P + r + d * slots) * ldx + vector_start<V>(lane + k * width, h.C));
+                    if (r + d * slots < count && lane + k * width < nv)
+                        to[d][k] = fetch<V>(x + (row0 + r + d * slots) * ldx + vector_start<V>(lane + k * width, h.C));
         }
     };
-    load(r0 + (threadIdx.x >> log_width), raw);
+    load(threadIdx.x >> log_width, raw);
     Affine<V> f[H];
     if constexpr (HELD > 0) {
 #pragma unroll
         for (int k = 0; k < HELD; ++k)
             if (lane + k * width < nv) load_affine<V>(h, stats, gamma, beta, vector_start<V>(lane + k * width, h.C), f[k]);
     }
-    for (int r = r0 + (threadIdx.x >> log_width); r < r1; r += DEEP * slots) {
+    for (int r = threadIdx.x >> log_width; r < count; r += DEEP * slots) {
         load(r + DEEP * slots, next);
 #pragma unroll
         for (int d = 0; d < DEEP; ++d) {
-            if (r + d * slots >= r1) continue;
-            const size_t row = (size_t)n * h.P + r + d * slots;
+            if (r + d * slots >= count) continue;
+            const size_t row = row0 + r + d * slots;
             float v[H][V];
             const auto each = [&](auto body) {       // body(first channel, its values, its coefficients)
                 if constexpr (HELD > 0) {
@@ -434,7 +435,7 @@ static void launch_rows(const NormShape &h, const NormForward &f, const float2 *
     const long most = (h.P + 2L * at_once - 1) / (2L * at_once);
     if (blocks > most) blocks = most;
     const int rows = (int)((h.P + blocks - 1) / blocks);
-    blocks = (h.P + rows - 1) / rows;
+    blocks = (h.P - 1) / rows + 1;
     hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * h.N)), dim3(256), 0, s, h, log_width, (int)blocks, rows, div_magic((unsigned)blocks),
                        static_cast<const TX *>(f.x), f.ldx, stats, f.gamma, f.beta, static_cast<TY *>(f.y), f.ldy, f.y_scale, f.saved,
                        f.saved_scale, f.past);
@@ -446,7 +447,7 @@ template <typename TX> constexpr int held_most() { return sizeof(TX) == 4 ? 8 : 
 template <typename TX, typename TY, int V, bool ONE>
 static void launch_held(const NormShape &h, const HeldGrid &g, const NormForward &f, float2 *stats, hipStream_t s) {
     constexpr int MOST = held_most<TX>();
-    const int held = (h.P + g.slots - 1) / g.slots, row = ONE ? g.seg / 8 : g.seg;
+    const int held = (h.P - 1) / g.slots + 1, row = ONE ? g.seg / 8 : g.seg;
     const auto kern = held <= 2 ? norm_held_kernel<TX, TY, V, 2, ONE>
                     : held <= MOST / 2 ? norm_held_kernel<TX, TY, V, MOST / 2, ONE> : norm_held_kernel<TX, TY, V, MOST, ONE>;
     const size_t lds = ((size_t)g.slots * row + 2 * (g.seg / h.D)) * sizeof(float);

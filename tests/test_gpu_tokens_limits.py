@@ -159,3 +159,58 @@ def test_pairs_as_lists(gpu):
     assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
     for p, q in zip(b.gspc_group_norm_backward(x, kept, st, None, None, 3), b.gspc_group_norm_backward(x, tuple(kept), st, None, None, 3)):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("C", [1])
+def test_norm_of_one_image_as_long_as_there_are(gpu, C):
+    """2^31 - 1 tokens: against 64 bits, piece by piece, with the tolerances of test_gpu_tokens (u = 2^-24, 2^-8 for a value rounded to bf16)."""
+    torch, b = gpu
+    P, step, U, B = 0x7fffffff, 1 << 25, 2.0 ** -24, 2.0 ** -8
+    pieces = [slice(at, min(at + step, P)) for at in range(0, P, step)]
+    x = torch.empty(1, P, C, dtype=torch.bfloat16, device="cuda")
+    for s in pieces:
+        x[0, s].normal_()
+    x[0, -1] = 50.0                                             # (the last token counts, and is seen)
+    gamma, beta = 1 + 0.1 * torch.randn(C, device="cuda"), 0.1 * torch.randn(C, device="cuda")
+    st = torch.empty(1, 1, 2, device="cuda")
+    y = b.gspc_group_norm(x, gamma, beta, 1, act=b.ACT_SILU, stats=st)
+    mean = sum(float(x[0, s].double().sum()) for s in pieces) / (P * C)
+    rstd = (sum(float((x[0, s].double() - mean).square().sum()) for s in pieces) / (P * C) + 1e-5) ** -0.5
+    assert abs(float(st[0, 0, 0]) - mean) * rstd <= 256 * U and abs(float(st[0, 0, 1]) / rstd - 1) <= 256 * U
+    rel = 1 + abs(mean) * rstd
+
+    def expected(s, mean, rstd):
+        xh = (x[0, s].double() - mean) * rstd
+        z = xh * gamma + beta
+        return xh, z, torch.sigmoid(z)
+    for s in pieces:
+        xh, z, sig = expected(s, mean, rstd)
+        tol = 256 * U * (rel + xh.abs()) * (gamma.abs() + z.abs()) + 1e-30
+        assert bool(((y[0, s].double() - z * sig).abs() <= tol + B * (z * sig).abs()).all()), s
+    del y
+    q, scale = b.gspc_group_norm(x, gamma, beta, 1, act=b.ACT_SILU, dtype=b.GSPC_I8)
+    for s in pieces:
+        xh, z, sig = expected(s, mean, rstd)
+        want = z * sig
+        tol = 256 * U * (rel + xh.abs()) * (gamma.abs() + z.abs()) + 1e-30
+        err = (q[s, :C].double() * scale[s, None] - want).abs()
+        assert bool((err <= 0.501 * want.abs().amax(1, keepdim=True) / 127 + 2 * tol + tol.amax(1, keepdim=True)).all()), s
+        assert not bool(q[s, C:].any())
+    del q, scale, want, err, tol
+    dx, dgamma, dbeta = b.gspc_group_norm_backward(x, x, st, gamma, beta, 1, b.ACT_SILU)
+    mean, rstd = (float(v) for v in st[0, 0])
+    sums = torch.zeros(4, C, dtype=torch.float64, device="cuda")
+
+    def slope(s):
+        xh, z, sig = expected(s, mean, rstd)
+        return xh, x[0, s].double() * sig * (1 + z * (1 - sig))
+    for s in pieces:
+        xh, dz = slope(s)
+        sums += torch.stack(((dz * xh).sum(0), dz.sum(0), (dz * xh).abs().sum(0), dz.abs().sum(0)))
+    assert bool(((dgamma - sums[0]).abs() <= 256 * U * rel * sums[2]).all()) and bool(((dbeta - sums[1]).abs() <= 256 * U * rel * sums[3]).all())
+    A, BB, a_size, b_size = (float((t * g).sum()) / (P * C) for t, g in zip(sums[[1, 0, 3, 2]], (gamma, gamma, gamma.abs(), gamma.abs())))
+    for s in pieces:
+        xh, dz = slope(s)
+        want = rstd * (gamma * dz - A - xh * BB)
+        size = rstd * ((gamma * dz).abs() + a_size + xh.abs() * b_size)
+        assert bool(((dx[0, s].double() - want).abs() <= 256 * U * size * (rel + xh.abs()) + B * want.abs() + 1e-30).all()), s

@@ -240,3 +240,32 @@ def test_norm_given_statistics_needs_no_workspace_for_them(runtime):
     for (_, found), first in zip(results[2:], (WS + own, WS)):
         assert number([args for k, _, _, args in found if k == "norm_stats_kernel"][0][2]) == first
         assert number([args for k, _, _, args in found if k == "norm_apply_kernel"][0][3]) == Y
+
+
+GRIDS = {"norm_stats_kernel": [(0, 28), (1, 40)], "norm_apply_kernel": [(0, 28), (1, 40)], "norm_grad_sums_kernel": [(0, 28), (1, 40)],
+         "norm_grad_apply_kernel": [(0, 28), (1, 40)], "norm_rows_kernel": [(2, 4), (3, 4)]}
+
+
+@pytest.mark.parametrize("P", [0x7fffffff, 0x7fffffff - 300, 0x7fffffff - (1 << 18), 0x7fffffff - (1 << 23), 1 << 30])
+@pytest.mark.parametrize("C", [1, 8, 24, 2056])
+@pytest.mark.parametrize("N", [1, 2])
+def test_long_images_are_cut_into_all_of_their_rows(runtime, N, P, C):
+    """Up to 2^31 - 1 tokens: rows of a block times blocks reach the last one, and no block begins past it."""
+    if N * P > 0x7fffffff:
+        P //= N
+    b = fake_runtime.b
+    need = [b.gspc_group_norm_workspace_bytes(N, P, C, 1, 1, rows8) for rows8 in (0, 1)] + [b.gspc_group_norm_backward_workspace_bytes(N, P, C, 1, 1, 1)]
+    norm = lambda kind, need: ("gspc_group_norm", [X, 1, C, None, None, N, P, C, 1, 1e-5, 2, Y, kind, C, YS, None, None, None, WS, need])  # noqa: E731
+    back = ("gspc_group_norm_backward", [Y, 1, C, X, 1, C, None, ST, None, None, N, P, C, 1, 2, DX, C, DG, DB, WS, need[2]])
+    for rc, found in fake_runtime.launches(runtime, [norm(1, need[0]), norm(2, need[1]), back], GRIDS):
+        assert rc == 0 and not any("held" in k for k, *_ in found)
+        for kernel, blocks, threads, args in found:
+            if kernel == "norm_rows_kernel":
+                chunks, rows = map(number, args)
+                assert blocks == N * chunks
+            elif args:
+                slabs, (chunks, rows) = struct.unpack("<i", args[1][4:8])[0], struct.unpack("<2i", args[1][20:28])
+                assert blocks >= N * chunks * slabs
+            else:
+                continue
+            assert (chunks - 1) * rows < P <= chunks * rows, kernel
