@@ -161,7 +161,7 @@ def test_pairs_as_lists(gpu):
         assert torch.equal(p, q)
 
 
-@pytest.mark.parametrize("C", [1])
+@pytest.mark.parametrize("C", [1, 8])
 def test_norm_of_one_image_as_long_as_there_are(gpu, C):
     """2^31 - 1 tokens: against 64 bits, piece by piece, with the tolerances of test_gpu_tokens (u = 2^-24, 2^-8 for a value rounded to bf16)."""
     torch, b = gpu
