@@ -242,8 +242,10 @@ int gspc_run_layer_chain(const gspc_layer_t *layers, int n_layers,
  *
  * Tensors may have 2^31 and more elements; rows (N * P, M) are below 2^31 in number.
  * Zero images, pixels, rows or tokens are no work (pointers may then be NULL) and no error.
- * Sums are fp32 (products of 8-bit rows: exact integers) and every result is rounded
- * once.  No atomics: the same call gives the same bits. */
+ * Sums are fp32 (a gradient's over images fp64, products of 8-bit rows exact integers).
+ * Results are rounded once to their type; a product's sum is rounded to fp32 before it is
+ * multiplied by its two scales and the bias is added, in fp32 too: four roundings before
+ * that one.  No atomics: the same call gives the same bits. */
 
 /* Bytes of one 8-bit row of cols values.  0 if cols is not positive or too large. */
 int gspc_rows8_pitch(int cols);

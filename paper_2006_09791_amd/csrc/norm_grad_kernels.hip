@@ -49,7 +49,8 @@ __device__ __forceinline__ void to_dx(const GradAffine<V, E> &f, const GradGroup
     for (int e = 0; e < V; ++e) dz[e] = fmaf(f.a[e], dz[e], fmaf(d[e], s.kappa[e * E / V], -s.lambda[e * E / V]));
 }
 // x -> d.  x of an 8-bit row is q * scale: with u = q + 128 (an unsigned byte converts to fp32 in one instruction)
-// d = u scale - (128 scale + mean), off by less than 2^-17 of a step of the row's.
+// d = u scale - (128 scale + mean), off by 2^-24 of 128 scale + |mean|: 2^-17 of a step of the row's, and where the mean is far larger than the row as
+// much as x - mean is rounded by.
 template <typename TX, int V, int E>
 __device__ __forceinline__ void widen_d(const GradAffine<V, E> &f, const Raw<TX, V> &r, float scale, float (&d)[V]) {
     if constexpr (sizeof(TX) == 1 && V == 8) {
@@ -84,8 +85,8 @@ template <typename TX, typename TG, int V> struct GradBatch {
 };
 
 // Per channel and block: sums of dz and of dz xh over the block's rows, parts [n][chunk][2][C].  5 images of 29x37, 60 channels in fp32:
-// 5.6 us, and 6.0 for dx, latency.  (64 images of 56x56, 256 channels in bf16: 105 us together, 515 MB with what is read
-// twice, 4.9 TB/s; over batches of images whose x and dy fit the memory-side cache 135.)
+// 5.6 us, and 6.0 for dx, latency.  (64 images of 56x56, 256 channels in bf16: 97 us together, 515 MB with what is read
+// twice, 5.3 TB/s; over batches of images whose x and dy fit the memory-side cache 135.)
 template <typename TX, typename TG, int V, int E>
 __global__ __launch_bounds__(kNormThreads) void norm_grad_sums_kernel(NormShape h, NormGrid g, const TG *__restrict__ dy, size_t lddy,
                                                                       const TX *__restrict__ x, size_t ldx,
@@ -278,7 +279,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_apply_kernel(NormShape
 // All but the sum over images in one launch, x and dy read once: a block holds its channels of an image, x as it came and dz in fp32,
 // so that the activation's slope is computed once (256 images of 14x14, 512 channels in bf16 with SiLU: 36 us; with x and dy held as
 // they came and it computed twice 44).  Four vectors a thread: with eight dz spills (69 us on 28x28, 128 channels from 8-bit rows; four in
-// 1024 threads 40 to 48: loads, arithmetic and stores of the one block that a compute unit has room for follow one another).
+// 1024 threads 41.6, 48 where the rows are not in the caches: loads, arithmetic and stores of the one block that a compute unit has room for follow
+// one another; x and dy as they came, eight vectors in 512 threads and the slope computed twice, 38).
 // sums: [n][2][C] for the parameters' gradients, or where there is one image these themselves.
 template <typename TX, typename TG, int V, int E, int HELD>
 __global__ __launch_bounds__(1024) void norm_grad_held_kernel(NormShape h, HeldGrid g, const TG *__restrict__ dy, size_t lddy,

@@ -220,7 +220,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_apply_kernel(NormShape h, N
 // Outputs in 8-bit rows need all of a row's channels: `width` lanes hold one row, HELD vectors each with their coefficients, and
 // walk down the rows of an image, several at a time so that their loads are in flight together (HELD = 0: rows of any length,
 // read and computed twice).  TY = int8_t: y is 8-bit rows; SAVE: x is written as 8-bit rows too.  64 images of 14x14, 512 channels
-// to 8-bit rows 9.3 us, half of it arithmetic; 256 of 28x28, 128 channels with SAVE 25.4 us, 128 MB.
+// to 8-bit rows 9.3 us, half of it arithmetic; 256 of 28x28, 128 channels with SAVE 24.9 us, 128 MB.
 template <typename TX, typename TY, int V, int HELD, bool SAVE>
 __global__ __launch_bounds__(256) void norm_rows_kernel(NormShape h, int log_width, int blocks, int rows, unsigned m_blocks,
                                                         const TX *__restrict__ x, size_t ldx, const float2 *__restrict__ stats,

@@ -6,7 +6,7 @@ namespace gspc {
 
 // `width` lanes (a power of two up to a wave) hold one row, lane l the vectors l, l + width, ...  HELD of them per lane stay in
 // registers between the maximum and the rounding; HELD = 0: rows of any length, read a second time.  Bound by memory: 2 or 4
-// bytes of a value in, one out; 50176 rows of 512 in bf16 16.9 us, 4.6 TB/s.  (Written past the caches, these took 5 us longer to write
+// bytes of a value in, one out; 50176 rows of 512 in bf16 14.5 us, 5.3 TB/s.  (Written past the caches, these took 5 us longer to write
 // and read back.)
 template <typename T, int V, int HELD>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict__ x, size_t ldx, unsigned rows, int cols, int width,
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict_
     if (lane == 0) scale[row] = c.scale;
 }
 
-// 50176 rows of 512 to bf16: 14.1 us, 5.5 TB/s.
+// 50176 rows of 512 to bf16: 13.9 us, 5.5 TB/s.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void dequantize_rows_kernel(const int8_t *__restrict__ q, const float *__restrict__ scale,
                                                               unsigned rows, int cols, int width, T *__restrict__ x, size_t ldx, int past) {
