@@ -441,7 +441,8 @@ def _change_layout(call, x, out, dtype, pack):
     shape = (N, P, C) if pack else (N, C, P)
     if out is None:
         out = _empty(shape, _torch_dtype(dtype), x.device)
-    elif out.dim() < 3 or out.shape[0] != N or out.shape[-1 if pack else 1] != C or out.numel() != x.numel():
+    elif not ((out.dim() >= 3 and out.shape[0] == N and out.shape[-1 if pack else 1] == C and out.numel() == x.numel())
+              or (pack and tuple(out.shape) == (N * P, C))):
         raise GspcError(-2, f"out has shape {tuple(out.shape)}, expected {shape}, with its pixels in one dimension or more")
     elif not _on_gpu(out, "out").is_contiguous():
         raise GspcError(-8, "out must be contiguous")
@@ -450,7 +451,7 @@ def _change_layout(call, x, out, dtype, pack):
 
 
 def gspc_pack_channels_last(x, out=None, dtype=GSPC_BF16):
-    """x [N, C, ...] (planes) -> [N, P, C] (tokens), P the pixels of a plane; `out`: a tensor [N, ..., C] to write into."""
+    """x [N, C, ...] (planes) -> [N, P, C] (tokens), P the pixels of a plane; `out`: a tensor [N, ..., C] or [N * P, C] to write into."""
     if out is not None and _fast is not None and _done(_fast.pack(x, out)):
         return out
     return _change_layout(load().gspc_pack_channels_last, x, out, dtype, True)

@@ -193,11 +193,11 @@ static int fits(int64_t v) { return v > 0 && v < 0x7ffffff0; }
     Py_END_ALLOW_THREADS             \
     return PyLong_FromLong(rc)
 
-/* pack(x [N, C, P], out [N, ..., C]), unpack(x [N, P, C], out [N, C, ...]) */
+/* pack(x [N, C, P], out [N, ..., C] or [N * P, C]), unpack(x [N, P, C], out [N, C, ...]) */
 static PyObject *layout(PyObject *const *a, Py_ssize_t n, int pack) {
     tensor_t x, out;
     if (n != 2 || !g_calls.pack || !tensor(a[0], &x) || x.dims != 3 || !fits(x.count) || x.type == 2 || !tensor(a[1], &out) || out.type == 2 ||
-        out.count != x.count || out.dims < 3 || out.first != x.first || (pack ? out.last != x.second : out.second != x.last))
+        out.count != x.count || out.dims < (pack ? 2 : 3) || (out.dims > 2 && out.first != x.first) || (pack ? out.last != x.second : out.second != x.last))
         GENERAL;
     const int N = (int)x.first, C = (int)(pack ? x.second : x.last);
     CALL((pack ? g_calls.pack : g_calls.unpack)(x.ptr, x.type, N, C, (int)(x.count / N / C), out.ptr, out.type));

@@ -214,3 +214,11 @@ def test_norm_of_one_image_as_long_as_there_are(gpu, C):
         want = rstd * (gamma * dz - A - xh * BB)
         size = rstd * ((gamma * dz).abs() + a_size + xh.abs() * b_size)
         assert bool(((dx[0, s].double() - want).abs() <= 256 * U * size * (rel + xh.abs()) + B * want.abs() + 1e-30).all()), s
+
+
+def test_layout_into_rows_of_tokens(gpu):
+    torch, b = gpu
+    x = torch.randn(2, 12, 35, device="cuda")
+    for out in (torch.empty(70, 12, device="cuda"), torch.empty(2, 5, 7, 12, device="cuda")):
+        assert b.gspc_pack_channels_last(x, out=out) is out and torch.equal(out.view(2, 35, 12), x.transpose(1, 2))
+        assert b.gspc_pack_channels_last(x.view(2, 12, 5, 7), out=out.zero_()) is out and torch.equal(out.view(2, 35, 12), x.transpose(1, 2))

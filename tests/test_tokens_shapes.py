@@ -14,13 +14,13 @@ class Fake(torch.Tensor):
 
 def test_layout_outputs(call):  # noqa: F811
     c, seen = call
-    for out in ((2, 5, 3), (2, 1, 5, 3), (2, 5, 1, 3)):
+    for out in ((2, 5, 3), (2, 1, 5, 3), (2, 5, 1, 3), (10, 3)):
         assert c.pack(fake(16, (2, 3, 5)), fake(32, out)) == -100
     for out in ((2, 3, 5), (2, 3, 5, 1), (2, 3, 1, 5)):
         assert c.unpack(fake(16, (2, 5, 3)), fake(32, out)) == -101
-    assert [a[2:5] for _, a in seen] == [(2, 3, 5)] * 6
+    assert [a[2:5] for _, a in seen] == [(2, 3, 5)] * 7
     del seen[:]
-    for out in ((2, 3, 5), (5, 2, 3), (3, 10), (30,), (10, 3), (1, 10, 3)):
+    for out in ((2, 3, 5), (5, 2, 3), (3, 10), (30,), (1, 10, 3), (5, 6), (30, 1)):
         assert c.pack(fake(16, (2, 3, 5)), fake(32, out)) is NotImplemented
         with pytest.raises(b.GspcError, match="out has shape"):
             b.gspc_pack_channels_last(torch.zeros(2, 3, 5).as_subclass(Fake), out=torch.zeros(out).as_subclass(Fake))
