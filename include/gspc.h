@@ -53,9 +53,9 @@ enum {
 };
 
 /* Element type of the input tensor and of the packed weights.  The output is
- * always fp32 and accumulation is always fp32.  (GSPC_I8, 8-bit rows: channels-last
- * operators only, see there.) */
-enum { GSPC_F32 = 0, GSPC_BF16 = 1, GSPC_I8 = 2 };
+ * always fp32 and accumulation is always fp32.  (GSPC_I8 and GSPC_F8, 8-bit rows of
+ * whole numbers and of e4m3: operators on tokens only, see there.) */
+enum { GSPC_F32 = 0, GSPC_BF16 = 1, GSPC_I8 = 2, GSPC_F8 = 3 };
 
 /* Kernel families (for gspc_force_path / gspc_last_path). */
 enum { GSPC_PATH_AUTO = -1, GSPC_PATH_DIRECT = 0, GSPC_PATH_MFMA = 1 };
@@ -303,6 +303,86 @@ int gspc_group_norm_backward(const void *dy, int dy_dtype, int64_t lddy, const v
  *   out  : dense rows, fp32 or bf16 (out_dtype, ldo) */
 int gspc_matmul_i8(const void *a, const float *a_scale, const void *w, const float *w_scale, const float *bias, int64_t M,
                    int N, int K, void *out, int out_dtype, int64_t ldo);
+
+/* ---- a residual block on tokens -----------------------------------------------
+ *
+ * What a residual block of pointwise layers is made of, for answering and for training: products in 8-bit floating point with their
+ * gradients, the norms before and after a block with its gate and residual, and dropout.  Dense rows as above.
+ *
+ *   8-bit float rows  (GSPC_F8) e4m3 values [rows][pitch], pitch = gspc_f8_pitch(cols) (cols rounded up to 128), ZERO past the last
+ *                     column, 16-byte aligned; and a byte for each 128 columns, [rows][gspc_f8_scale_pitch(cols)] (rounded up to four),
+ *                     4-byte aligned: the exponent, plus 127, of the power of two that they are multiplied by (255: no number).
+ *
+ * Zero rows are no work.  Sums are fp32 (over blocks of tokens fp64), results rounded once to their type.  No atomics: the same
+ * call gives the same bits. */
+
+/* Bytes of one row's values, and of its powers of two.  0 if cols is not positive or too large. */
+int gspc_f8_pitch(int cols);
+int gspc_f8_scale_pitch(int cols);
+
+/* Writes dense rows x [rows][cols] as 8-bit float rows: along the rows (q, scale: rows of cols), along the columns (qt, scale_t: the transpose,
+ * cols rows of `rows` values), or both in one pass; either pair may be NULL.  In each block of 128 values the power of two is the
+ * smallest from 2^-127 on that brings the largest finite magnitude to 448 at most (2^-127 where all are 0); values are rounded to nearest,
+ * ties to even; infinities and NaN become NaN, in their places, and have no say in the power of two. */
+int gspc_quantize_rows_f8(const void *x, int dtype, int64_t ldx, int64_t rows, int cols, void *q, uint8_t *scale, void *qt, uint8_t *scale_t);
+/* Reads rows back (in bf16 exactly, down to its smallest normal number). */
+int gspc_dequantize_rows_f8(const void *q, const uint8_t *scale, int64_t rows, int cols, void *x, int dtype, int64_t ldx);
+
+/* out[m][n] = sum over k < K of a[m][k] w[n][k] (+ bias[n]), a [M] and w [N] 8-bit float rows of K values, K at most 2^22.  The gradients of
+ * y = x w^T are the same product: dx of dy's rows and w's columns form, dw of dy's and x's columns forms.
+ *   bias      : dev fp32 [N], or NULL
+ *   out       : dense rows, fp32 or bf16 (out_dtype, ldo)
+ *   workspace : dev, 16-byte aligned, as large as said (0: none is needed): parts of long sums of few outputs; not initialised */
+size_t gspc_matmul_f8_workspace_bytes(int64_t M, int N, int K);
+int gspc_matmul_f8(const void *a, const uint8_t *a_scale, const void *w, const uint8_t *w_scale, const float *bias, int64_t M, int N, int K,
+                   void *out, int out_dtype, int64_t ldo, void *workspace, size_t workspace_bytes);
+
+/* Dropout: each value is dropped (0 whatever it was) or kept and divided by 1 - drop; drop, from 0 to 1, counts in steps of 2^-16.  Which, says Philox
+ * 4x32-10 under the key `seed` for the counter (column / 8, row, low and high word of offset + *step): of its words' eight 16-bit
+ * halves, low ones first, each column's is compared with 65536 drop.  No mask is stored: the same call on dy is the gradient.  A
+ * program takes another offset for each call.
+ *   step : dev, 8-byte aligned, added to offset as the kernel runs (a captured graph's replays take their offsets from it), or NULL
+ *   y    : type of x; may be x itself */
+int gspc_dropout(const void *x, int dtype, int64_t ldx, int64_t rows, int cols, double drop, uint64_t seed, uint64_t offset, const uint64_t *step,
+                 void *y, int64_t ldy);
+
+/* Norm over a token's channels: NORM_RMS x / sqrt(mean x^2 + eps), NORM_LAYER (x - mean) / sqrt(var + eps). */
+enum { GSPC_NORM_NONE = 0, GSPC_NORM_RMS = 1, GSPC_NORM_LAYER = 2 };
+
+/* Between two blocks: u = post_gamma * post(h) + post_beta, x' = scale * x + gate * dropout(u), z = act(pre_gamma * pre(x') + pre_beta): the output h of
+ * one normalised, gated and added to the residual stream x, and the stream normalised for the next. */
+typedef struct gspc_residual {
+    int64_t rows, gates;        /* tokens, and gates: token t has gate t / (rows / gates); ignored without gate */
+    int cols;                   /* channels, at most 8192 */
+    int post, pre, act;         /* norm of h, norm of x', activation behind it */
+    const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;     /* dev fp32 [cols], or NULL for 1 and 0 (as they must be without the norm) */
+    const float *gate;          /* dev fp32 [gates][cols], or NULL for 1 */
+    float scale, eps;
+    double drop;                /* dropout as above, of rows and columns of u */
+    uint64_t seed, offset;
+    const uint64_t *step;
+} gspc_residual_t;
+
+/*   h       : dense rows; or NULL: x' = scale * x (then without post, gate and dropout)
+ *   xo      : receives x', type of x; may be x itself; or NULL
+ *   z       : dense rows, fp32 or bf16, or 8-bit float rows (GSPC_F8; ldz ignored) with z_scale; of x' before it is rounded; or NULL
+ *   stats   : dev fp32 [rows][4], 16-byte aligned, receives h's mean and 1 / sqrt(var + eps), then x''s (0 and 1 without the norm), for the gradient; or
+ *             NULL */
+int gspc_residual_norm(const gspc_residual_t *r, const void *x, int x_dtype, int64_t ldx, const void *h, int h_dtype, int64_t ldh, void *xo,
+                       int64_t ldxo, void *z, int z_dtype, int64_t ldz, uint8_t *z_scale, float *stats);
+
+/* Its gradient: dx, dh and the parameters' from dz and dxo, the gradients of z and x' (dxo: what comes down the residual stream).
+ *   dz, dxo : dense rows, dxo of x's type; either may be NULL for zero
+ *   xo, h   : from the forward call (xo may be NULL where dz is; x_dtype is dx's type too, h_dtype dh's)
+ *   stats   : from the forward call
+ *   dx, dh  : dx may be dxo itself, dh may be h itself; dh NULL without h
+ *   dgate [gates][cols], dpost_gamma, dpost_beta, dpre_gamma, dpre_beta [cols] : dev fp32, overwritten (zeros where there are no tokens), or NULL
+ *   workspace : dev, 16-byte aligned, as large as said; not initialised.  gates: 1 without a gate */
+size_t gspc_residual_norm_backward_workspace_bytes(int64_t rows, int cols, int64_t gates);
+int gspc_residual_norm_backward(const gspc_residual_t *r, const void *dz, int dz_dtype, int64_t lddz, const void *dxo, int64_t lddxo,
+                                const void *xo, int x_dtype, int64_t ldxo, const void *h, int h_dtype, int64_t ldh, const float *stats, void *dx,
+                                int64_t lddx, void *dh, int64_t lddh, float *dgate, float *dpost_gamma, float *dpost_beta, float *dpre_gamma,
+                                float *dpre_beta, void *workspace, size_t workspace_bytes);
 
 #ifdef __cplusplus
 }

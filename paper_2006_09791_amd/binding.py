@@ -6,6 +6,7 @@ torch tensors (PyTorch is used for device memory and streams, nothing else);
 every computation runs in the library's HIP kernels.  There is no CPU
 fallback: if the library is missing or a call fails, an exception is raised.
 """
+import collections
 import ctypes
 import os
 import threading
@@ -13,11 +14,13 @@ import threading
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libgspc.so")
 
-GSPC_F32, GSPC_BF16, GSPC_I8 = 0, 1, 2
+GSPC_F32, GSPC_BF16, GSPC_I8, GSPC_F8 = 0, 1, 2, 3
 PATH_AUTO, PATH_DIRECT, PATH_MFMA = -1, 0, 1
 OP_CONV, OP_MAXPOOL, OP_ADD, OP_RELU = 0, 1, 2, 3
 FLAG_RELU = 1
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+F8_ROWS, F8_COLUMNS, F8_BOTH = 1, 2, 3
 
 ERROR_NAMES = {0: "GSPC_OK", -1: "GSPC_ERR_NULL", -2: "GSPC_ERR_DIM", -3: "GSPC_ERR_GROUPS",
                -4: "GSPC_ERR_DTYPE", -5: "GSPC_ERR_MISMATCH", -6: "GSPC_ERR_SPACE",
@@ -30,6 +33,8 @@ EXPORTS = [
     "gspc_last_path", "gspc_last_kernel", "gspc_set_graph_mode", "gspc_set_chain_fusion", "gspc_set_winograd", "gspc_run_layer_chain",
     "gspc_rows8_pitch", "gspc_pack_channels_last", "gspc_unpack_channels_last", "gspc_quantize_rows", "gspc_dequantize_rows",
     "gspc_group_norm_workspace_bytes", "gspc_group_norm_backward_workspace_bytes", "gspc_group_norm", "gspc_group_norm_backward", "gspc_matmul_i8",
+    "gspc_f8_pitch", "gspc_f8_scale_pitch", "gspc_quantize_rows_f8", "gspc_dequantize_rows_f8", "gspc_matmul_f8_workspace_bytes", "gspc_matmul_f8",
+    "gspc_dropout", "gspc_residual_norm", "gspc_residual_norm_backward_workspace_bytes", "gspc_residual_norm_backward",
 ]
 
 
@@ -48,6 +53,14 @@ class GspcLayer(ctypes.Structure):
                 ("w", ctypes.c_void_p)]
 
 
+class GspcResidual(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("gates", ctypes.c_int64), ("cols", ctypes.c_int), ("post", ctypes.c_int),
+                ("pre", ctypes.c_int), ("act", ctypes.c_int), ("post_gamma", ctypes.c_void_p), ("post_beta", ctypes.c_void_p),
+                ("pre_gamma", ctypes.c_void_p), ("pre_beta", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("drop", ctypes.c_double), ("seed", ctypes.c_uint64),
+                ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
 _thread = threading.local()     # stream: the library's, as gspc_set_stream was last given it
 _lib = None
 _conv = None     # gspc_conv2d_grouped through _gspc_call, or _no_conv
@@ -62,6 +75,7 @@ def _no_conv(*args):
 class _NoFast:
     """Every call of a channels-last operator is one that only ctypes converts."""
     pack = unpack = quantize = dequantize = norm = norm_backward = matmul = staticmethod(_no_conv)
+    quantize_f8 = dequantize_f8 = matmul_f8 = dropout = residual_norm = residual_norm_backward = staticmethod(_no_conv)
 
 
 def load():
@@ -131,6 +145,25 @@ def load():
     lib.gspc_group_norm_backward.argtypes = [vp, i, ll, vp, i, ll, vp, vp, vp, vp, i, i, i, i, i, vp, ll, vp, vp, vp, sz]
     lib.gspc_matmul_i8.restype = i
     lib.gspc_matmul_i8.argtypes = [vp, vp, vp, vp, vp, ll, i, i, vp, i, ll]
+    d, u64, rp = ctypes.c_double, ctypes.c_uint64, ctypes.POINTER(GspcResidual)
+    lib.gspc_f8_pitch.restype = lib.gspc_f8_scale_pitch.restype = i
+    lib.gspc_f8_pitch.argtypes = lib.gspc_f8_scale_pitch.argtypes = [i]
+    lib.gspc_quantize_rows_f8.restype = i
+    lib.gspc_quantize_rows_f8.argtypes = [vp, i, ll, ll, i, vp, vp, vp, vp]
+    lib.gspc_dequantize_rows_f8.restype = i
+    lib.gspc_dequantize_rows_f8.argtypes = [vp, vp, ll, i, vp, i, ll]
+    lib.gspc_matmul_f8_workspace_bytes.restype = sz
+    lib.gspc_matmul_f8_workspace_bytes.argtypes = [ll, i, i]
+    lib.gspc_matmul_f8.restype = i
+    lib.gspc_matmul_f8.argtypes = [vp, vp, vp, vp, vp, ll, i, i, vp, i, ll, vp, sz]
+    lib.gspc_dropout.restype = i
+    lib.gspc_dropout.argtypes = [vp, i, ll, ll, i, d, u64, u64, vp, vp, ll]
+    lib.gspc_residual_norm.restype = i
+    lib.gspc_residual_norm.argtypes = [rp, vp, i, ll, vp, i, ll, vp, ll, vp, i, ll, vp, vp]
+    lib.gspc_residual_norm_backward_workspace_bytes.restype = sz
+    lib.gspc_residual_norm_backward_workspace_bytes.argtypes = [ll, i, ll]
+    lib.gspc_residual_norm_backward.restype = i
+    lib.gspc_residual_norm_backward.argtypes = [rp, vp, i, ll, vp, ll, vp, i, ll, vp, i, ll, vp, vp, ll, vp, ll, vp, vp, vp, vp, vp, vp, sz]
     try:
         from . import _gspc_call
     except ImportError:          # not built for this interpreter
@@ -140,6 +173,9 @@ def load():
         _gspc_call.bind_tokens(*[ctypes.cast(f, vp).value for f in (
             lib.gspc_pack_channels_last, lib.gspc_unpack_channels_last, lib.gspc_quantize_rows, lib.gspc_dequantize_rows, lib.gspc_group_norm,
             lib.gspc_group_norm_backward, lib.gspc_matmul_i8)], torch.float32, torch.bfloat16, torch.int8)
+        _gspc_call.bind_block(*[ctypes.cast(f, vp).value for f in (
+            lib.gspc_quantize_rows_f8, lib.gspc_dequantize_rows_f8, lib.gspc_matmul_f8, lib.gspc_dropout, lib.gspc_residual_norm,
+            lib.gspc_residual_norm_backward)], torch.float8_e4m3fn, torch.uint8, torch.int64)
         _conv, _fast = _gspc_call.conv, _gspc_call
     _lib = lib
     return lib
@@ -621,3 +657,244 @@ def gspc_matmul_i8(a, w, bias=None, out=None, dtype=GSPC_BF16, cols=None):
     _check(lib.gspc_matmul_i8(qa, sa, qw, sw, _flat(bias, torch.float32, N, "bias"), M, N, K, out.data_ptr(), _dtype(out, "out"),
                               _row_stride(out, "out")))
     return out
+
+
+# ---- a residual block on tokens ------------------------------------------------------------------
+# 8-bit float rows are a pair (float8_e4m3fn tensor [rows, pitch], uint8 tensor [rows, scale pitch]).
+
+def gspc_f8_pitch(cols):
+    if cols <= 0 or cols > 0x7ffffc00:
+        raise GspcError(-2, f"{cols} columns")
+    return (cols + 127) // 128 * 128
+
+
+def gspc_f8_scale_pitch(cols):
+    return gspc_f8_pitch(cols) and (cols + 511) // 512 * 4
+
+
+def _rows_f8(pair, rows, cols, what):
+    import torch
+    q, scale = pair
+    return (_flat(q, torch.float8_e4m3fn, rows * gspc_f8_pitch(cols), what),
+            _flat(scale, torch.uint8, rows * gspc_f8_scale_pitch(cols), what + " scales"))
+
+
+def _new_rows_f8(rows, cols, device):
+    import torch
+    return (_empty((rows, gspc_f8_pitch(cols)), torch.float8_e4m3fn, device), _empty((rows, gspc_f8_scale_pitch(cols)), torch.uint8, device))
+
+
+def gspc_quantize_rows_f8(x, out=None, out_t=None, which=None):
+    """x [..., cols] -> 8-bit float rows, pairs: along the rows (F8_ROWS, the default), along the columns (F8_COLUMNS: the rows of the transpose, `cols` of
+    them), or (rows, columns) in one pass (F8_BOTH).  out, out_t: pairs to write the rows and the columns form into, which say by themselves what is
+    written."""
+    if (out is not None or out_t is not None) and which is None and _fast is not None and _done(_fast.quantize_f8(x, out, out_t)):
+        return out if out_t is None else out_t if out is None else (out, out_t)
+    lib = load()
+    if which is None:
+        which = (F8_ROWS if out is not None or out_t is None else 0) | (F8_COLUMNS if out_t is not None else 0)
+    if which not in (F8_ROWS, F8_COLUMNS, F8_BOTH) or (out is not None and not which & F8_ROWS) or (out_t is not None and not which & F8_COLUMNS):
+        raise GspcError(-8, f"forms {which}, with out {'given' if out is not None else 'None'}, out_t {'given' if out_t is not None else 'None'}")
+    ld, cols = _row_stride(x, "x"), x.shape[-1]
+    if cols == 0:
+        raise GspcError(-2, "x has no columns")
+    rows = x.numel() // cols
+    if which & F8_COLUMNS and rows == 0:
+        raise GspcError(-2, "x has no rows, of which each column's form is made")
+    if which & F8_ROWS and out is None:
+        out = _new_rows_f8(rows, cols, x.device)
+    if which & F8_COLUMNS and out_t is None:
+        out_t = _new_rows_f8(cols, rows, x.device)
+    q, scale = _rows_f8(out, rows, cols, "out") if which & F8_ROWS else (None, None)
+    qt, scale_t = _rows_f8(out_t, cols, rows, "out_t") if which & F8_COLUMNS else (None, None)
+    _check(lib.gspc_quantize_rows_f8(x.data_ptr(), _dtype(x, "x"), ld, rows, cols, q, scale, qt, scale_t))
+    return out if which == F8_ROWS else out_t if which == F8_COLUMNS else (out, out_t)
+
+
+def gspc_dequantize_rows_f8(rows8, cols, out=None, dtype=GSPC_F32):
+    """8-bit float rows of `cols` values -> [rows, cols]; `out`: a tensor [..., cols] to write into."""
+    if out is not None and _fast is not None and _done(_fast.dequantize_f8(rows8, cols, out)):
+        return out
+    lib = load()
+    rows = rows8[1].numel() // gspc_f8_scale_pitch(cols)
+    q, scale = _rows_f8(rows8, rows, cols, "rows8")
+    if out is None:
+        out = _empty((rows, cols), _torch_dtype(dtype), rows8[0].device)
+    elif out.shape[-1] != cols or out.numel() != rows * cols:
+        raise GspcError(-2, f"out has shape {tuple(out.shape)}, expected {rows} rows of {cols}")
+    _check(lib.gspc_dequantize_rows_f8(q, scale, rows, cols, out.data_ptr(), _dtype(out, "out"), _row_stride(out, "out")))
+    return out
+
+
+def gspc_matmul_f8_workspace_bytes(M, N, K):
+    return int(load().gspc_matmul_f8_workspace_bytes(M, N, K))
+
+
+def gspc_matmul_f8(a, w, bias=None, out=None, dtype=GSPC_BF16, cols=None, workspace=None):
+    """8-bit float rows a (M tokens) and w (N filters) of the same length -> [M, N]; `out`: a tensor [..., N] to write into.  cols: that length,
+    checked against both; without it all of the rows' pitch is summed, whose padding is zero."""
+    if out is not None and _fast is not None:
+        rc = _fast.matmul_f8(a, w, bias, out, cols, workspace)
+        if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
+            need = gspc_matmul_f8_workspace_bytes(a[0].shape[0], w[0].shape[0], a[0].shape[-1])
+            rc = _fast.matmul_f8(a, w, bias, out, cols, _scratch(need, out.device))
+        if _done(rc):
+            return out
+    lib = load()
+    K = a[0].shape[-1]
+    if K == 0 or w[0].shape[-1] != K:
+        raise GspcError(-5, f"tokens of {K} values, filters of {w[0].shape[-1]}")
+    if K % 128 or (cols is not None and gspc_f8_pitch(cols) != K):
+        raise GspcError(-5, f"rows of {K if cols is None else cols} values have a pitch of {gspc_f8_pitch(K if cols is None else cols)}, these of {K}")
+    M, N = a[0].numel() // K, w[0].numel() // K
+    qa, sa = _rows_f8(a, M, K, "a")
+    qw, sw = _rows_f8(w, N, K, "w")
+    if out is None:
+        out = _empty((M, N), _torch_dtype(dtype), a[0].device)
+    elif out.shape[-1] != N or out.numel() != M * N:
+        raise GspcError(-2, f"out has shape {tuple(out.shape)}, expected {M} rows of {N}")
+    ws, ws_bytes, held = _workspace(workspace, workspace is None and M and N and gspc_matmul_f8_workspace_bytes(M, N, K), out.device)
+    _check(lib.gspc_matmul_f8(qa, sa, qw, sw, _flat(bias, _f32(), N, "bias"), M, N, K, out.data_ptr(), _dtype(out, "out"),
+                              _row_stride(out, "out"), ws, ws_bytes))
+    return out
+
+
+def _f32():
+    import torch
+    return torch.float32
+
+
+def _word(value, what):
+    if not isinstance(value, int) or not 0 <= value < 1 << 64:
+        raise GspcError(-8, f"{what}: a number of 64 bits is needed")
+    return value
+
+
+def _step(step):
+    import torch
+    return _flat(step, torch.int64, 1, "step")
+
+
+def gspc_dropout(x, drop, seed, offset=0, step=None, out=None):
+    """x [..., cols] with each value dropped (zero) with the probability `drop`, or kept and divided by 1 - drop; the same call on its gradient is the
+    gradient.  seed, offset: numbers of 64 bits, another offset for each call; step: an int64 tensor of one value that is added to the offset as the
+    kernel runs (for captured graphs); out: a tensor of x's shape and type to write into, or x itself."""
+    if out is not None and _fast is not None and _done(_fast.dropout(x, drop, seed, offset, step, out)):
+        return out
+    lib = load()
+    ld, cols = _row_stride(x, "x"), x.shape[-1]
+    if cols == 0:
+        raise GspcError(-2, "x has no columns")
+    if out is None:
+        out = _empty(x.shape, x.dtype, x.device)
+    _same_shape(out, x.shape, "out")
+    if out.dtype != x.dtype:
+        raise GspcError(-4, f"out is {out.dtype}, x {x.dtype}")
+    _check(lib.gspc_dropout(x.data_ptr(), _dtype(x, "x"), ld, x.numel() // cols, cols, drop, _word(seed, "seed"), _word(offset, "offset"), _step(step),
+                            out.data_ptr(), _row_stride(out, "out")))
+    return out
+
+
+def _residual(rows, cols, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, eps, drop, seed, offset, step):
+    f32 = _f32()
+    gates = 1
+    if gate is not None:
+        gates = gate.numel() // cols
+        if gate.shape[-1] != cols:
+            raise GspcError(-2, f"gate has shape {tuple(gate.shape)}, channels {cols}")
+    return GspcResidual(rows, gates, cols, post, pre, act, _flat(post_gamma, f32, cols, "post_gamma"), _flat(post_beta, f32, cols, "post_beta"),
+                        _flat(pre_gamma, f32, cols, "pre_gamma"), _flat(pre_beta, f32, cols, "pre_beta"), _flat(gate, f32, gates * cols, "gate"),
+                        scale, eps, drop, _word(seed, "seed"), _word(offset, "offset"), _step(step))
+
+
+def gspc_residual_norm(x, h=None, gate=None, post=NORM_NONE, post_gamma=None, post_beta=None, pre=NORM_NONE, pre_gamma=None, pre_beta=None,
+                       act=ACT_NONE, scale=1.0, eps=1e-5, drop=0.0, seed=0, offset=0, step=None, xo=None, out=None, dtype=None, stats=None):
+    """x, h [..., C] -> (x', z): x' = scale x + gate dropout(post(h)), z = act(pre(x')), both of x's shape.  post, pre: NORM_NONE, NORM_RMS or
+    NORM_LAYER over the channels, with fp32 parameters [C] or None; gate: fp32 [..., C], one for all tokens or for as many stretches of them as it has
+    rows; drop, seed, offset, step: as gspc_dropout.  x' is of x's type, `xo` a tensor to write it into, or x itself; without h and a scale it is x.
+    z is of type `dtype`, by default x's, or 8-bit float rows where that is GSPC_F8 or `out` is a pair; None without a norm.  stats: fp32
+    [tokens, 4] to write what the gradient needs to."""
+    if out is not None and (xo is not None or (h is None and scale == 1)) and _fast is not None and \
+            _done(_fast.residual_norm(x, h, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, eps, drop, seed, offset, step,
+                                      xo, out, stats)):
+        return x if xo is None else xo, out
+    lib = load()
+    ldx, C = _row_stride(x, "x"), x.shape[-1]
+    if C == 0:
+        raise GspcError(-2, "x has no channels")
+    rows = x.numel() // C
+    r = _residual(rows, C, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, eps, drop, seed, offset, step)
+    if h is not None:
+        _same_shape(h, x.shape, "h")
+    if xo is None and (h is not None or scale != 1):
+        xo = _empty(x.shape, x.dtype, x.device)
+    if xo is not None:
+        _same_shape(xo, x.shape, "xo")
+        if xo.dtype != x.dtype:
+            raise GspcError(-4, f"xo is {xo.dtype}, x {x.dtype}")
+    if out is None and pre != NORM_NONE:
+        out = _new_rows_f8(rows, C, x.device) if dtype == GSPC_F8 else _empty(x.shape, x.dtype if dtype is None else _torch_dtype(dtype), x.device)
+    z, kind, ldz, z_scale = None, GSPC_F32, 0, None
+    if isinstance(out, (tuple, list)):
+        (z, z_scale), kind = _rows_f8(out, rows, C, "out"), GSPC_F8
+    elif out is not None:
+        _same_shape(out, x.shape, "out")
+        z, kind, ldz = out.data_ptr(), _dtype(out, "out"), _row_stride(out, "out")
+    _check(lib.gspc_residual_norm(r, x.data_ptr(), _dtype(x, "x"), ldx, *_dense(h, "h"), *_dense(xo, "xo")[::2], z, kind, ldz, z_scale,
+                                  _flat(stats, _f32(), rows * 4, "stats")))
+    return x if xo is None else xo, out
+
+
+def _dense(t, what):
+    """(address, type, distance of rows), or none of them."""
+    return (None, GSPC_F32, 0) if t is None else (_on_gpu(t, what).data_ptr(), _dtype(t, what), _row_stride(t, what))
+
+
+ResidualGradients = collections.namedtuple("ResidualGradients", "dx dh dgate dpost_gamma dpost_beta dpre_gamma dpre_beta")
+
+
+def gspc_residual_norm_backward_workspace_bytes(rows, cols, gates=1):
+    return int(load().gspc_residual_norm_backward_workspace_bytes(rows, cols, gates))
+
+
+def gspc_residual_norm_backward(dz, dxo, xo, h, stats, gate=None, post=NORM_NONE, post_gamma=None, post_beta=None, pre=NORM_NONE, pre_gamma=None,
+                                pre_beta=None, act=ACT_NONE, scale=1.0, drop=0.0, seed=0, offset=0, step=None, dx=None, dh=None, dgate=None,
+                                dpost_gamma=None, dpost_beta=None, dpre_gamma=None, dpre_beta=None, workspace=None):
+    """The gradient of gspc_residual_norm: dz, dxo (either may be None for zero), xo, h and stats of the forward call, and its other arguments ->
+    ResidualGradients, None for what was not there.  dx is of xo's type and may be dxo itself, dh of h's and may be h itself."""
+    given = (dx, dh, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta)
+    if dx is not None and _fast is not None and all((g is None) == (v is None) for g, v in zip(
+            given[1:], (h, gate, post_gamma, post_beta, pre_gamma, pre_beta))):
+        call = lambda ws: _fast.residual_norm_backward(dz, dxo, xo, h, stats, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta,  # noqa: E731
+                                                       act, scale, drop, seed, offset, step, *given, ws)
+        rc = call(workspace)
+        if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
+            C = dx.shape[-1]
+            rc = call(_scratch(gspc_residual_norm_backward_workspace_bytes(dx.numel() // C, C, 1 if gate is None else gate.numel() // C), dx.device))
+        if _done(rc):
+            return ResidualGradients(*given)
+    lib = load()
+    like = xo if xo is not None else dxo
+    if like is None:
+        raise GspcError(-1, "neither xo nor dxo is given")
+    C, f32 = like.shape[-1], _f32()
+    if C == 0:
+        raise GspcError(-2, "xo has no channels")
+    rows = like.numel() // C
+    r = _residual(rows, C, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, 1.0, drop, seed, offset, step)
+    new = lambda t, of, kind=None: _empty(of.shape, kind or of.dtype, of.device) if t is None and of is not None else t  # noqa: E731
+    dx, dh, dgate = new(dx, like), new(dh, h), new(dgate, gate)
+    dpost_gamma, dpost_beta, dpre_gamma, dpre_beta = (new(*p) for p in ((dpost_gamma, post_gamma), (dpost_beta, post_beta), (dpre_gamma, pre_gamma),
+                                                                        (dpre_beta, pre_beta)))
+    for t, what, kind in ((dz, "dz", None), (dxo, "dxo", like.dtype), (dx, "dx", like.dtype), (h, "h", None), (dh, "dh", None if h is None else h.dtype)):
+        if t is not None:
+            _same_shape(t, like.shape, what)
+            if kind not in (None, t.dtype):
+                raise GspcError(-4, f"{what} is {t.dtype}, expected {kind}")
+    ws, ws_bytes, held = _workspace(workspace, workspace is None and gspc_residual_norm_backward_workspace_bytes(rows, C, r.gates), like.device)
+    _check(lib.gspc_residual_norm_backward(r, *_dense(dz, "dz"), *_dense(dxo, "dxo")[::2], *((None, _dtype(like, "dxo"), 0) if xo is None else _dense(xo, "xo")),
+                                           *_dense(h, "h"), _flat(stats, f32, rows * 4, "stats"), *_dense(dx, "dx")[::2], *_dense(dh, "dh")[::2],
+                                           _flat(dgate, f32, r.gates * C, "dgate"), _flat(dpost_gamma, f32, C, "dpost_gamma"),
+                                           _flat(dpost_beta, f32, C, "dpost_beta"), _flat(dpre_gamma, f32, C, "dpre_gamma"),
+                                           _flat(dpre_beta, f32, C, "dpre_beta"), ws, ws_bytes))
+    return ResidualGradients(dx, dh, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta)

@@ -171,14 +171,4 @@ template <int V> __device__ __forceinline__ void load_params(const float *__rest
     }
 }
 
-template <int V> __device__ __forceinline__ void activate_all(int act, float (&z)[V]) {
-    if (act == kActRelu) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) z[e] = activate<kActRelu>(z[e]);
-    } else if (act == kActSilu) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) z[e] = activate<kActSilu>(z[e]);
-    }
-}
-
 }  // namespace gspc

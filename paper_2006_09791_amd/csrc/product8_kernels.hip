@@ -1,37 +1,11 @@
 // out[m][n] = a_scale[m] w_scale[n] sum_k a[m][k] w[n][k] + bias[n], a and w 8-bit rows: integer sums on the matrix cores, exact.
-#include "tokens.h"
+#include "product_common.h"
 #include "tokens_internal.h"
 
 namespace gspc {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
-
-constexpr int kRsrc = 0x00020000;       // raw buffer descriptor: accesses past its end (kOob among them) read zero
-constexpr size_t kMostBytes = 1u << 30; // a block's rows are within that: at most 256 of 133152 bytes
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_at(const void *p, size_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)(bytes < kMostBytes ? bytes : kMostBytes), kRsrc);
-}
-
-// Waits until at most LEFT of the wave's loads are under way, and for all of its LDS operations.
-template <int LEFT> __device__ __forceinline__ void wait_loads() {
-    static_assert(LEFT < 64, "six bits");
-    __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
-}
-
-// Barriers around LDS that loads write directly and other lanes have written: nothing is to be moved across them.  (No fence: that
-// would wait for the loads that are to stay under way.)
-__device__ __forceinline__ void barrier_of_block() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ void barrier_of_wave() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");
-}
 
 struct ProductArgs {
     const int8_t *a, *w;
@@ -145,17 +119,6 @@ __global__ __launch_bounds__(64 * WAVES) void product8_small_kernel(ProductArgs 
     }
 }
 
-// Workgroups go to the eight XCDs in turn.  Each XCD gets consecutive tiles, and these run through bands of kBand tiles of tokens,
-// so that the 32 tiles that an XCD works on together share rows of both operands in its L2.
-constexpr unsigned kBand = 8;
-__device__ __forceinline__ uint2 tile_of(const ProductArgs &p, unsigned b) {
-    const unsigned tiles = p.mtiles * p.ntiles, each = tiles / 8, more = tiles % 8, xcd = b & 7;
-    const unsigned t = xcd * each + min(xcd, more) + (b >> 3);
-    const unsigned band = t / (kBand * p.ntiles), first = band * kBand, high = min(kBand, p.mtiles - first);
-    const unsigned in = t - band * kBand * p.ntiles;
-    return make_uint2(first + in % high, in / high);
-}
-
 // ---- many tokens: tiles through LDS ---------------------------------------------------------------------------------------------
 constexpr int kStep = 128;              // bytes of a row that one stage holds: a cache line (stages of 64 bytes, twice as many of
                                         // them, make two requests of a line: 8192 x 4096 x 8192 took 285 us)
@@ -174,7 +137,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product8_tile_kernel(ProductArgs
     static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "a load is of one operand");
     __shared__ __attribute__((aligned(16))) char stages[STAGES * STAGE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const uint2 tile = tile_of(p, blockIdx.x);
+    const uint2 tile = tile_of(p.mtiles, p.ntiles, blockIdx.x);
     const size_t m0 = (size_t)tile.x * BM;
     const int n0 = tile.y * BN;
     const __amdgpu_buffer_rsrc_t ra = bytes_at(p.a + m0 * p.pitch, (p.M - m0) * p.pitch);

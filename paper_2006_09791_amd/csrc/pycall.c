@@ -90,7 +90,8 @@ static struct {
     norm_backward_fn norm_backward;
     matmul_fn matmul;
 } g_calls;
-static PyObject *g_types[3];               /* torch.float32, bfloat16, int8, in the order of the library's numbers */
+static PyObject *g_types[6];               /* torch.float32, bfloat16, int8, float8_e4m3fn, in the order of the library's numbers; uint8, int64 */
+enum { F32, BF16, I8, F8, U8, I64, TYPES };
 static PyObject *s_is_cuda, *s_dtype, *s_shape, *s_is_contiguous;
 
 static PyObject *bind_tokens(PyObject *self, PyObject *const *a, Py_ssize_t n) {
@@ -130,14 +131,14 @@ static int is_true(PyObject *v) {
     return yes;
 }
 
-/* A contiguous tensor on the GPU of one of the three types.  0: not one (no exception is left). */
-static int tensor(PyObject *t, tensor_t *o) {
+/* A contiguous tensor on the GPU of one of the types.  0: not one (no exception is left). */
+static int tensor_of_any(PyObject *t, tensor_t *o) {
     if (!is_true(PyObject_GetAttr(t, s_is_cuda))) goto no;
     PyObject *v = PyObject_GetAttr(t, s_dtype);
     if (!v) goto no;
-    for (o->type = 0; o->type < 3 && v != g_types[o->type]; ++o->type) {}
+    for (o->type = 0; o->type < TYPES && v != g_types[o->type]; ++o->type) {}
     Py_DECREF(v);
-    if (o->type == 3 || !is_true(PyObject_CallMethodNoArgs(t, s_is_contiguous))) goto no;
+    if (o->type == TYPES || !is_true(PyObject_CallMethodNoArgs(t, s_is_contiguous))) goto no;
     v = PyObject_GetAttr(t, s_shape);
     if (!v || !PyTuple_Check(v)) {
         Py_XDECREF(v);
@@ -158,12 +159,14 @@ no:
     PyErr_Clear();
     return 0;
 }
+/* One of the first three. */
+static int tensor(PyObject *t, tensor_t *o) { return tensor_of_any(t, o) && o->type <= I8; }
 /* One of a type and of a number of elements, or NULL where none is allowed. */
 static int vector(PyObject *t, int type, int64_t count, int none, void **ptr) {
     tensor_t o;
     *ptr = NULL;
     if (t == Py_None) return none;
-    if (!tensor(t, &o) || o.type != type || o.count != count) return 0;
+    if (!tensor_of_any(t, &o) || o.type != type || o.count != count) return 0;
     *ptr = o.ptr;
     return 1;
 }
@@ -232,7 +235,7 @@ static PyObject *dequantize(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     CALL(g_calls.dequantize(q, scale, x.count / cols, cols, x.ptr, x.type, cols));
 }
 
-static size_t bytes_of(const tensor_t *t) { return t->ptr ? (size_t)t->count * (t->type == 0 ? 4 : t->type == 1 ? 2 : 1) : 0; }
+static size_t bytes_of(const tensor_t *t) { return t->ptr ? (size_t)t->count * (t->type == I64 ? 8 : t->type == F32 ? 4 : t->type == BF16 ? 2 : 1) : 0; }
 
 /* Whether two tensors of up to four dimensions (more: no) have the same shape. */
 static int same_shape(const tensor_t *a, const tensor_t *b) {
@@ -304,11 +307,201 @@ static PyObject *matmul(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     CALL(g_calls.matmul(x.ptr, sa, w.ptr, sw, bias, x.first, (int)w.first, cols ? cols : (int)x.last, out.ptr, out.type, w.first));
 }
 
+/* ---- a residual block on tokens: the same ---------------------------------------------------------------------------- */
+typedef struct {
+    int64_t rows, gates;
+    int cols, post, pre, act;
+    void *post_gamma, *post_beta, *pre_gamma, *pre_beta, *gate;
+    float scale, eps;
+    double drop;
+    uint64_t seed, offset;
+    void *step;
+} residual_t;                       /* gspc_residual_t */
+typedef int (*quantize_f8_fn)(const void *, int, int64_t, int64_t, int, void *, void *, void *, void *);
+typedef int (*dequantize_f8_fn)(const void *, const void *, int64_t, int, void *, int, int64_t);
+typedef int (*matmul_f8_fn)(const void *, const void *, const void *, const void *, const void *, int64_t, int, int, void *, int, int64_t, void *, size_t);
+typedef int (*dropout_fn)(const void *, int, int64_t, int64_t, int, double, uint64_t, uint64_t, const void *, void *, int64_t);
+typedef int (*residual_norm_fn)(const residual_t *, const void *, int, int64_t, const void *, int, int64_t, void *, int64_t, void *, int, int64_t, void *, void *);
+typedef int (*residual_norm_backward_fn)(const residual_t *, const void *, int, int64_t, const void *, int64_t, const void *, int, int64_t, const void *, int,
+                                         int64_t, const void *, void *, int64_t, void *, int64_t, void *, void *, void *, void *, void *, void *, size_t);
+static struct {
+    quantize_f8_fn quantize;
+    dequantize_f8_fn dequantize;
+    matmul_f8_fn matmul;
+    dropout_fn dropout;
+    residual_norm_fn residual_norm;
+    residual_norm_backward_fn residual_norm_backward;
+} g_block;
+
+static PyObject *bind_block(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    if (n != 9) {
+        PyErr_SetString(PyExc_TypeError, "six addresses and three types");
+        return NULL;
+    }
+    void *p[6];
+    for (int i = 0; i < 6; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i] && PyErr_Occurred()) return NULL;
+    }
+    g_block.quantize = (quantize_f8_fn)p[0];
+    g_block.dequantize = (dequantize_f8_fn)p[1];
+    g_block.matmul = (matmul_f8_fn)p[2];
+    g_block.dropout = (dropout_fn)p[3];
+    g_block.residual_norm = (residual_norm_fn)p[4];
+    g_block.residual_norm_backward = (residual_norm_backward_fn)p[5];
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(a[6 + i]);
+        g_types[F8 + i] = a[6 + i];
+    }
+    Py_RETURN_NONE;
+}
+
+/* 8-bit float rows: a pair of e4m3 [rows * pitch] and uint8 [rows * scale pitch]. */
+static int rows_f8(PyObject *t, int64_t rows, int64_t cols, void **q, void **scale) {
+    return PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 2 && vector(PyTuple_GET_ITEM(t, 0), F8, rows * ((cols + 127) / 128 * 128), 0, q) &&
+           vector(PyTuple_GET_ITEM(t, 1), U8, rows * ((cols + 511) / 512 * 4), 0, scale);
+}
+static int word(PyObject *v, uint64_t *out) {
+    if (!PyLong_CheckExact(v)) return 0;
+    *out = PyLong_AsUnsignedLongLong(v);
+    return !PyErr_Occurred();
+}
+static int real(PyObject *v, double *out) {
+    if (!PyFloat_CheckExact(v)) return 0;
+    *out = PyFloat_AS_DOUBLE(v);
+    return 1;
+}
+static int is_dense(PyObject *t, tensor_t *o) { return tensor_of_any(t, o) && o->type <= BF16; }
+static int fits_f8(int64_t v) { return v > 0 && v <= 0x7ffffc00; }
+
+/* quantize_f8(x [..., cols], (q, scale) or None, (qt, scale_t) or None) */
+static PyObject *quantize_f8(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    tensor_t x;
+    void *q = NULL, *scale = NULL, *qt = NULL, *scale_t = NULL;
+    if (n != 3 || !g_block.quantize || !is_dense(a[0], &x) || !fits_f8(x.last) || !fits_f8(x.count / x.last)) GENERAL;
+    const int64_t rows = x.count / x.last;
+    if ((a[1] != Py_None && !rows_f8(a[1], rows, x.last, &q, &scale)) || (a[2] != Py_None && !rows_f8(a[2], x.last, rows, &qt, &scale_t))) GENERAL;
+    CALL(g_block.quantize(x.ptr, x.type, x.last, rows, (int)x.last, q, scale, qt, scale_t));
+}
+
+/* dequantize_f8((q, scale), cols, out [..., cols]) */
+static PyObject *dequantize_f8(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    tensor_t x;
+    void *q, *scale;
+    int cols;
+    if (n != 3 || !g_block.dequantize || !small(a[1], &cols) || !is_dense(a[2], &x) || !fits_f8(cols) || x.last != cols ||
+        !rows_f8(a[0], x.count / cols, cols, &q, &scale))
+        GENERAL;
+    CALL(g_block.dequantize(q, scale, x.count / cols, cols, x.ptr, x.type, cols));
+}
+
+/* matmul_f8((q, scale), (q, scale), bias, out [..., N], cols or None: all of the pitch, workspace) */
+static PyObject *matmul_f8(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    tensor_t x, w, out, ws = {0};
+    void *sa, *sw, *bias;
+    int cols = 0;
+    if (n != 6 || (a[4] != Py_None && (!small(a[4], &cols) || cols <= 0)) || !g_block.matmul || !PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 2 ||
+        !PyTuple_CheckExact(a[1]) || PyTuple_GET_SIZE(a[1]) != 2 || !tensor_of_any(PyTuple_GET_ITEM(a[0], 0), &x) ||
+        !tensor_of_any(PyTuple_GET_ITEM(a[1], 0), &w) || x.type != F8 || w.type != F8 || x.dims != 2 || w.dims != 2 || x.last != w.last || x.last % 128 ||
+        !fits_f8(x.last) || (cols && (cols + (int64_t)127) / 128 * 128 != x.last) || !fits(w.first) ||
+        !vector(PyTuple_GET_ITEM(a[0], 1), U8, x.first * ((x.last + 511) / 512 * 4), 0, &sa) ||
+        !vector(PyTuple_GET_ITEM(a[1], 1), U8, w.first * ((x.last + 511) / 512 * 4), 0, &sw) || !vector(a[2], F32, w.first, 1, &bias) ||
+        !is_dense(a[3], &out) || out.last != w.first || out.count != x.first * w.first || (a[5] != Py_None && !tensor_of_any(a[5], &ws)))
+        GENERAL;
+    CALL(g_block.matmul(x.ptr, sa, w.ptr, sw, bias, x.first, (int)w.first, (int)x.last, out.ptr, out.type, w.first, ws.ptr, bytes_of(&ws)));
+}
+
+/* dropout(x [..., cols], drop, seed, offset, step, out) */
+static PyObject *dropout(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    tensor_t x, out;
+    double drop;
+    uint64_t seed, offset;
+    void *step;
+    if (n != 6 || !g_block.dropout || !is_dense(a[0], &x) || !real(a[1], &drop) || !word(a[2], &seed) || !word(a[3], &offset) ||
+        !vector(a[4], I64, 1, 1, &step) || !is_dense(a[5], &out) || out.type != x.type || !same_shape(&out, &x) || !fits(x.last))
+        GENERAL;
+    CALL(g_block.dropout(x.ptr, x.type, x.last, x.count / x.last, (int)x.last, drop, seed, offset, step, out.ptr, x.last));
+}
+
+/* What the forward call and the gradient have in common: gate, post, its parameters, pre, its parameters, act, scale; then drop, seed, offset, step. */
+static int residual(PyObject *const *a, PyObject *const *b, int64_t rows, int64_t cols, residual_t *r) {
+    double scale;
+    tensor_t gate;
+    r->rows = rows;
+    r->cols = (int)cols;
+    r->gates = 1;
+    r->gate = NULL;
+    if (a[0] != Py_None) {
+        if (!tensor_of_any(a[0], &gate) || gate.type != F32 || gate.last != cols) return 0;
+        r->gate = gate.ptr;
+        r->gates = gate.count / cols;
+    }
+    if (!small(a[1], &r->post) || !vector(a[2], F32, cols, 1, &r->post_gamma) || !vector(a[3], F32, cols, 1, &r->post_beta) || !small(a[4], &r->pre) ||
+        !vector(a[5], F32, cols, 1, &r->pre_gamma) || !vector(a[6], F32, cols, 1, &r->pre_beta) || !small(a[7], &r->act) || !real(a[8], &scale) ||
+        !real(b[0], &r->drop) || !word(b[1], &r->seed) || !word(b[2], &r->offset) || !vector(b[3], I64, 1, 1, &r->step))
+        return 0;
+    r->scale = (float)scale;
+    return 1;
+}
+/* A dense tensor of a type (-1: of either) and of the shape of another, or none. */
+static int alike(PyObject *t, const tensor_t *of, int type, tensor_t *o) {
+    o->ptr = NULL;
+    o->type = F32;
+    return t == Py_None || (is_dense(t, o) && (type < 0 || o->type == type) && same_shape(o, of));
+}
+
+/* residual_norm(x, h, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, eps, drop, seed, offset, step, xo, out, stats) */
+static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    tensor_t x, h, xo, z = {0};
+    residual_t r;
+    double eps;
+    void *stats, *z_scale = NULL;
+    if (n != 19 || !g_block.residual_norm || !is_dense(a[0], &x) || x.last <= 0 || x.last > 8192 || !alike(a[1], &x, -1, &h) || !real(a[11], &eps) ||
+        !alike(a[16], &x, x.type, &xo))
+        GENERAL;
+    const int64_t rows = x.count / x.last;
+    if (!residual(a + 2, a + 12, rows, x.last, &r) || !vector(a[18], F32, rows * 4, 1, &stats)) GENERAL;
+    if (PyTuple_CheckExact(a[17])) {
+        if (!rows_f8(a[17], rows, x.last, &z.ptr, &z_scale)) GENERAL;
+        z.type = F8;
+    } else if (a[17] == Py_None || !alike(a[17], &x, -1, &z))
+        GENERAL;
+    r.eps = (float)eps;
+    CALL(g_block.residual_norm(&r, x.ptr, x.type, x.last, h.ptr, h.type, x.last, xo.ptr, x.last, z.ptr, z.type, x.last, z_scale, stats));
+}
+
+/* residual_norm_backward(dz, dxo, xo, h, stats, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, drop, seed, offset, step, dx, dh,
+ * dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta, workspace) */
+static PyObject *residual_norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    tensor_t dz, dxo, xo, h, dx, dh, ws = {0};
+    residual_t r;
+    void *stats, *g[5];
+    if (n != 26 || !g_block.residual_norm_backward || !is_dense(a[18], &dx) || dx.last <= 0 || dx.last > 8192 || !alike(a[0], &dx, -1, &dz) ||
+        !alike(a[1], &dx, dx.type, &dxo) || !alike(a[2], &dx, dx.type, &xo) || !alike(a[3], &dx, -1, &h) || !alike(a[19], &dx, h.type, &dh) ||
+        (a[25] != Py_None && !tensor_of_any(a[25], &ws)))
+        GENERAL;
+    const int64_t rows = dx.count / dx.last, cols = dx.last;
+    if (!residual(a + 5, a + 14, rows, cols, &r) || !vector(a[4], F32, rows * 4, 0, &stats) || !vector(a[20], F32, r.gates * cols, 1, &g[0])) GENERAL;
+    for (int i = 1; i < 5; ++i)
+        if (!vector(a[20 + i], F32, cols, 1, &g[i])) GENERAL;
+    r.eps = 1.f;
+    CALL(g_block.residual_norm_backward(&r, dz.ptr, dz.type, cols, dxo.ptr, cols, xo.ptr, dx.type, cols, h.ptr, h.type, cols, stats, dx.ptr, cols, dh.ptr,
+                                        cols, g[0], g[1], g[2], g[3], g[4], ws.ptr, bytes_of(&ws)));
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {
     {"bind", bind, METH_O, "bind(address of gspc_conv2d_grouped)"},
     {"conv", (PyCFunction)(void (*)(void))conv, METH_FASTCALL, "one grouped convolution"},
     FAST(bind_tokens), FAST(pack), FAST(unpack), FAST(quantize), FAST(dequantize), FAST(norm), FAST(norm_backward), FAST(matmul),
+    FAST(bind_block), FAST(quantize_f8), FAST(dequantize_f8), FAST(matmul_f8), FAST(dropout), FAST(residual_norm), FAST(residual_norm_backward),
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gspc_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -1,0 +1,274 @@
+// Gradient of a block's residual norms.  With hh and xh the normalised h and x', w what dropout multiplies by, u = g1 hh + b1, v = g2 xh + b2:
+//   dv = dz act'(v), t = g2 dv, dX = dx' + r2 (t - mean t - xh mean(t xh)), dx = scale dX,
+//   q = g1 gate w dX, dh = r1 (q - mean q - hh mean(q hh))                     (no mean t, mean q behind a root mean square)
+// and over tokens, with A = sum w dX hh and B = sum w dX of the tokens that share a gate: dg1 = gate A, db1 = gate B, dgate = g1 A + b1 B (two sums
+// serve the three), dg2 = sum dv xh, db2 = sum dv.
+#include "residual_common.h"
+
+namespace gspc {
+
+constexpr int kSums = 5;        // dg1, db1, dg2, db2, dgate
+
+struct GradPlan {
+    unsigned chunks;            // blocks that share a gate's tokens, or 0: a team takes whole gates
+    unsigned rows;              // tokens of such a block, or of a team
+    unsigned each;              // tokens of a team
+    unsigned blocks;
+};
+
+// A team walks down its tokens and keeps the sums of its columns; a block's teams add theirs up and leave one part.  Bound by memory where there are
+// many tokens: dz, dx', x' and h in, dx and dh out.  GATES: a team's tokens have several gates, whose gradients it writes itself.
+template <typename TX, typename TH, bool GATES>
+__global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, ResidualBackward f, GradPlan g, int team, unsigned m_chunks,
+                                                                 float *__restrict__ parts) {
+    __shared__ float2 s_place[2][kMaxTeam / kWave];
+    __shared__ float s_sum[kTeamThreads * 8];              // (of several teams)
+    TeamSums sums{s_place, 0};
+    const int lane = threadIdx.x & (team - 1), at = lane * 8, n = max(0, min(8, a.cols - at));
+    const unsigned teams = blockDim.x / team, mine = threadIdx.x / team;
+    unsigned first, last, gate_row = 0;
+    if constexpr (GATES) {
+        first = (blockIdx.x * teams + mine) * g.each;
+        last = min(first + g.each, a.rows);
+        gate_row = first / a.gate_rows;
+    } else {
+        const unsigned group = fast_div_any(blockIdx.x, g.chunks, m_chunks), chunk = blockIdx.x - group * g.chunks;
+        const unsigned end = min(chunk * g.rows + g.rows, a.gate_rows);
+        first = group * a.gate_rows + min(chunk * g.rows + mine * g.each, end);
+        last = min(first + g.each, group * a.gate_rows + end);
+        gate_row = group;
+    }
+    const float inv = 1.f / (float)a.cols;
+    const bool centre1 = a.post == kNormLayer, centre2 = a.pre == kNormLayer;
+    const uint64_t call = a.drop.offset + (a.drop.step ? *a.drop.step : 0);
+    float g2[8], b2[8], gg[8];                                  // gg: g1 gate
+    some_params(a.pre_gamma, at, n, 1.f, g2);
+    some_params(a.pre_beta, at, n, 0.f, b2);
+    const auto new_gate = [&] {
+        float gate[8];
+        some_params(a.post_gamma, at, n, 1.f, gg);
+        if (a.gate) {
+            some_params(a.gate + (size_t)gate_row * a.cols, at, n, 1.f, gate);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) gg[e] *= gate[e];
+        }
+    };
+    if (!GATES || first < last) new_gate();
+    float sa[8] = {}, sb[8] = {}, sg2[8] = {}, sb2[8] = {}, sg1[GATES ? 8 : 1] = {}, sb1[GATES ? 8 : 1] = {};
+    // A gate's tokens are through: its gradient, and what its sums are to the parameters'.
+    const auto end_gate = [&](float (&dgate)[8], float (&dg1)[8], float (&db1)[8]) {
+        float gate[8], g1[8], b1[8];
+        some_params(a.gate ? a.gate + (size_t)gate_row * a.cols : nullptr, at, n, 1.f, gate);
+        some_params(a.post_gamma, at, n, 1.f, g1);
+        some_params(a.post_beta, at, n, 0.f, b1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            dgate[e] = fmaf(g1[e], sa[e], b1[e] * sb[e]);
+            dg1[e] = gate[e] * sa[e];
+            db1[e] = gate[e] * sb[e];
+        }
+    };
+    unsigned left = a.gate_rows;                                // tokens of this gate to come (GATES)
+    for (unsigned k = 0; k < g.each; ++k) {                     // as often in every team: there are barriers
+        const unsigned row = first + k;
+        const bool there = row < last;
+        const int some = there ? n : 0;
+        const size_t at_row = there ? row : 0;
+        float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
+        if (there) st = *reinterpret_cast<const float4 *>(f.stats + at_row * 4);
+        float dv[8] = {}, d[8] = {}, xh[8], hh[8];
+        if (f.dz) {
+            if (f.dz_dtype == GSPC_F32) widen(fetch_some(static_cast<const float *>(f.dz) + at_row * f.lddz + at, some), dv);
+            else widen(fetch_some(static_cast<const uint16_t *>(f.dz) + at_row * f.lddz + at, some), dv);
+            widen(fetch_some(static_cast<const TX *>(f.xo) + at_row * f.ldxo + at, some), xh);
+        }
+        if (f.dxo) widen(fetch_some(static_cast<const TX *>(f.dxo) + at_row * f.lddxo + at, some), d);
+        if (f.h) widen(fetch_some(static_cast<const TH *>(f.h) + at_row * f.ldh + at, some), hh);
+        if (f.dz) {
+            float2 s = make_float2(0.f, 0.f);
+            float t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) xh[e] = e < some ? (xh[e] - st.z) * st.w : 0.f;
+            if (a.act != kActNone) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = fmaf(xh[e], g2[e], b2[e]);
+                    dv[e] *= a.act == kActRelu ? slope<kActRelu>(v) : slope<kActSilu>(v);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sg2[e] = fmaf(dv[e], xh[e], sg2[e]);
+                sb2[e] += dv[e];
+                t[e] = g2[e] * dv[e];
+                s.x += t[e];
+                s.y = fmaf(t[e], xh[e], s.y);
+            }
+            s = team_sum(s, team, sums);
+            const float m = centre2 ? s.x * inv : 0.f, c = s.y * inv;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = fmaf(st.w, t[e] - m - xh[e] * c, d[e]);
+        }
+        if (there) {
+            float out[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] = a.scale * d[e];
+            store_some(static_cast<TX *>(f.dx) + at_row * f.lddx + at, out, n, f.past);
+        }
+        if (f.h) {
+            if (a.drop.limit) {
+                float w[8];
+                dropout_factors(a.drop, call, row, lane, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = w[e] != 0.f ? d[e] * w[e] : 0.f;
+            }
+            float2 s = make_float2(0.f, 0.f);
+            float q[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                d[e] = e < some ? d[e] : 0.f;
+                hh[e] = e < some ? (hh[e] - st.x) * st.y : 0.f;
+                sa[e] = fmaf(d[e], hh[e], sa[e]);
+                sb[e] += d[e];
+                q[e] = gg[e] * d[e];
+                s.x += q[e];
+                s.y = fmaf(q[e], hh[e], s.y);
+            }
+            if (a.post != kNormNone) {
+                s = team_sum(s, team, sums);
+                const float m = centre1 ? s.x * inv : 0.f, c = s.y * inv;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[e] = st.y * (q[e] - m - hh[e] * c);
+            }
+            if (there) store_some(static_cast<TH *>(f.dh) + at_row * f.lddh + at, q, n, f.past);
+        }
+        if constexpr (GATES) {
+            if (--left == 0) {
+                if (there) {
+                    float dgate[8], dg1[8], db1[8];
+                    end_gate(dgate, dg1, db1);
+                    if (f.dgate) store_some(f.dgate + (size_t)gate_row * a.cols + at, dgate, n);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sg1[e] += dg1[e], sb1[e] += db1[e], sa[e] = sb[e] = 0.f;
+                    ++gate_row;
+                    if (row + 1 < last) new_gate();
+                }
+                left = a.gate_rows;
+            }
+        }
+    }
+    float dgate[8], dg1[8], db1[8];
+    if constexpr (GATES) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dg1[e] = sg1[e], db1[e] = sb1[e];
+    } else
+        end_gate(dgate, dg1, db1);
+    // The teams' sums as one part of the block, a kind at a time.
+    const auto leave = [&](const float (&v)[8], float *to) {
+        if (teams == 1) {
+            store_some(to + at, v, n);
+            return;
+        }
+        __syncthreads();
+        store(s_sum + mine * team * 8 + at, v);
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+            float sum = s_sum[c];
+            for (unsigned k = 1; k < teams; ++k) sum += s_sum[k * team * 8 + c];
+            to[c] = sum;
+        }
+    };
+    float *part = parts + (size_t)blockIdx.x * kSums * a.cols;
+    if (f.dpost_gamma) leave(dg1, part);
+    if (f.dpost_beta) leave(db1, part + a.cols);
+    if (f.dpre_gamma) leave(sg2, part + 2 * a.cols);
+    if (f.dpre_beta) leave(sb2, part + 3 * a.cols);
+    if (!GATES && f.dgate) leave(dgate, g.chunks == 1 ? f.dgate + (size_t)gate_row * a.cols : part + 4 * a.cols);
+}
+
+// Adds up the blocks' parts, in 64 bits: 64 columns a block, sixteen stretches of the parts side by side.  Block (kind, columns): the four parameters'
+// over all parts, then each gate's over those of its own blocks.
+__global__ __launch_bounds__(1024) void residual_join_kernel(const float *__restrict__ parts, unsigned blocks, unsigned chunks, int cols, unsigned slabs,
+                                                             float *dg1, float *db1, float *dg2, float *db2, float *dgate) {
+    __shared__ double s_sum[16][kWave];
+    const unsigned kind = blockIdx.x / slabs, slab = blockIdx.x - kind * slabs, gate = kind - 4;
+    const int lane = threadIdx.x % kWave, slice = threadIdx.x / kWave, c = slab * kWave + lane;
+    float *to = kind == 0 ? dg1 : kind == 1 ? db1 : kind == 2 ? dg2 : kind == 3 ? db2 : dgate + (size_t)gate * cols;
+    if (kind < 4 && !to) return;
+    const unsigned first = kind < 4 ? 0 : gate * chunks, count = kind < 4 ? blocks : chunks;
+    const float *p = parts + ((size_t)first * kSums + min(kind, 4u)) * cols + min(c, cols - 1);
+    double sum = 0;
+#pragma unroll 4
+    for (unsigned k = slice; k < count; k += 16) sum += p[(size_t)k * kSums * cols];
+    s_sum[slice][lane] = sum;
+    __syncthreads();
+    if (slice != 0 || c >= cols) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) sum += s_sum[k][lane];
+    to[c] = (float)sum;
+}
+
+__global__ __launch_bounds__(256) void residual_clear_kernel(float *p, size_t count) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) p[i] = 0.f;
+}
+
+static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
+    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 1024;
+    GradPlan p;
+    if (gates > 1 && gates >= wanted * t.teams) {       // whole gates for each team
+        const unsigned of_team = (gates - 1) / (wanted * t.teams) + 1, most = gate_rows < 1024 ? 1024 / gate_rows : 1;
+        p.chunks = 0;
+        p.each = p.rows = (of_team < most ? of_team : most) * gate_rows;
+        p.blocks = (unsigned)(((size_t)rows - 1) / ((size_t)p.each * t.teams) + 1);
+        return p;
+    }
+    // blocks of a gate: until there are enough of them, of two tokens a team at least, and 1024 at most
+    const unsigned most = (gate_rows - 1) / (2 * t.teams) + 1, least = (gate_rows - 1) / (1024 * t.teams) + 1;
+    unsigned want = wanted / gates;
+    if (want > most) want = most;
+    if (want < least) want = least;
+    p.rows = (gate_rows - 1) / want + 1;
+    p.chunks = (gate_rows - 1) / p.rows + 1;
+    p.each = (p.rows - 1) / t.teams + 1;
+    p.blocks = gates * p.chunks;
+    return p;
+}
+
+size_t residual_grad_bytes(const Residual &a) {
+    return a.rows ? (size_t)plan_grad(a, team_grid(a.cols, 8)).blocks * kSums * a.cols * sizeof(float) : 0;
+}
+
+hipError_t launch_residual_grad(const Residual &a, ResidualBackward f, void *ws, hipStream_t s) {
+    if (a.rows == 0) {          // no tokens: the parameters' gradients are zero
+        const auto clear = [&](float *p, size_t count) {
+            const size_t blocks = (count + 255) / 256;
+            if (p) hipLaunchKernelGGL(residual_clear_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, p, count);
+        };
+        for (float *p : {f.dpost_gamma, f.dpost_beta, f.dpre_gamma, f.dpre_beta}) clear(p, a.cols);
+        clear(f.dgate, (size_t)a.gates * a.cols);
+        return hipGetLastError();
+    }
+    const TeamGrid g = team_grid(a.cols, 8);
+    const GradPlan p = plan_grad(a, g);
+    float *parts = static_cast<float *>(ws);
+    f.past = (size_t)a.rows * a.cols * 2 >= kPastCaches && (f.x_dtype == GSPC_F32 || whole_pieces(f.dx, a.cols * 2, f.lddx * 2)) &&
+             (!f.h || f.h_dtype == GSPC_F32 || whole_pieces(f.dh, a.cols * 2, f.lddh * 2));
+    const auto run = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(p.blocks), dim3(g.threads), 0, s, a, f, p, g.team, div_magic(p.chunks ? p.chunks : 1), parts);
+    };
+    const bool x32 = f.x_dtype == GSPC_F32, h32 = f.h_dtype == GSPC_F32;
+    if (p.chunks) {
+        if (x32) h32 ? run(residual_grad_kernel<float, float, false>) : run(residual_grad_kernel<float, uint16_t, false>);
+        else h32 ? run(residual_grad_kernel<uint16_t, float, false>) : run(residual_grad_kernel<uint16_t, uint16_t, false>);
+    } else {
+        if (x32) h32 ? run(residual_grad_kernel<float, float, true>) : run(residual_grad_kernel<float, uint16_t, true>);
+        else h32 ? run(residual_grad_kernel<uint16_t, float, true>) : run(residual_grad_kernel<uint16_t, uint16_t, true>);
+    }
+    const unsigned slabs = (a.cols + kWave - 1) / kWave, kinds = 4 + (f.dgate && p.chunks > 1 ? a.gates : 0);
+    if (kinds > 4 || f.dpost_gamma || f.dpost_beta || f.dpre_gamma || f.dpre_beta)
+        hipLaunchKernelGGL(residual_join_kernel, dim3(kinds * slabs), dim3(1024), 0, s, parts, p.blocks, p.chunks, a.cols, slabs, f.dpost_gamma,
+                           f.dpost_beta, f.dpre_gamma, f.dpre_beta, f.dgate);
+    return hipGetLastError();
+}
+
+}  // namespace gspc

@@ -224,5 +224,14 @@ template <int ACT> __device__ __forceinline__ float slope(float z) {
     }
     return 1.f;
 }
+template <int V> __device__ __forceinline__ void activate_all(int act, float (&z)[V]) {
+    if (act == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = activate<kActRelu>(z[e]);
+    } else if (act == kActSilu) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = activate<kActSilu>(z[e]);
+    }
+}
 
 }  // namespace gspc

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "gspc_internal.h"
+#include "philox.h"
 
 namespace gspc {
 
@@ -69,5 +70,78 @@ struct ProductI8 {
     int N, K, out_dtype;
 };
 hipError_t launch_matmul_i8(const ProductI8 &p, hipStream_t s, const char **name);
+
+// 8-bit float rows: along the rows (q, scale), along the columns (qt, scale_t), or both
+struct QuantizeF8 {
+    const void *x;
+    int dtype;
+    size_t ldx, rows;
+    int cols;
+    uint8_t *q, *scale, *qt, *scale_t;
+};
+hipError_t launch_quantize_f8(const QuantizeF8 &a, hipStream_t s);
+hipError_t launch_dequantize_f8(const uint8_t *q, const uint8_t *scale, size_t rows, int cols, void *x, int dtype, size_t ldx, hipStream_t s);
+
+// out[m][n] = sum_k a[m][k] w[n][k] + bias[n], both 8-bit float rows
+struct ProductF8 {
+    const uint8_t *a, *a_scale, *w, *w_scale;
+    const float *bias;
+    void *out;
+    size_t M, ldo;
+    int N, K, out_dtype;
+};
+size_t matmul_f8_bytes(size_t M, int N, int K);
+hipError_t launch_matmul_f8(const ProductF8 &p, void *ws, hipStream_t s, const char **name);
+
+hipError_t launch_dropout(const Dropout &d, const void *x, int dtype, size_t ldx, size_t rows, int cols, void *y, size_t ldy, hipStream_t s);
+
+// A block's residual norms: x' = scale x + gate drop(post(h)), z = act(pre(x')).  Rows of the tensors are tokens.
+enum { kNormNone = 0, kNormRms = 1, kNormLayer = 2 };
+struct Residual {
+    unsigned rows, gates, gate_rows;        // gate_rows: tokens of each of `gates` gates
+    int cols, post, pre, act;
+    const float *post_gamma, *post_beta, *pre_gamma, *pre_beta, *gate;      // nullptr: 1, 0, 1, 0, 1
+    float scale, eps;
+    Dropout drop;
+};
+struct ResidualForward {
+    const void *x;
+    int x_dtype;                    // of xo too
+    size_t ldx;
+    const void *h;                  // or nullptr: x' = scale x
+    int h_dtype;
+    size_t ldh;
+    void *xo;                       // or nullptr
+    size_t ldxo;
+    void *z;                        // or nullptr
+    int z_dtype;                    // GSPC_F32, GSPC_BF16 or GSPC_F8 (8-bit float rows, with z_scale)
+    size_t ldz;
+    uint8_t *z_scale;
+    float *stats;                   // [rows][4]: mean and 1 / deviation of h, then of x'; or nullptr
+    int past;                       // xo and z are stored past the caches (set by the launch)
+};
+struct ResidualBackward {
+    const void *dz;                 // or nullptr
+    int dz_dtype;
+    size_t lddz;
+    const void *dxo;                // type of x; or nullptr
+    size_t lddxo;
+    const void *xo;
+    int x_dtype;
+    size_t ldxo;
+    const void *h;
+    int h_dtype;                    // of dh too
+    size_t ldh;
+    const float *stats;
+    void *dx;
+    size_t lddx;
+    void *dh;
+    size_t lddh;
+    float *dgate, *dpost_gamma, *dpost_beta, *dpre_gamma, *dpre_beta;       // any may be nullptr
+    int past;
+};
+size_t residual_grad_bytes(const Residual &a);
+hipError_t launch_residual_norm(const Residual &a, ResidualForward f, hipStream_t s);
+hipError_t launch_residual_grad(const Residual &a, ResidualBackward f, void *ws, hipStream_t s);
 
 }  // namespace gspc
