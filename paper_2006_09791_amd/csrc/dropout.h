@@ -7,13 +7,13 @@
 
 namespace gspc {
 
-// What columns 8 vec .. 8 vec + 7 of a row are multiplied by: d.up or 0.
-__device__ __forceinline__ void dropout_factors(const Dropout &d, uint64_t call, unsigned row, unsigned vec, float (&m)[8]) {
+// Columns 8 vec .. 8 vec + 7 of a row: those that are dropped become 0, whatever they are.
+__device__ __forceinline__ void drop_some(const Dropout &d, uint64_t call, unsigned row, unsigned vec, float (&v)[8]) {
     const Philox p = philox(vec, row, (uint32_t)call, (uint32_t)(call >> 32), d.seed);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        m[2 * e] = (p.word[e] & 0xffffu) >= d.limit ? d.up : 0.f;
-        m[2 * e + 1] = p.word[e] >> 16 >= d.limit ? d.up : 0.f;
+        v[2 * e] = (p.word[e] & 0xffffu) >= d.limit ? v[2 * e] : 0.f;
+        v[2 * e + 1] = p.word[e] >> 16 >= d.limit ? v[2 * e + 1] : 0.f;
     }
 }
 

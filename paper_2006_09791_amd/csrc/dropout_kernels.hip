@@ -7,30 +7,31 @@ namespace gspc {
 
 // A lane has eight columns of a row at a time.  Bound by memory as long as the generator's ten rounds (twenty products of 32 by 32 bits for eight
 // values) are hidden behind it.
-template <typename T>
+template <typename T, Rows ROWS>
 __global__ __launch_bounds__(256) void dropout_kernel(Dropout d, const T *x, size_t ldx, unsigned first, unsigned vectors, int cols, unsigned nv,
                                                       unsigned m_nv, T *y, size_t ldy, int past) {
     const unsigned i = blockIdx.x * 256 + threadIdx.x;
     if (i >= vectors) return;
-    const unsigned row = fast_div_any(i, nv, m_nv), vec = i - row * nv, at = vec * 8;
-    const int some = min(8, cols - (int)at);
-    const Raw<T, 8> raw = fetch_some(x + row * ldx + at, some);
+    const unsigned row = fast_div_any(i, nv, m_nv), vec = i - row * nv;
+    const Place at = place_of(vec * 8, cols);
+    const Raw<T, 8> raw = fetch_some<ROWS>(x + row * ldx, at);
     const uint64_t call = d.offset + (d.step ? *d.step : 0);
-    float m[8], v[8];
-    dropout_factors(d, call, first + row, vec, m);
-    widen(raw, v);
+    float v[8];
+    widen_some<ROWS>(raw, at, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = m[e] != 0.f ? v[e] * m[e] : 0.f;
-    store_some(y + row * ldy + at, v, some, past);
+    for (int e = 0; e < 8; ++e) v[e] *= d.up;
+    drop_some(d, call, first + row, vec, v);
+    store_some<ROWS>(y + row * ldy, at, v, past);
 }
 
 template <typename T> static hipError_t dropout(const Dropout &d, const T *x, size_t ldx, size_t rows, int cols, T *y, size_t ldy, hipStream_t s) {
     const unsigned nv = (cols + 7) / 8;
     const size_t most = (1u << 30) / nv;                // vectors of a launch
+    const auto kern = cols % 8 == 0 ? dropout_kernel<T, kWhole> : dropout_kernel<T, kThin>;
     const int past = sizeof(T) == 2 && rows * cols * 2 >= kPastCaches && whole_pieces(y, cols * sizeof(T), ldy * sizeof(T));
     for (size_t at = 0; at < rows; at += most) {
         const size_t n = (rows - at < most ? rows - at : most) * nv;
-        hipLaunchKernelGGL(dropout_kernel<T>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, d, x + at * ldx, ldx, (unsigned)at, (unsigned)n, cols, nv,
+        hipLaunchKernelGGL(kern, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, d, x + at * ldx, ldx, (unsigned)at, (unsigned)n, cols, nv,
                            div_magic(nv), y + at * ldy, ldy, past);
     }
     return hipGetLastError();

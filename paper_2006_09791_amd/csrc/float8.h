@@ -48,24 +48,67 @@ __device__ __forceinline__ unsigned top_of(const float (&v)[8]) {
     return top;
 }
 
-// Eight columns of a row of which the first n (0 .. 8) are there; the others are 0.
-template <typename T> __device__ __forceinline__ Raw<T, 8> fetch_some(const T *p, int n) {
-    if (n >= 8) return fetch<8>(p);
+// Eight columns of a row from `at` on, of which the first n (8, fewer at the row's end, or none) are there.  In rows of whole eights (kWhole) n is 8 or
+// 0.  What is there at the end of others (kRagged) is read as the row's last eight columns, in one access, and moved to its place when it is widened;
+// rows that may have fewer than eight columns (kThin) are read one by one where they have.
+enum Rows { kWhole, kRagged, kThin };
+struct Place {
+    unsigned at;
+    int n, shift;
+};
+__device__ __forceinline__ Place place_of(int at, int cols) {
+    Place p = {(unsigned)at, max(0, min(8, cols - at)), 0};
+    p.shift = cols >= 8 && p.n > 0 ? 8 - p.n : 0;
+    return p;
+}
+template <Rows ROWS, typename T> __device__ __forceinline__ Raw<T, 8> fetch_some(const T *row, const Place &p, bool there = true) {
     Raw<T, 8> r{};
+    if constexpr (ROWS == kWhole) {
+        if (there && p.n) r = fetch<8>(beyond(row, p.at * (unsigned)sizeof(T)));
+    } else {
+        if (there && p.n + p.shift == 8) r = fetch<8>(beyond(row, (p.at - p.shift) * (unsigned)sizeof(T)));
+        else if constexpr (ROWS == kThin) {
+            if (there)
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-        if (e < n) {
-            if constexpr (sizeof(T) == 4) (e < 4 ? r.a : r.b)[e & 3] = p[e];
-            else r.a[e / 2] |= (unsigned)p[e] << (e % 2 * 16);
+                for (int e = 0; e < 7; ++e)
+                    if (e < p.n) {
+                        if constexpr (sizeof(T) == 4) (e < 4 ? r.a : r.b)[e & 3] = row[p.at + e];
+                        else r.a[e / 2] |= (unsigned)row[p.at + e] << (e % 2 * 16);
+                    }
         }
+    }
     return r;
 }
-template <typename T> __device__ __forceinline__ void store_some(T *p, const float (&v)[8], int n, bool past = false) {
-    if (n >= 8) store(p, v, past);
-    else {
+// Columns that are not there become 0.
+template <Rows ROWS, typename R> __device__ __forceinline__ void widen_some(const R &raw, const Place &p, float (&v)[8]) {
+    widen(raw, v);
+    if constexpr (ROWS != kWhole) {
 #pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (e < n) put(p + e, v[e]);
+        for (int by = 4; by >= 1; by /= 2)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+            const float here = v[e], further = e + by < 8 ? v[(e + by) & 7] : 0.f;
+            v[e] = p.shift & by ? further : here;
+        }
+    }
+}
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *reinterpret_cast<f32x4_any *>(p) = (f32x4){a, b, c, d}; }
+__device__ __forceinline__ void store4(uint16_t *p, float a, float b, float c, float d) {
+    *reinterpret_cast<u32x2_any *>(p) = (u32x2){bf16_pair(a, b), bf16_pair(c, d)};
+}
+template <Rows ROWS, typename T> __device__ __forceinline__ void store_some(T *row, const Place &p, const float (&v)[8], bool past = false) {
+    T *to = beyond(row, p.at * (unsigned)sizeof(T));
+    if (p.n == 8) store(to, v, past);
+    else if constexpr (ROWS != kWhole) {                 // four, two and one of them (by value: a choice between places would put v into memory)
+        const bool four = p.n & 4, two = p.n & 2;
+        const float v0 = v[0], v1 = v[1], v2 = v[2], v4 = v[4], v5 = v[5], v6 = v[6];
+        const float pair0 = four ? v4 : v0, pair1 = four ? v5 : v1, low = two ? v2 : v0, high = two ? v6 : v4, one = four ? high : low;
+        if (four) store4(to, v0, v1, v2, v[3]);
+        if (two) {
+            put(to + (p.n & 4), pair0);
+            put(to + (p.n & 4) + 1, pair1);
+        }
+        if (p.n & 1) put(to + (p.n & 6), one);
     }
 }
 

@@ -54,12 +54,13 @@ __device__ __forceinline__ Wide widened(const i32x8 &v, unsigned code) {
 
 // ---- few tokens or few outputs: no staging --------------------------------------------------------------------------------------
 // A block has 16 TN channels x 16 TM tokens; its waves split the reduction into stretches, operands straight from memory into the registers of
-// v_mfma_scale_f32_16x16x128 (channels are the rows, tokens the columns of its result), DEEP steps of 128 in flight, and join their sums in LDS.
+// v_mfma_scale_f32_16x16x128 (channels are the rows, tokens the columns of its result; a lane's 32 columns are two pieces of 16, so that a
+// load of sixteen rows is of 64 bytes of each), DEEP steps of 128 in flight, and join their sums in LDS.
 // WIDE: operands as bf16.
 template <typename T, bool WIDE, int TN, int TM, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8Args p) {
     __shared__ f32x4 s_part[WAVES][TN * TM][kWave];
-    const unsigned nt = blockIdx.x % p.ntiles, mt = blockIdx.x / p.ntiles;
+    const unsigned part = blockIdx.x / p.tiles, tile = blockIdx.x - part * p.tiles, nt = tile % p.ntiles, mt = tile / p.ntiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n0 = nt * 16 * TN;
     const size_t m0 = (size_t)mt * 16 * TM;
@@ -67,9 +68,9 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
     const __amdgpu_buffer_rsrc_t ra = bytes_at(p.a + m0 * p.pitch, (p.M - m0) * p.pitch);
     const __amdgpu_buffer_rsrc_t rsw = bytes_at(p.w_scale + (size_t)n0 * p.s_pitch, (size_t)(p.N - n0) * p.s_pitch);
     const __amdgpu_buffer_rsrc_t rsa = bytes_at(p.a_scale + m0 * p.s_pitch, (p.M - m0) * p.s_pitch);
-    const unsigned row = lane % 16, lane_off = row * p.pitch + lane / 16 * 32, lane_scale = row * p.s_pitch;
-    const int steps = p.pitch / kBlock8, share = (steps + WAVES - 1) / WAVES;
-    const int first = wave * share, last = min(first + share, steps);
+    const unsigned row = lane % 16, lane_off = row * p.pitch + lane / 16 * 16, lane_scale = row * p.s_pitch;
+    const int begin = (int)part * p.stretch, end = min(begin + p.stretch, p.pitch / kBlock8), share = (end - begin + WAVES - 1) / WAVES;
+    const int first = begin + wave * share, last = min(first + share, end);
     f32x4 acc[TN][TM] = {};
     u32x4 w[DEEP][TN][2], a[DEEP][TM][2];
     unsigned sw[DEEP][TN], sa[DEEP][TM];
@@ -79,14 +80,14 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
         for (int i = 0; i < TN; ++i) {
             const unsigned off = lane_off + i * 16 * p.pitch + k;
             w[d][i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off, 0, 0));
-            w[d][i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off + 16, 0, 0));
+            w[d][i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off + 64, 0, 0));
             sw[d][i] = __builtin_amdgcn_raw_buffer_load_b32(rsw, lane_scale + i * 16 * p.s_pitch + s, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
             const unsigned off = lane_off + j * 16 * p.pitch + k;
             a[d][j][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off, 0, 0));
-            a[d][j][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off + 16, 0, 0));
+            a[d][j][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off + 64, 0, 0));
             sa[d][j] = __builtin_amdgcn_raw_buffer_load_b32(rsa, lane_scale + j * 16 * p.s_pitch + s, 0, 0);
         }
     };
@@ -129,17 +130,17 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
 #pragma unroll
         for (int j = 0; j < TM; ++j) s_part[wave][i * TM + j][lane] = acc[i][j];
     __syncthreads();
-    for (int tile = wave; tile < TN * TM; tile += WAVES) {
-        f32x4 sum = s_part[0][tile][lane];
+    for (int t = wave; t < TN * TM; t += WAVES) {
+        f32x4 sum = s_part[0][t][lane];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += s_part[v][tile][lane];
-        const size_t m = m0 + tile % TM * 16 + row;
-        const int n = n0 + tile / TM * 16 + lane / 16 * 4;
+        for (int v = 1; v < WAVES; ++v) sum += s_part[v][t][lane];
+        const size_t m = m0 + t % TM * 16 + row;
+        const int n = n0 + t / TM * 16 + lane / 16 * 4;
         if (m >= p.M || n >= p.N) continue;
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = p.bias ? sum[e] + p.bias[min(n + e, p.N - 1)] : sum[e];
-        T *o = static_cast<T *>(p.out) + m * p.ldo + n;
+        T *o = static_cast<T *>(p.out) + part * p.part + m * p.ldo + n;
         if (n + 3 < p.N) {
             if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any *>(o) = (f32x4){v[0], v[1], v[2], v[3]};
             else *reinterpret_cast<u32x2_any *>(o) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(256) void product_f8_join_kernel(const float *__res
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------------------
-enum { kSmall1, kSmall2, kTile64, kTile128, kTile256 };
+enum { kSmall1, kSmall2, kTile64, kTile128, kTile256, kTile128Deep };
 struct PlanF8 {
     int kernel, bm, bn, threads;
     int parts, stretch;     // stretches of K, and steps of each
@@ -374,18 +375,27 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     const int steps = f8_pitch(K) / kBlock8;
     const auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * (size_t)((N + bn - 1) / bn); };
     PlanF8 p;
+    // (M x K x N, us of a call among others, bf16 outputs; both sides)
+    //   256 x 256 from 160 tiles on: 12544 x 512 x 1024 has 196, 13.0 against 15.8 in tiles of 128; 2048 x 512 x 4096 has 128, 12.0 against 9.0.  Not
+    //   for 128 tokens or filters and fewer, where more than half of a tile is empty;
+    //   128 x 128 from 192 tiles on: 1000 x 2000 x 3000 has 192, 13.4 against 13.7 in 64 x 128; 512 x 4096 x 4096 has 128, 19.9 against 16.0.  Four
+    //   stages where a compute unit has one block: 2048 x 65536 x 2048, 340 against 507 with two; 12544 x 512 x 1024 (784 tiles), 23.6 against 15.8;
+    //   without staging where a block's steps, or those of all blocks, are few: 197 x 1280 x 1001, 5.0 against 7.2 in 64 x 128; 64 x 4096 x 4096, 13.4
+    //   against 12.0.  In 16 x 16 where these are few, too: 16 x 4096 x 4096, 8.0 against 11.6 in 32 x 32, 8 x 8192 x 8192, 19.2 against 15.9 in 64 x 128;
+    //   64 x 512 x 512, 2.6 against 3.1; 200 x 1024 x 1024 (832 blocks), 6.6 against 4.3.
+    const size_t small = tiles(16, 16);
     if (!wide && M > 128 && N > 128 && tiles(256, 256) >= 160) p = {kTile256, 256, 256, 512, 1, steps};
-    else if (M > 64 && tiles(128, 128) >= 256) p = {kTile128, 128, 128, 256, 1, steps};
-    else if (M <= 16 && tiles(64, 128) < 256) p = {kSmall1, 16, 16, 512, 1, steps};
-    else if (tiles(32, 32) <= 256 || tiles(32, 32) * (size_t)steps <= 1280) p = {kSmall2, 32, 32, 512, 1, steps};
+    else if (M > 64 && tiles(128, 128) >= 192) p = {tiles(128, 128) <= 256 ? kTile128Deep : kTile128, 128, 128, 256, 1, steps};
+    else if ((M <= 16 && tiles(64, 128) < 256 && small * steps <= 16384) || (small <= 256 && small * steps <= 2560)) p = {kSmall1, 16, 16, 512, 1, steps};
+    else if (tiles(32, 32) * steps <= 2560) p = {kSmall2, 32, 32, 512, 1, steps};
     else p = {kTile64, 64, 128, 256, 1, steps};
-    // Few tiles of a long sum: K in stretches of 1024 and more, until every compute unit has a block.
+    // Few blocks of a long sum: stretches of K, of 8 steps at least (32, where the block's waves share them), until every compute unit has a block.  512 x
+    // 12544 x 512 has 32 tiles: 36.1 whole, 15.0 in eight stretches and their join; 64 x 4096 x 4096, 14.4 and 12.0 in four.
     const size_t count = tiles(p.bm, p.bn);
-    if (p.kernel >= kTile64 && count < 256 && steps >= 16) {
-        int want = (int)(256 / count), most = steps / 8;
-        if (want > most) want = most;
-        if (want > 1) {
-            p.stretch = ((steps + want - 1) / want + 3) / 4 * 4;
+    if (count <= 128) {
+        const int want = (int)(256 / count), most = steps / (p.kernel < kTile64 ? 32 : 8), parts = want < most ? want : most;
+        if (parts > 1) {
+            p.stretch = ((steps + parts - 1) / parts + 3) / 4 * 4;
             p.parts = (steps + p.stretch - 1) / p.stretch;
         }
     }
@@ -421,12 +431,11 @@ template <typename T, bool WIDE> static void run_f8(const PlanF8 &plan, ProductF
             }
     };
     switch (plan.kernel) {
+    case kSmall1: return run(product_f8_small_kernel<T, WIDE, 1, 1, 8, 4>, "product_f8_small<1,1>");
+    case kSmall2: return run(product_f8_small_kernel<T, WIDE, 2, 2, 8, 2>, "product_f8_small<2,2>");
     case kTile64: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 1, 2, 3>, "product_f8_tile<64,128>");
+    case kTile128Deep: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 2, 2, 4>, "product_f8_tile<128,128>");
     case kTile128: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 2, 2, 2>, "product_f8_tile<128,128>");
-    }
-    if constexpr (WIDE == (sizeof(T) == 4)) {
-        if (plan.kernel == kSmall1) run(product_f8_small_kernel<T, WIDE, 1, 1, 8, 2>, "product_f8_small<1,1>");
-        if (plan.kernel == kSmall2) run(product_f8_small_kernel<T, WIDE, 2, 2, 8, 1>, "product_f8_small<2,2>");
     }
     if constexpr (sizeof(T) == 2)
         if (plan.kernel == kTile256) run(product_f8_tile_kernel<T, WIDE, 2, 4, 4, 2, 2>, "product_f8_tile<256,256>");

@@ -17,15 +17,17 @@ struct GradPlan {
 };
 
 // A team walks down its tokens and keeps the sums of its columns; a block's teams add theirs up and leave one part.  Bound by memory where there are
-// many tokens: dz, dx', x' and h in, dx and dh out.  GATES: a team's tokens have several gates, whose gradients it writes itself.
-template <typename TX, typename TH, bool GATES>
-__global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, ResidualBackward f, GradPlan g, int team, unsigned m_chunks,
+// many tokens: dz, dx', x' and h in, dx and dh out.  GATES: a team's tokens have several gates, whose gradients it writes itself.  LARGE: teams of
+// more than 512 lanes, which leave 128 registers each: parameters are read again for each token, and no token ahead.
+template <typename TX, typename TH, bool GATES, bool LARGE, Rows ROWS>
+__global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad_kernel(Residual a, ResidualBackward f, GradPlan g, int of_team, unsigned m_chunks,
                                                                  float *__restrict__ parts) {
     __shared__ float2 s_place[2][kMaxTeam / kWave];
     __shared__ float s_sum[kTeamThreads * 8];              // (of several teams)
     TeamSums sums{s_place, 0};
-    const int lane = threadIdx.x & (team - 1), at = lane * 8, n = max(0, min(8, a.cols - at));
-    const unsigned teams = blockDim.x / team, mine = threadIdx.x / team;
+    const int team = LARGE ? kMaxTeam : of_team, lane = threadIdx.x & (team - 1);
+    Place at = place_of(lane * 8, a.cols);
+    const unsigned teams = LARGE ? 1 : blockDim.x / team, mine = LARGE ? 0 : threadIdx.x / team;
     unsigned first, last, gate_row = 0;
     if constexpr (GATES) {
         first = (blockIdx.x * teams + mine) * g.each;
@@ -38,57 +40,110 @@ __global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, Res
         last = min(first + g.each, group * a.gate_rows + end);
         gate_row = group;
     }
+    const TX *const xo = static_cast<const TX *>(f.xo), *const dxo = static_cast<const TX *>(f.dxo);
+    const TH *const h = static_cast<const TH *>(f.h);
+    // A token's values, raw: the next one's are on their way while this one's are worked on.
+    RawAny r_dz{};
+    Raw<TX, 8> r_xo{}, r_dxo{};
+    Raw<TH, 8> r_h{};
+    float4 r_st = make_float4(0.f, 1.f, 0.f, 1.f);
+    const auto load_norm = [&](unsigned row, bool there) {
+        const size_t r = there ? row : 0;
+        if (there) r_st = *reinterpret_cast<const float4 *>(f.stats + r * 4);
+        if (f.dz) {
+            r_dz = fetch_any<ROWS>(f.dz, f.dz_dtype, r * f.lddz, at, there);
+            r_xo = fetch_some<ROWS>(xo + r * f.ldxo, at, there);
+        }
+    };
+    const auto load_stream = [&](unsigned row, bool there) {
+        if (f.dxo) r_dxo = fetch_some<ROWS>(dxo + (there ? row : 0) * f.lddxo, at, there);
+    };
+    const auto load_h = [&](unsigned row, bool there) {
+        if (f.h) r_h = fetch_some<ROWS>(h + (there ? row : 0) * f.ldh, at, there);
+    };
+    if constexpr (!LARGE) {
+        load_norm(first, first < last);
+        load_stream(first, first < last);
+        load_h(first, first < last);
+    }
     const float inv = 1.f / (float)a.cols;
     const bool centre1 = a.post == kNormLayer, centre2 = a.pre == kNormLayer;
     const uint64_t call = a.drop.offset + (a.drop.step ? *a.drop.step : 0);
-    float g2[8], b2[8], gg[8];                                  // gg: g1 gate
-    some_params(a.pre_gamma, at, n, 1.f, g2);
-    some_params(a.pre_beta, at, n, 0.f, b2);
+    float g2[8], b2[8], gg[8];                                  // gg: g1 gate, times what makes up for the dropped
+    const auto pre_params = [&] {
+        some_params<ROWS>(a.pre_gamma, at, 1.f, g2);
+        some_params<ROWS>(a.pre_beta, at, 0.f, b2);
+    };
+    if constexpr (!LARGE) pre_params();
     const auto new_gate = [&] {
         float gate[8];
-        some_params(a.post_gamma, at, n, 1.f, gg);
-        if (a.gate) {
-            some_params(a.gate + (size_t)gate_row * a.cols, at, n, 1.f, gate);
+        some_params<ROWS>(a.post_gamma, at, 1.f, gg);
+        some_params<ROWS>(a.gate ? a.gate + (size_t)gate_row * a.cols : nullptr, at, 1.f, gate);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) gg[e] *= gate[e];
-        }
+        for (int e = 0; e < 8; ++e) gg[e] *= gate[e] * a.drop.up;
     };
-    if (!GATES || first < last) new_gate();
-    float sa[8] = {}, sb[8] = {}, sg2[8] = {}, sb2[8] = {}, sg1[GATES ? 8 : 1] = {}, sb1[GATES ? 8 : 1] = {};
+    if constexpr (!LARGE)
+        if (!GATES || first < last) new_gate();
+    float sa[8] = {}, sb[8] = {}, sg2[LARGE ? 1 : 8] = {}, sb2[LARGE ? 1 : 8] = {}, sg1[GATES && !LARGE ? 8 : 1] = {}, sb1[GATES && !LARGE ? 8 : 1] = {};
+    // (a large team keeps the sums over gates, and dg2 and db2, in LDS)
+    __shared__ float s_gates[LARGE && GATES ? 16 : 1][kMaxTeam], s_pre[LARGE ? 16 : 1][kMaxTeam];
+    if constexpr (LARGE)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s_pre[e][threadIdx.x] = 0.f;
+            if constexpr (GATES) s_gates[e][threadIdx.x] = 0.f;
+        }
     // A gate's tokens are through: its gradient, and what its sums are to the parameters'.
     const auto end_gate = [&](float (&dgate)[8], float (&dg1)[8], float (&db1)[8]) {
         float gate[8], g1[8], b1[8];
-        some_params(a.gate ? a.gate + (size_t)gate_row * a.cols : nullptr, at, n, 1.f, gate);
-        some_params(a.post_gamma, at, n, 1.f, g1);
-        some_params(a.post_beta, at, n, 0.f, b1);
+        some_params<ROWS>(a.gate ? a.gate + (size_t)gate_row * a.cols : nullptr, at, 1.f, gate);
+        some_params<ROWS>(a.post_gamma, at, 1.f, g1);
+        some_params<ROWS>(a.post_beta, at, 0.f, b1);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            dgate[e] = fmaf(g1[e], sa[e], b1[e] * sb[e]);
-            dg1[e] = gate[e] * sa[e];
-            db1[e] = gate[e] * sb[e];
+            const float da = sa[e] * a.drop.up, db = sb[e] * a.drop.up;
+            dgate[e] = fmaf(g1[e], da, b1[e] * db);
+            dg1[e] = gate[e] * da;
+            db1[e] = gate[e] * db;
+        }
+    };
+    const auto phase = [] {                                     // (nothing is loaded ahead of it where registers are few)
+        if constexpr (LARGE) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     unsigned left = a.gate_rows;                                // tokens of this gate to come (GATES)
     for (unsigned k = 0; k < g.each; ++k) {                     // as often in every team: there are barriers
         const unsigned row = first + k;
         const bool there = row < last;
-        const int some = there ? n : 0;
-        const size_t at_row = there ? row : 0;
-        float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
-        if (there) st = *reinterpret_cast<const float4 *>(f.stats + at_row * 4);
+        asm volatile("" : "+v"(at.at));         // (no address of a lane's own is kept over tokens: two registers for each tensor)
+        if constexpr (LARGE) load_norm(row, there);
+        const float4 st = there ? r_st : make_float4(0.f, 1.f, 0.f, 1.f);
+        const int n = there ? at.n : 0;
         float dv[8] = {}, d[8] = {}, xh[8], hh[8];
         if (f.dz) {
-            if (f.dz_dtype == GSPC_F32) widen(fetch_some(static_cast<const float *>(f.dz) + at_row * f.lddz + at, some), dv);
-            else widen(fetch_some(static_cast<const uint16_t *>(f.dz) + at_row * f.lddz + at, some), dv);
-            widen(fetch_some(static_cast<const TX *>(f.xo) + at_row * f.ldxo + at, some), xh);
+            widen_any<ROWS>(r_dz, f.dz_dtype, at, dv);
+            widen_some<ROWS>(r_xo, at, xh);
         }
-        if (f.dxo) widen(fetch_some(static_cast<const TX *>(f.dxo) + at_row * f.lddxo + at, some), d);
-        if (f.h) widen(fetch_some(static_cast<const TH *>(f.h) + at_row * f.ldh + at, some), hh);
+        if constexpr (!LARGE) {
+            if (f.dxo) widen_some<ROWS>(r_dxo, at, d);
+            if (f.h) widen_some<ROWS>(r_h, at, hh);
+            const bool more = k + 1 < g.each && row + 1 < last;
+            load_norm(row + 1, more);
+            load_stream(row + 1, more);
+            load_h(row + 1, more);
+        }
         if (f.dz) {
+            if constexpr (LARGE) pre_params();
+            phase();
             float2 s = make_float2(0.f, 0.f);
             float t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) xh[e] = e < some ? (xh[e] - st.z) * st.w : 0.f;
+            for (int e = 0; e < 8; ++e) xh[e] = (xh[e] - st.z) * st.w;
+            if constexpr (ROWS != kWhole)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xh[e] = e < n ? xh[e] : 0.f;        // (dv is 0 where nothing is there, but a parameter's slope may be none)
             if (a.act != kActNone) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -98,36 +153,52 @@ __global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, Res
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sg2[e] = fmaf(dv[e], xh[e], sg2[e]);
-                sb2[e] += dv[e];
+                if constexpr (LARGE) {
+                    s_pre[e][threadIdx.x] = fmaf(dv[e], xh[e], s_pre[e][threadIdx.x]);
+                    s_pre[8 + e][threadIdx.x] += dv[e];
+                } else {
+                    sg2[e] = fmaf(dv[e], xh[e], sg2[e]);
+                    sb2[e] += dv[e];
+                }
                 t[e] = g2[e] * dv[e];
                 s.x += t[e];
                 s.y = fmaf(t[e], xh[e], s.y);
             }
             s = team_sum(s, team, sums);
             const float m = centre2 ? s.x * inv : 0.f, c = s.y * inv;
+            phase();
+            if constexpr (LARGE) {
+                load_stream(row, there);
+                if (f.dxo) widen_some<ROWS>(r_dxo, at, d);
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = fmaf(st.w, t[e] - m - xh[e] * c, d[e]);
+        } else if constexpr (LARGE) {
+            load_stream(row, there);
+            if (f.dxo) widen_some<ROWS>(r_dxo, at, d);
         }
+        phase();
         if (there) {
             float out[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = a.scale * d[e];
-            store_some(static_cast<TX *>(f.dx) + at_row * f.lddx + at, out, n, f.past);
+            store_some<ROWS>(static_cast<TX *>(f.dx) + row * f.lddx, at, out, f.past);
         }
         if (f.h) {
-            if (a.drop.limit) {
-                float w[8];
-                dropout_factors(a.drop, call, row, lane, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] = w[e] != 0.f ? d[e] * w[e] : 0.f;
+            if (a.drop.limit) drop_some(a.drop, call, row, lane, d);
+            phase();
+            if constexpr (LARGE) {
+                load_h(row, there);
+                widen_some<ROWS>(r_h, at, hh);
+                if (there) new_gate();
             }
+            phase();
             float2 s = make_float2(0.f, 0.f);
             float q[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] = e < some ? d[e] : 0.f;
-                hh[e] = e < some ? (hh[e] - st.x) * st.y : 0.f;
+                d[e] = (ROWS == kWhole ? n > 0 : e < n) ? d[e] : 0.f;
+                hh[e] = (hh[e] - st.x) * st.y;
                 sa[e] = fmaf(d[e], hh[e], sa[e]);
                 sb[e] += d[e];
                 q[e] = gg[e] * d[e];
@@ -140,18 +211,23 @@ __global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, Res
 #pragma unroll
                 for (int e = 0; e < 8; ++e) q[e] = st.y * (q[e] - m - hh[e] * c);
             }
-            if (there) store_some(static_cast<TH *>(f.dh) + at_row * f.lddh + at, q, n, f.past);
+            if (there) store_some<ROWS>(static_cast<TH *>(f.dh) + row * f.lddh, at, q, f.past);
         }
         if constexpr (GATES) {
             if (--left == 0) {
                 if (there) {
                     float dgate[8], dg1[8], db1[8];
                     end_gate(dgate, dg1, db1);
-                    if (f.dgate) store_some(f.dgate + (size_t)gate_row * a.cols + at, dgate, n);
+                    if (f.dgate) store_some<ROWS>(f.dgate + (size_t)gate_row * a.cols, at, dgate);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sg1[e] += dg1[e], sb1[e] += db1[e], sa[e] = sb[e] = 0.f;
+                    for (int e = 0; e < 8; ++e) {
+                        if constexpr (LARGE) s_gates[e][threadIdx.x] += dg1[e], s_gates[8 + e][threadIdx.x] += db1[e];
+                        else sg1[e] += dg1[e], sb1[e] += db1[e];
+                        sa[e] = sb[e] = 0.f;
+                    }
                     ++gate_row;
-                    if (row + 1 < last) new_gate();
+                    if constexpr (!LARGE)
+                        if (row + 1 < last) new_gate();
                 }
                 left = a.gate_rows;
             }
@@ -160,17 +236,20 @@ __global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, Res
     float dgate[8], dg1[8], db1[8];
     if constexpr (GATES) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dg1[e] = sg1[e], db1[e] = sb1[e];
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (LARGE) dg1[e] = s_gates[e][threadIdx.x], db1[e] = s_gates[8 + e][threadIdx.x];
+            else dg1[e] = sg1[e], db1[e] = sb1[e];
+        }
     } else
         end_gate(dgate, dg1, db1);
     // The teams' sums as one part of the block, a kind at a time.
     const auto leave = [&](const float (&v)[8], float *to) {
         if (teams == 1) {
-            store_some(to + at, v, n);
+            store_some<ROWS>(to, at, v);
             return;
         }
         __syncthreads();
-        store(s_sum + mine * team * 8 + at, v);
+        store(s_sum + mine * team * 8 + at.at, v);
         __syncthreads();
         for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
             float sum = s_sum[c];
@@ -181,8 +260,14 @@ __global__ __launch_bounds__(kMaxTeam) void residual_grad_kernel(Residual a, Res
     float *part = parts + (size_t)blockIdx.x * kSums * a.cols;
     if (f.dpost_gamma) leave(dg1, part);
     if (f.dpost_beta) leave(db1, part + a.cols);
-    if (f.dpre_gamma) leave(sg2, part + 2 * a.cols);
-    if (f.dpre_beta) leave(sb2, part + 3 * a.cols);
+    float dg2[8], db2[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (LARGE) dg2[e] = s_pre[e][threadIdx.x], db2[e] = s_pre[8 + e][threadIdx.x];
+        else dg2[e] = sg2[e], db2[e] = sb2[e];
+    }
+    if (f.dpre_gamma) leave(dg2, part + 2 * a.cols);
+    if (f.dpre_beta) leave(db2, part + 3 * a.cols);
     if (!GATES && f.dgate) leave(dgate, g.chunks == 1 ? f.dgate + (size_t)gate_row * a.cols : part + 4 * a.cols);
 }
 
@@ -213,7 +298,7 @@ __global__ __launch_bounds__(256) void residual_clear_kernel(float *p, size_t co
 }
 
 static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
-    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 1024;
+    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 256 * 12 * kWave / t.threads;
     GradPlan p;
     if (gates > 1 && gates >= wanted * t.teams) {       // whole gates for each team
         const unsigned of_team = (gates - 1) / (wanted * t.teams) + 1, most = gate_rows < 1024 ? 1024 / gate_rows : 1;
@@ -256,14 +341,19 @@ hipError_t launch_residual_grad(const Residual &a, ResidualBackward f, void *ws,
     const auto run = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3(p.blocks), dim3(g.threads), 0, s, a, f, p, g.team, div_magic(p.chunks ? p.chunks : 1), parts);
     };
-    const bool x32 = f.x_dtype == GSPC_F32, h32 = f.h_dtype == GSPC_F32;
-    if (p.chunks) {
-        if (x32) h32 ? run(residual_grad_kernel<float, float, false>) : run(residual_grad_kernel<float, uint16_t, false>);
-        else h32 ? run(residual_grad_kernel<uint16_t, float, false>) : run(residual_grad_kernel<uint16_t, uint16_t, false>);
-    } else {
-        if (x32) h32 ? run(residual_grad_kernel<float, float, true>) : run(residual_grad_kernel<float, uint16_t, true>);
-        else h32 ? run(residual_grad_kernel<uint16_t, float, true>) : run(residual_grad_kernel<uint16_t, uint16_t, true>);
-    }
+    const auto of = [&](auto x, auto h, auto gates) {
+        typedef decltype(x) TX;
+        typedef decltype(h) TH;
+        constexpr bool GATES = decltype(gates)::value;
+        if (g.team > kMaxTeam / 2) run(residual_grad_kernel<TX, TH, GATES, true, kRagged>);
+        else if (a.cols % 8 == 0) run(residual_grad_kernel<TX, TH, GATES, false, kWhole>);
+        else run(residual_grad_kernel<TX, TH, GATES, false, kThin>);
+    };
+    const auto by_types = [&](auto gates) {
+        if (f.x_dtype == GSPC_F32) f.h_dtype == GSPC_F32 ? of(0.f, 0.f, gates) : of(0.f, uint16_t(), gates);
+        else f.h_dtype == GSPC_F32 ? of(uint16_t(), 0.f, gates) : of(uint16_t(), uint16_t(), gates);
+    };
+    p.chunks ? by_types(std::false_type()) : by_types(std::true_type());
     const unsigned slabs = (a.cols + kWave - 1) / kWave, kinds = 4 + (f.dgate && p.chunks > 1 ? a.gates : 0);
     if (kinds > 4 || f.dpost_gamma || f.dpost_beta || f.dpre_gamma || f.dpre_beta)
         hipLaunchKernelGGL(residual_join_kernel, dim3(kinds * slabs), dim3(1024), 0, s, parts, p.blocks, p.chunks, a.cols, slabs, f.dpost_gamma,
