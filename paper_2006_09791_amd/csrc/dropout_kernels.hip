@@ -27,7 +27,8 @@ __global__ __launch_bounds__(256) void dropout_kernel(Dropout d, const T *x, siz
 template <typename T> static hipError_t dropout(const Dropout &d, const T *x, size_t ldx, size_t rows, int cols, T *y, size_t ldy, hipStream_t s) {
     const unsigned nv = (cols + 7) / 8;
     const size_t most = (1u << 30) / nv;                // vectors of a launch
-    const auto kern = cols % 8 == 0 ? dropout_kernel<T, kWhole> : dropout_kernel<T, kThin>;
+    const Rows kind = rows_of(cols);
+    const auto kern = kind == kWhole ? dropout_kernel<T, kWhole> : kind == kRagged ? dropout_kernel<T, kRagged> : dropout_kernel<T, kThin>;
     const int past = sizeof(T) == 2 && rows * cols * 2 >= kPastCaches && whole_pieces(y, cols * sizeof(T), ldy * sizeof(T));
     for (size_t at = 0; at < rows; at += most) {
         const size_t n = (rows - at < most ? rows - at : most) * nv;

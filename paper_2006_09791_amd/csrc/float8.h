@@ -50,46 +50,51 @@ __device__ __forceinline__ unsigned top_of(const float (&v)[8]) {
 
 // Eight columns of a row from `at` on, of which the first n (8, fewer at the row's end, or none) are there.  In rows of whole eights (kWhole) n is 8 or
 // 0.  What is there at the end of others (kRagged) is read as the row's last eight columns, in one access, and moved to its place when it is widened;
-// rows that may have fewer than eight columns (kThin) are read one by one where they have.
+// rows of fewer than eight columns (kThin) are read one by one.  Lanes without a column read the row's first ones: no load hangs on a branch, behind
+// which a wait for older loads would have to be one for all.
 enum Rows { kWhole, kRagged, kThin };
+inline Rows rows_of(int cols) { return cols % 8 == 0 ? kWhole : cols > 8 ? kRagged : kThin; }
 struct Place {
-    unsigned at;
+    unsigned at, start;         // start: of what is read
     int n, shift;
 };
 __device__ __forceinline__ Place place_of(int at, int cols) {
-    Place p = {(unsigned)at, max(0, min(8, cols - at)), 0};
-    p.shift = cols >= 8 && p.n > 0 ? 8 - p.n : 0;
+    Place p;
+    p.at = at;
+    p.n = max(0, min(8, cols - at));
+    p.shift = p.n > 0 ? 8 - p.n : 0;
+    p.start = p.n > 0 ? at - p.shift : 0;
     return p;
 }
-template <Rows ROWS, typename T> __device__ __forceinline__ Raw<T, 8> fetch_some(const T *row, const Place &p, bool there = true) {
-    Raw<T, 8> r{};
-    if constexpr (ROWS == kWhole) {
-        if (there && p.n) r = fetch<8>(beyond(row, p.at * (unsigned)sizeof(T)));
-    } else {
-        if (there && p.n + p.shift == 8) r = fetch<8>(beyond(row, (p.at - p.shift) * (unsigned)sizeof(T)));
-        else if constexpr (ROWS == kThin) {
-            if (there)
+template <Rows ROWS, typename T> __device__ __forceinline__ Raw<T, 8> fetch_some(const T *row, const Place &p) {
+    if constexpr (ROWS != kThin) return fetch<8>(beyond(row, p.start * (unsigned)sizeof(T)));
+    else {
+        Raw<T, 8> r{};
 #pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (e < p.n) {
-                        if constexpr (sizeof(T) == 4) (e < 4 ? r.a : r.b)[e & 3] = row[p.at + e];
-                        else r.a[e / 2] |= (unsigned)row[p.at + e] << (e % 2 * 16);
-                    }
+        for (int e = 0; e < 7; ++e) {
+            const T x = row[max(0, min(e, p.n - 1))];
+            if constexpr (sizeof(T) == 4) (e < 4 ? r.a : r.b)[e & 3] = x;
+            else r.a[e / 2] |= (unsigned)x << (e % 2 * 16);
         }
+        return r;
     }
-    return r;
 }
-// Columns that are not there become 0.
-template <Rows ROWS, typename R> __device__ __forceinline__ void widen_some(const R &raw, const Place &p, float (&v)[8]) {
+// Columns that are not there become 0; all of them do without `there`.
+template <Rows ROWS, typename R> __device__ __forceinline__ void widen_some(R raw, const Place &p, float (&v)[8], bool there = true) {
+    keep_if(raw, there && p.n > 0);
     widen(raw, v);
-    if constexpr (ROWS != kWhole) {
+    if constexpr (ROWS == kRagged) {
 #pragma unroll
         for (int by = 4; by >= 1; by /= 2)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-            const float here = v[e], further = e + by < 8 ? v[(e + by) & 7] : 0.f;
-            v[e] = p.shift & by ? further : here;
-        }
+                const float here = v[e], further = e + by < 8 ? v[(e + by) & 7] : 0.f;
+                v[e] = p.shift & by ? further : here;
+            }
+    }
+    if constexpr (ROWS == kThin) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < p.n ? v[e] : 0.f;
     }
 }
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *reinterpret_cast<f32x4_any *>(p) = (f32x4){a, b, c, d}; }

@@ -25,84 +25,98 @@ inline TeamGrid team_grid(int cols, int least) {
 }
 
 // Sums over a team of two numbers at once; every lane gets them.  Waves of a team meet in LDS, in two places by turns: when a place is written
-// again, a barrier has passed since it was read.
+// again, a barrier has passed since it was read.  WAVES: the team is one wave or several (its width in a wave is a constant, and a sum is without
+// branches); else it is 8, 16 or 32 lanes.
 struct TeamSums {
     float2 (*place)[kMaxTeam / kWave];
     int turn;
 };
-__device__ __forceinline__ float2 team_sum(float2 v, int team, TeamSums &t) {
-    const int width = min(team, kWave);
-    v.x = lanes_sum(v.x, width);
-    v.y = lanes_sum(v.y, width);
-    if (team > kWave) {
-        const int waves = team / kWave, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-        if (lane == 0) t.place[t.turn][wave] = v;
-        __syncthreads();
-        v = t.place[t.turn][(wave & -waves) + (lane & (waves - 1))];
-        v.x = lanes_sum(v.x, waves);
-        v.y = lanes_sum(v.y, waves);
-        t.turn ^= 1;
+template <bool WAVES> __device__ __forceinline__ float2 wave_sum(float2 v, int team) {
+    const auto sums = [&](auto width) {
+        constexpr int WIDTH = decltype(width)::value;
+        return make_float2(lanes_sum(v.x, WIDTH), lanes_sum(v.y, WIDTH));
+    };
+    if constexpr (WAVES) return sums(std::integral_constant<int, 64>());
+    else return team == 32 ? sums(std::integral_constant<int, 32>()) : team == 16 ? sums(std::integral_constant<int, 16>()) : sums(std::integral_constant<int, 8>());
+}
+// What the other waves of the team have: lane l of the first sixteen that of wave l, 0 where there is none.
+__device__ __forceinline__ float2 team_exchange(float2 v, int team, TeamSums &t) {
+    const int waves = team / kWave, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if (lane == 0) t.place[t.turn][wave] = v;
+    __syncthreads();
+    v = t.place[t.turn][(wave & -waves) + (lane & (waves - 1))];
+    t.turn ^= 1;
+    return lane % 16 < waves ? v : make_float2(0.f, 0.f);
+}
+template <bool WAVES> __device__ __forceinline__ float2 team_sum(float2 v, int team, TeamSums &t) {
+    v = wave_sum<WAVES>(v, team);
+    if (WAVES && team > kWave) {
+        const float2 o = team_exchange(v, team, t);
+        v = make_float2(lanes_sum(o.x, 16), lanes_sum(o.y, 16));
     }
     return v;
 }
 
+// a / n by the reciprocal, corrected once: exact where the quotient is a number (a constant token's mean is its value).
+__device__ __forceinline__ float ratio(float a, float n) {
+    const float r = __builtin_amdgcn_rcpf(n), q = a * r;
+    return fmaf(fmaf(-q, n, a), r, q);
+}
+
 // Mean and 1 / deviation of a token, of the values of v that are there (n of a lane's; the others are 0): a wave's own mean and the squares around it,
 // joined over the waves (so that an offset does not cancel in them).  seg: the wave's number in its team.
-template <Rows ROWS>
+template <Rows ROWS, bool WAVES>
 __device__ __forceinline__ float2 team_stats(const float (&v)[8], int n, int cols, int kind, float eps, int team, int seg, TeamSums &t) {
     const float count = (float)cols;
     float sum = 0.f;
     if (kind == kNormRms) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
-        return make_float2(0.f, 1.f / sqrtf(team_sum(make_float2(sum, 0.f), team, t).x / count + eps));
+        return make_float2(0.f, rsqrtf(ratio(team_sum<WAVES>(make_float2(sum, 0.f), team, t).x, count) + eps));
     }
-    const int width = min(team, kWave);
     const auto of = [&](int wave) { return (float)max(0, min(cols - wave * 8 * kWave, 8 * kWave)); };
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += v[e];
     const float mine = of(seg);
-    float mean = mine > 0.f ? lanes_sum(sum, width) / mine : 0.f, squares = 0.f;
+    float mean = mine > 0.f ? ratio(wave_sum<WAVES>(make_float2(sum, 0.f), team).x, mine) : 0.f, squares = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float d = ROWS == kWhole || e < n ? v[e] - mean : 0.f;
         squares = fmaf(d, d, squares);
     }
-    squares = lanes_sum(ROWS == kWhole && n == 0 ? 0.f : squares, width);
-    if (team > kWave) {
-        const int waves = team / kWave, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, other = lane & (waves - 1);
-        if (lane == 0) t.place[t.turn][wave] = make_float2(mean, squares);
-        __syncthreads();
-        const float2 o = t.place[t.turn][(wave & -waves) + other];
-        mean = lanes_sum(of(other) * o.x, waves) / count;
-        squares = lanes_sum(o.y + of(other) * (o.x - mean) * (o.x - mean), waves);
-        t.turn ^= 1;
+    squares = wave_sum<WAVES>(make_float2(ROWS == kWhole && n == 0 ? 0.f : squares, 0.f), team).x;
+    if (WAVES && team > kWave) {
+        const float2 o = team_exchange(make_float2(mean, squares), team, t);
+        const int other = threadIdx.x % 16;             // (a wave that is not there has no columns)
+        mean = ratio(lanes_sum(of(other) * o.x, 16), count);
+        squares = lanes_sum(o.y + of(other) * (o.x - mean) * (o.x - mean), 16);
     }
-    return make_float2(mean, 1.f / sqrtf(squares / count + eps));
+    return make_float2(mean, rsqrtf(ratio(squares, count) + eps));
 }
 
 // Eight values of a parameter, or `none` for each.
 template <Rows ROWS> __device__ __forceinline__ void some_params(const float *__restrict__ p, const Place &at, float none, float (&v)[8]) {
-    if (p) widen_some<ROWS>(fetch_some<ROWS>(p, at), at, v);
-    else {
+    float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = none;
-    }
+    for (int e = 0; e < 8; ++e) w[e] = none;
+    if (p) widen_some<ROWS>(fetch_some<ROWS>(p, at), at, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = w[e];        // (in one order, whichever: stores of two would be put together, and v into memory)
 }
 
 // Eight values of a type that the launch names, raw until they are used.
-struct RawAny {
-    Raw32 r;
-};
-template <Rows ROWS> __device__ __forceinline__ RawAny fetch_any(const void *t, int dtype, size_t off, const Place &at, bool there) {
-    if (dtype == GSPC_F32) return {fetch_some<ROWS>(static_cast<const float *>(t) + off, at, there)};
-    RawAny a{};
-    a.r.a = __builtin_bit_cast(f32x4, fetch_some<ROWS>(static_cast<const uint16_t *>(t) + off, at, there).a);
-    return a;
+template <Rows ROWS> __device__ __forceinline__ Raw32 fetch_any(const void *t, int dtype, size_t off, const Place &at) {
+    if (dtype == GSPC_F32) return fetch_some<ROWS>(static_cast<const float *>(t) + off, at);
+    Raw32 r{};
+    r.a = __builtin_bit_cast(f32x4, fetch_some<ROWS>(static_cast<const uint16_t *>(t) + off, at).a);
+    return r;
 }
-template <Rows ROWS> __device__ __forceinline__ void widen_any(const RawAny &a, int dtype, const Place &at, float (&v)[8]) {
-    if (dtype == GSPC_F32) widen_some<ROWS>(a.r, at, v);
-    else widen_some<ROWS>(Raw16{__builtin_bit_cast(u32x4, a.r.a)}, at, v);
+template <Rows ROWS> __device__ __forceinline__ void widen_any(const Raw32 &r, int dtype, const Place &at, float (&v)[8], bool there) {
+    if (dtype == GSPC_F32) widen_some<ROWS>(r, at, v, there);
+    else widen_some<ROWS>(Raw16{__builtin_bit_cast(u32x4, r.a)}, at, v, there);
 }
+
+// The number of a team's token, the same for a wave where a team is one or more.
+template <bool WAVES> __device__ __forceinline__ unsigned token(unsigned n) { return WAVES ? __builtin_amdgcn_readfirstlane(n) : n; }
 
 }  // namespace gspc

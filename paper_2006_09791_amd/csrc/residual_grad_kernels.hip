@@ -19,7 +19,7 @@ struct GradPlan {
 // A team walks down its tokens and keeps the sums of its columns; a block's teams add theirs up and leave one part.  Bound by memory where there are
 // many tokens: dz, dx', x' and h in, dx and dh out.  GATES: a team's tokens have several gates, whose gradients it writes itself.  LARGE: teams of
 // more than 512 lanes, which leave 128 registers each: parameters are read again for each token, and no token ahead.
-template <typename TX, typename TH, bool GATES, bool LARGE, Rows ROWS>
+template <typename TX, typename TH, bool GATES, bool LARGE, Rows ROWS, bool WAVES>
 __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad_kernel(Residual a, ResidualBackward f, GradPlan g, int of_team, unsigned m_chunks,
                                                                  float *__restrict__ parts) {
     __shared__ float2 s_place[2][kMaxTeam / kWave];
@@ -30,41 +30,36 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
     const unsigned teams = LARGE ? 1 : blockDim.x / team, mine = LARGE ? 0 : threadIdx.x / team;
     unsigned first, last, gate_row = 0;
     if constexpr (GATES) {
-        first = (blockIdx.x * teams + mine) * g.each;
+        first = token<WAVES>((blockIdx.x * teams + mine) * g.each);
         last = min(first + g.each, a.rows);
         gate_row = first / a.gate_rows;
     } else {
         const unsigned group = fast_div_any(blockIdx.x, g.chunks, m_chunks), chunk = blockIdx.x - group * g.chunks;
         const unsigned end = min(chunk * g.rows + g.rows, a.gate_rows);
-        first = group * a.gate_rows + min(chunk * g.rows + mine * g.each, end);
+        first = token<WAVES>(group * a.gate_rows + min(chunk * g.rows + mine * g.each, end));
         last = min(first + g.each, group * a.gate_rows + end);
         gate_row = group;
     }
     const TX *const xo = static_cast<const TX *>(f.xo), *const dxo = static_cast<const TX *>(f.dxo);
     const TH *const h = static_cast<const TH *>(f.h);
     // A token's values, raw: the next one's are on their way while this one's are worked on.
-    RawAny r_dz{};
+    Raw32 r_dz{};
     Raw<TX, 8> r_xo{}, r_dxo{};
     Raw<TH, 8> r_h{};
     float4 r_st = make_float4(0.f, 1.f, 0.f, 1.f);
-    const auto load_norm = [&](unsigned row, bool there) {
-        const size_t r = there ? row : 0;
-        if (there) r_st = *reinterpret_cast<const float4 *>(f.stats + r * 4);
-        if (f.dz) {
-            r_dz = fetch_any<ROWS>(f.dz, f.dz_dtype, r * f.lddz, at, there);
-            r_xo = fetch_some<ROWS>(xo + r * f.ldxo, at, there);
-        }
+    // (of a token that is there; tensors that are not are read somewhere else, and not used)
+    const auto load_norm = [&](unsigned row) {
+        const size_t r = min(row, a.rows - 1);
+        r_st = *reinterpret_cast<const float4 *>(f.stats + r * 4);
+        r_dz = fetch_any<ROWS>(f.dz, f.dz_dtype, r * f.lddz, at);
+        r_xo = fetch_some<ROWS>(xo + r * f.ldxo, at);
     };
-    const auto load_stream = [&](unsigned row, bool there) {
-        if (f.dxo) r_dxo = fetch_some<ROWS>(dxo + (there ? row : 0) * f.lddxo, at, there);
-    };
-    const auto load_h = [&](unsigned row, bool there) {
-        if (f.h) r_h = fetch_some<ROWS>(h + (there ? row : 0) * f.ldh, at, there);
-    };
+    const auto load_stream = [&](unsigned row) { r_dxo = fetch_some<ROWS>(dxo + (size_t)min(row, a.rows - 1) * f.lddxo, at); };
+    const auto load_h = [&](unsigned row) { r_h = fetch_some<ROWS>(h + (size_t)min(row, a.rows - 1) * f.ldh, at); };
     if constexpr (!LARGE) {
-        load_norm(first, first < last);
-        load_stream(first, first < last);
-        load_h(first, first < last);
+        load_norm(first);
+        load_stream(first);
+        load_h(first);
     }
     const float inv = 1.f / (float)a.cols;
     const bool centre1 = a.post == kNormLayer, centre2 = a.pre == kNormLayer;
@@ -84,15 +79,7 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
     };
     if constexpr (!LARGE)
         if (!GATES || first < last) new_gate();
-    float sa[8] = {}, sb[8] = {}, sg2[LARGE ? 1 : 8] = {}, sb2[LARGE ? 1 : 8] = {}, sg1[GATES && !LARGE ? 8 : 1] = {}, sb1[GATES && !LARGE ? 8 : 1] = {};
-    // (a large team keeps the sums over gates, and dg2 and db2, in LDS)
-    __shared__ float s_gates[LARGE && GATES ? 16 : 1][kMaxTeam], s_pre[LARGE ? 16 : 1][kMaxTeam];
-    if constexpr (LARGE)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            s_pre[e][threadIdx.x] = 0.f;
-            if constexpr (GATES) s_gates[e][threadIdx.x] = 0.f;
-        }
+    float sa[8] = {}, sb[8] = {}, sg2[8] = {}, sb2[8] = {}, sg1[GATES ? 8 : 1] = {}, sb1[GATES ? 8 : 1] = {};
     // A gate's tokens are through: its gradient, and what its sums are to the parameters'.
     const auto end_gate = [&](float (&dgate)[8], float (&dg1)[8], float (&db1)[8]) {
         float gate[8], g1[8], b1[8];
@@ -117,24 +104,21 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
     for (unsigned k = 0; k < g.each; ++k) {                     // as often in every team: there are barriers
         const unsigned row = first + k;
         const bool there = row < last;
-        asm volatile("" : "+v"(at.at));         // (no address of a lane's own is kept over tokens: two registers for each tensor)
-        if constexpr (LARGE) load_norm(row, there);
+        asm volatile("" : "+v"(at.at), "+v"(at.start));     // (no address of a lane's own is kept over tokens: two registers for each tensor)
+        if constexpr (LARGE) load_norm(row);
         const float4 st = there ? r_st : make_float4(0.f, 1.f, 0.f, 1.f);
         const int n = there ? at.n : 0;
         float dv[8] = {}, d[8] = {}, xh[8], hh[8];
-        if (f.dz) {
-            widen_any<ROWS>(r_dz, f.dz_dtype, at, dv);
-            widen_some<ROWS>(r_xo, at, xh);
-        }
+        widen_any<ROWS>(r_dz, f.dz_dtype, at, dv, there && f.has_dz);
+        widen_some<ROWS>(r_xo, at, xh, there);
         if constexpr (!LARGE) {
-            if (f.dxo) widen_some<ROWS>(r_dxo, at, d);
-            if (f.h) widen_some<ROWS>(r_h, at, hh);
-            const bool more = k + 1 < g.each && row + 1 < last;
-            load_norm(row + 1, more);
-            load_stream(row + 1, more);
-            load_h(row + 1, more);
+            widen_some<ROWS>(r_dxo, at, d, there && f.has_dxo);
+            widen_some<ROWS>(r_h, at, hh, there);
+            load_norm(row + 1);
+            load_stream(row + 1);
+            load_h(row + 1);
         }
-        if (f.dz) {
+        if (f.has_dz) {
             if constexpr (LARGE) pre_params();
             phase();
             float2 s = make_float2(0.f, 0.f);
@@ -153,29 +137,24 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if constexpr (LARGE) {
-                    s_pre[e][threadIdx.x] = fmaf(dv[e], xh[e], s_pre[e][threadIdx.x]);
-                    s_pre[8 + e][threadIdx.x] += dv[e];
-                } else {
-                    sg2[e] = fmaf(dv[e], xh[e], sg2[e]);
-                    sb2[e] += dv[e];
-                }
+                sg2[e] = fmaf(dv[e], xh[e], sg2[e]);
+                sb2[e] += dv[e];
                 t[e] = g2[e] * dv[e];
                 s.x += t[e];
                 s.y = fmaf(t[e], xh[e], s.y);
             }
-            s = team_sum(s, team, sums);
+            s = team_sum<WAVES>(s, team, sums);
             const float m = centre2 ? s.x * inv : 0.f, c = s.y * inv;
             phase();
             if constexpr (LARGE) {
-                load_stream(row, there);
-                if (f.dxo) widen_some<ROWS>(r_dxo, at, d);
+                load_stream(row);
+                widen_some<ROWS>(r_dxo, at, d, there && f.has_dxo);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = fmaf(st.w, t[e] - m - xh[e] * c, d[e]);
         } else if constexpr (LARGE) {
-            load_stream(row, there);
-            if (f.dxo) widen_some<ROWS>(r_dxo, at, d);
+            load_stream(row);
+            widen_some<ROWS>(r_dxo, at, d, there && f.has_dxo);
         }
         phase();
         if (there) {
@@ -184,12 +163,12 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             for (int e = 0; e < 8; ++e) out[e] = a.scale * d[e];
             store_some<ROWS>(static_cast<TX *>(f.dx) + row * f.lddx, at, out, f.past);
         }
-        if (f.h) {
+        if (f.has_h) {
             if (a.drop.limit) drop_some(a.drop, call, row, lane, d);
             phase();
             if constexpr (LARGE) {
-                load_h(row, there);
-                widen_some<ROWS>(r_h, at, hh);
+                load_h(row);
+                widen_some<ROWS>(r_h, at, hh, there);
                 if (there) new_gate();
             }
             phase();
@@ -206,7 +185,7 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
                 s.y = fmaf(q[e], hh[e], s.y);
             }
             if (a.post != kNormNone) {
-                s = team_sum(s, team, sums);
+                s = team_sum<WAVES>(s, team, sums);
                 const float m = centre1 ? s.x * inv : 0.f, c = s.y * inv;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) q[e] = st.y * (q[e] - m - hh[e] * c);
@@ -220,11 +199,7 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
                     end_gate(dgate, dg1, db1);
                     if (f.dgate) store_some<ROWS>(f.dgate + (size_t)gate_row * a.cols, at, dgate);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if constexpr (LARGE) s_gates[e][threadIdx.x] += dg1[e], s_gates[8 + e][threadIdx.x] += db1[e];
-                        else sg1[e] += dg1[e], sb1[e] += db1[e];
-                        sa[e] = sb[e] = 0.f;
-                    }
+                    for (int e = 0; e < 8; ++e) sg1[e] += dg1[e], sb1[e] += db1[e], sa[e] = sb[e] = 0.f;
                     ++gate_row;
                     if constexpr (!LARGE)
                         if (row + 1 < last) new_gate();
@@ -236,10 +211,7 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
     float dgate[8], dg1[8], db1[8];
     if constexpr (GATES) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (LARGE) dg1[e] = s_gates[e][threadIdx.x], db1[e] = s_gates[8 + e][threadIdx.x];
-            else dg1[e] = sg1[e], db1[e] = sb1[e];
-        }
+        for (int e = 0; e < 8; ++e) dg1[e] = sg1[e], db1[e] = sb1[e];
     } else
         end_gate(dgate, dg1, db1);
     // The teams' sums as one part of the block, a kind at a time.
@@ -260,14 +232,8 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
     float *part = parts + (size_t)blockIdx.x * kSums * a.cols;
     if (f.dpost_gamma) leave(dg1, part);
     if (f.dpost_beta) leave(db1, part + a.cols);
-    float dg2[8], db2[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if constexpr (LARGE) dg2[e] = s_pre[e][threadIdx.x], db2[e] = s_pre[8 + e][threadIdx.x];
-        else dg2[e] = sg2[e], db2[e] = sb2[e];
-    }
-    if (f.dpre_gamma) leave(dg2, part + 2 * a.cols);
-    if (f.dpre_beta) leave(db2, part + 3 * a.cols);
+    if (f.dpre_gamma) leave(sg2, part + 2 * a.cols);
+    if (f.dpre_beta) leave(sb2, part + 3 * a.cols);
     if (!GATES && f.dgate) leave(dgate, g.chunks == 1 ? f.dgate + (size_t)gate_row * a.cols : part + 4 * a.cols);
 }
 
@@ -333,11 +299,18 @@ hipError_t launch_residual_grad(const Residual &a, ResidualBackward f, void *ws,
         clear(f.dgate, (size_t)a.gates * a.cols);
         return hipGetLastError();
     }
+    // (what is not there: the row's place of something that is, again and again)
+    f.has_dz = f.dz != nullptr, f.has_dxo = f.dxo != nullptr, f.has_h = f.h != nullptr;
+    const void *const some = f.dxo ? f.dxo : f.xo;
+    if (!f.xo) f.xo = some, f.ldxo = 0;
+    if (!f.dxo) f.dxo = some, f.lddxo = 0;
+    if (!f.dz) f.dz = some, f.lddz = 0, f.dz_dtype = f.x_dtype;
+    if (!f.h) f.h = some, f.ldh = 0, f.h_dtype = f.x_dtype;
     const TeamGrid g = team_grid(a.cols, 8);
     const GradPlan p = plan_grad(a, g);
     float *parts = static_cast<float *>(ws);
     f.past = (size_t)a.rows * a.cols * 2 >= kPastCaches && (f.x_dtype == GSPC_F32 || whole_pieces(f.dx, a.cols * 2, f.lddx * 2)) &&
-             (!f.h || f.h_dtype == GSPC_F32 || whole_pieces(f.dh, a.cols * 2, f.lddh * 2));
+             (!f.has_h || f.h_dtype == GSPC_F32 || whole_pieces(f.dh, a.cols * 2, f.lddh * 2));
     const auto run = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3(p.blocks), dim3(g.threads), 0, s, a, f, p, g.team, div_magic(p.chunks ? p.chunks : 1), parts);
     };
@@ -345,9 +318,12 @@ hipError_t launch_residual_grad(const Residual &a, ResidualBackward f, void *ws,
         typedef decltype(x) TX;
         typedef decltype(h) TH;
         constexpr bool GATES = decltype(gates)::value;
-        if (g.team > kMaxTeam / 2) run(residual_grad_kernel<TX, TH, GATES, true, kRagged>);
-        else if (a.cols % 8 == 0) run(residual_grad_kernel<TX, TH, GATES, false, kWhole>);
-        else run(residual_grad_kernel<TX, TH, GATES, false, kThin>);
+        const Rows kind = rows_of(a.cols);
+        if (g.team > kMaxTeam / 2) run(residual_grad_kernel<TX, TH, GATES, true, kRagged, true>);
+        else if (g.team >= kWave) kind == kWhole ? run(residual_grad_kernel<TX, TH, GATES, false, kWhole, true>) : run(residual_grad_kernel<TX, TH, GATES, false, kRagged, true>);
+        else if (kind == kWhole) run(residual_grad_kernel<TX, TH, GATES, false, kWhole, false>);
+        else if (kind == kRagged) run(residual_grad_kernel<TX, TH, GATES, false, kRagged, false>);
+        else run(residual_grad_kernel<TX, TH, GATES, false, kThin, false>);
     };
     const auto by_types = [&](auto gates) {
         if (f.x_dtype == GSPC_F32) f.h_dtype == GSPC_F32 ? of(0.f, 0.f, gates) : of(0.f, uint16_t(), gates);

@@ -6,19 +6,20 @@ namespace gspc {
 
 // A team keeps its parameters and walks down consecutive tokens; the next token's values are on their way while this one's are worked on.  Bound by
 // memory where there are many tokens: x and h in, x' and z out.  H: there is an h.
-template <typename TX, typename TH, bool H, Rows ROWS>
+template <typename TX, typename TH, bool H, Rows ROWS, bool WAVES>
 __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, ResidualForward f, int team, unsigned each, unsigned m_gate) {
     __shared__ float2 s_place[2][kMaxTeam / kWave];
     TeamSums sums{s_place, 0};
     const int lane = threadIdx.x & (team - 1), seg = lane / kWave;
-    const Place at = place_of(lane * 8, a.cols);
-    const unsigned first = ((size_t)blockIdx.x * (blockDim.x / team) + threadIdx.x / team) * each;
-    const unsigned last = min(first + each, a.rows);            // (fewer than 2^32)
+    Place at = place_of(lane * 8, a.cols);
+    const unsigned first = token<WAVES>((blockIdx.x * (blockDim.x / team) + threadIdx.x / team) * each);    // (fewer than 2^32)
+    const unsigned last = min(first + each, a.rows);
     const TX *x = static_cast<const TX *>(f.x);
     const TH *h = static_cast<const TH *>(f.h);
-    Raw<TX, 8> rx = fetch_some<ROWS>(x + (first < last ? first * f.ldx : 0), at, first < last);
+    const auto some_row = [&](unsigned row) { return (size_t)min(row, a.rows - 1); };       // (one that is there)
+    Raw<TX, 8> rx = fetch_some<ROWS>(x + some_row(first) * f.ldx, at);
     Raw<TH, 8> rh{};
-    if constexpr (H) rh = fetch_some<ROWS>(h + (first < last ? first * f.ldh : 0), at, first < last);
+    if constexpr (H) rh = fetch_some<ROWS>(h + some_row(first) * f.ldh, at);
     float g1[8], b1[8], g2[8], b2[8], gate[8];                  // (gate: times what makes up for the dropped)
     if constexpr (H) {
         some_params<ROWS>(a.post_gamma, at, 1.f, g1);
@@ -31,18 +32,18 @@ __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, Res
     for (unsigned k = 0; k < each; ++k) {                       // as often in every team: there are barriers
         const unsigned row = first + k;
         const bool there = row < last;
+        asm volatile("" : "+v"(at.at), "+v"(at.start));     // (no address of a lane's own is kept over tokens: two registers for each tensor)
         float v[8], u[8];
         float2 st1 = make_float2(0.f, 1.f), st2 = make_float2(0.f, 1.f);
         widen_some<ROWS>(rx, at, v);
         if constexpr (H) widen_some<ROWS>(rh, at, u);
-        const bool more = k + 1 < each && row + 1 < last;
-        rx = fetch_some<ROWS>(x + (more ? (row + 1) * f.ldx : 0), at, more);
-        if constexpr (H) rh = fetch_some<ROWS>(h + (more ? (row + 1) * f.ldh : 0), at, more);
+        rx = fetch_some<ROWS>(x + some_row(row + 1) * f.ldx, at);
+        if constexpr (H) rh = fetch_some<ROWS>(h + some_row(row + 1) * f.ldh, at);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= a.scale;
         if constexpr (H) {
             if (a.post != kNormNone) {
-                st1 = team_stats<ROWS>(u, at.n, a.cols, a.post, a.eps, team, seg, sums);
+                st1 = team_stats<ROWS, WAVES>(u, at.n, a.cols, a.post, a.eps, team, seg, sums);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[e] = fmaf((u[e] - st1.x) * st1.y, g1[e], b1[e]);
             }
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, Res
         }
         if (there && f.xo) store_some<ROWS>(static_cast<TX *>(f.xo) + row * f.ldxo, at, v, f.past);
         if (a.pre != kNormNone) {
-            st2 = team_stats<ROWS>(v, at.n, a.cols, a.pre, a.eps, team, seg, sums);
+            st2 = team_stats<ROWS, WAVES>(v, at.n, a.cols, a.pre, a.eps, team, seg, sums);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = fmaf((v[e] - st2.x) * st2.y, g2[e], b2[e]);
             activate_all(a.act, v);
@@ -86,12 +87,12 @@ __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, Res
 hipError_t launch_residual_norm(const Residual &a, ResidualForward f, hipStream_t s) {
     const TeamGrid g = team_grid(a.cols, f.z_dtype == GSPC_F8 ? 16 : 8);
     // tokens of a team: as few as keep every compute unit full
-    const size_t teams = (size_t)(256 * (f.h ? 16 : 24) * kWave / g.threads) * g.teams;
+    const size_t teams = (size_t)(256 * (f.h ? 16 : 28) * kWave / g.threads) * g.teams;
     const unsigned each = (unsigned)((a.rows + teams - 1) / teams), of_block = each * g.teams;
     const unsigned blocks = (a.rows - 1) / of_block + 1;
     f.past = (size_t)a.rows * a.cols * 2 >= kPastCaches && (!f.xo || f.x_dtype == GSPC_F32 || whole_pieces(f.xo, a.cols * 2, f.ldxo * 2)) &&
              (f.z_dtype != GSPC_BF16 || whole_pieces(f.z, a.cols * 2, f.ldz * 2));
-    const bool full = a.cols % 8 == 0;
+    const Rows kind = rows_of(a.cols);
     const auto run = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3(blocks), dim3(g.threads), 0, s, a, f, g.team, each, div_magic(a.gate_rows));
         return hipGetLastError();
@@ -100,7 +101,9 @@ hipError_t launch_residual_norm(const Residual &a, ResidualForward f, hipStream_
         typedef decltype(x) TX;
         typedef decltype(h) TH;
         constexpr bool H = decltype(has)::value;
-        return full ? run(residual_norm_kernel<TX, TH, H, kWhole>) : run(residual_norm_kernel<TX, TH, H, kThin>);
+        if (g.team >= kWave) return kind == kWhole ? run(residual_norm_kernel<TX, TH, H, kWhole, true>) : run(residual_norm_kernel<TX, TH, H, kRagged, true>);
+        return kind == kWhole ? run(residual_norm_kernel<TX, TH, H, kWhole, false>)
+             : kind == kRagged ? run(residual_norm_kernel<TX, TH, H, kRagged, false>) : run(residual_norm_kernel<TX, TH, H, kThin, false>);
     };
     const std::true_type yes;
     const std::false_type no;

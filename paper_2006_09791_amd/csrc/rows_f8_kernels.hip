@@ -56,11 +56,11 @@ __global__ __launch_bounds__(512) void quantize_f8_turned_kernel(const T *__rest
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const unsigned row = r0 + ty * 4 + i;
-        raw[i] = fetch_some<ROWS>(x + (size_t)min(row, rows - 1) * ldx, some, row < rows);
+        raw[i] = fetch_some<ROWS>(x + (size_t)min(row, rows - 1) * ldx, some);
     }
     float v[4][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) widen_some<ROWS>(raw[i], some, v[i]);
+    for (int i = 0; i < 4; ++i) widen_some<ROWS>(raw[i], some, v[i], r0 + ty * 4 + i < rows);
     if (q) {
         const size_t pitch = (size_t)blocks * kBlock8, s_pitch = f8_scale_pitch(cols);
 #pragma unroll
@@ -132,9 +132,10 @@ template <typename F> static hipError_t by_rows(size_t rows, int blocks, const F
 template <typename T> static hipError_t quantize(const QuantizeF8 &a, hipStream_t s) {
     const T *x = static_cast<const T *>(a.x);
     const int pitch = f8_pitch(a.cols), blocks = pitch / kBlock8, s_pitch = f8_scale_pitch(a.cols);
-    const bool full = a.cols % 8 == 0;
-    const auto rows_only = full ? quantize_f8_kernel<T, kWhole> : quantize_f8_kernel<T, kThin>;
-    const auto turned = full ? quantize_f8_turned_kernel<T, kWhole> : quantize_f8_turned_kernel<T, kThin>;
+    const Rows kind = rows_of(a.cols);
+    const auto rows_only = kind == kWhole ? quantize_f8_kernel<T, kWhole> : kind == kRagged ? quantize_f8_kernel<T, kRagged> : quantize_f8_kernel<T, kThin>;
+    const auto turned = kind == kWhole ? quantize_f8_turned_kernel<T, kWhole>
+                      : kind == kRagged ? quantize_f8_turned_kernel<T, kRagged> : quantize_f8_turned_kernel<T, kThin>;
     if (!a.qt)
         return by_rows(a.rows, blocks, [&](size_t at, unsigned units, dim3 grid) {
             hipLaunchKernelGGL(rows_only, grid, dim3(256), 0, s, x + at * a.ldx, a.ldx, units, a.cols, blocks, div_magic(blocks),
@@ -151,7 +152,7 @@ template <typename T>
 static hipError_t dequantize(const uint8_t *q, const uint8_t *scale, size_t rows, int cols, T *x, size_t ldx, hipStream_t s) {
     const int pitch = f8_pitch(cols), blocks = pitch / kBlock8, s_pitch = f8_scale_pitch(cols);
     const int past = sizeof(T) == 2 && rows * cols * 2 >= kPastCaches && whole_pieces(x, cols * sizeof(T), ldx * sizeof(T));
-    const auto kern = cols % 8 == 0 ? dequantize_f8_kernel<T, kWhole> : dequantize_f8_kernel<T, kThin>;
+    const auto kern = cols % 8 == 0 ? dequantize_f8_kernel<T, kWhole> : dequantize_f8_kernel<T, kRagged>;
     return by_rows(rows, blocks, [&](size_t at, unsigned units, dim3 grid) {
         hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, q + at * pitch, scale + at * s_pitch, units, cols, blocks, div_magic(blocks),
                            x + at * ldx, ldx, past);

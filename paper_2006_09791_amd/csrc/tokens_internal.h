@@ -138,7 +138,7 @@ struct ResidualBackward {
     void *dh;
     size_t lddh;
     float *dgate, *dpost_gamma, *dpost_beta, *dpre_gamma, *dpre_beta;       // any may be nullptr
-    int past;
+    int past, has_dz, has_dxo, has_h;   // (set by the launch)
 };
 size_t residual_grad_bytes(const Residual &a);
 hipError_t launch_residual_norm(const Residual &a, ResidualForward f, hipStream_t s);
