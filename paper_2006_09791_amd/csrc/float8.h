@@ -22,10 +22,19 @@ __device__ __forceinline__ float block_up(unsigned code) { return __uint_as_floa
 __device__ __forceinline__ float block_down(unsigned code) {
     return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7fc00000u : code << 23);
 }
-// A magnitude where it is finite, else 0: what is not finite has no say in its block's power of two.
-__device__ __forceinline__ unsigned finite_magnitude(float v) {
-    const unsigned m = magnitude(v);
-    return m < 0x7f800000u ? m : 0u;
+// The largest finite magnitude of some values: what is not finite has no say in its block's power of two.  (The maximum drops what is no number by itself,
+// three magnitudes an instruction; values are looked at one by one only where it is an infinity.)
+template <int N> __device__ __forceinline__ unsigned top_of(const float (&v)[N]) {
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = fmaxf(top, fabsf(v[e]));
+    unsigned m = __float_as_uint(top);
+    if (m == 0x7f800000u) {
+        m = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = max(m, magnitude(v[e]) < 0x7f800000u ? magnitude(v[e]) : 0u);
+    }
+    return m;
 }
 // Four codes, to nearest, ties to even; infinities and what is no number become no number.
 __device__ __forceinline__ unsigned f8_word(float a, float b, float c, float d) {
@@ -41,13 +50,6 @@ __device__ __forceinline__ void f8_values(u32x2 q, float (&v)[8]) {
         v[4 * i] = lo[0], v[4 * i + 1] = lo[1], v[4 * i + 2] = hi[0], v[4 * i + 3] = hi[1];
     }
 }
-__device__ __forceinline__ unsigned top_of(const float (&v)[8]) {
-    unsigned top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, finite_magnitude(v[e]));
-    return top;
-}
-
 // Eight columns of a row from `at` on, of which the first n (8, fewer at the row's end, or none) are there.  In rows of whole eights (kWhole) n is 8 or
 // 0.  What is there at the end of others (kRagged) is read as the row's last eight columns, in one access, and moved to its place when it is widened;
 // rows of fewer than eight columns (kThin) are read one by one.  Lanes without a column read the row's first ones: no load hangs on a branch, behind

@@ -39,6 +39,16 @@ template <bool WAVES> __device__ __forceinline__ float2 wave_sum(float2 v, int t
     if constexpr (WAVES) return sums(std::integral_constant<int, 64>());
     else return team == 32 ? sums(std::integral_constant<int, 32>()) : team == 16 ? sums(std::integral_constant<int, 16>()) : sums(std::integral_constant<int, 8>());
 }
+// A sum over the teams of a wave, of 8, 16 or 32 lanes: of the lanes that have the same columns.
+__device__ __forceinline__ float sum_across(float v, int team) {
+    if (team == 8) v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));     // row_ror: lane ^ 8
+    if (team <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 // What the other waves of the team have: lane l of the first sixteen that of wave l, 0 where there is none.
 __device__ __forceinline__ float2 team_exchange(float2 v, int team, TeamSums &t) {
     const int waves = team / kWave, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;

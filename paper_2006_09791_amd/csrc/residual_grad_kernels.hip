@@ -214,18 +214,22 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
         for (int e = 0; e < 8; ++e) dg1[e] = sg1[e], db1[e] = sb1[e];
     } else
         end_gate(dgate, dg1, db1);
-    // The teams' sums as one part of the block, a kind at a time.
-    const auto leave = [&](const float (&v)[8], float *to) {
-        if (teams == 1) {
+    // The teams' sums as one part of the block, a kind at a time: those of a wave's teams by lanes, then waves through LDS.
+    const auto leave = [&](float (&v)[8], float *to) {
+        if constexpr (!WAVES)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = sum_across(v[e], team);
+        const int width = WAVES ? team * 8 : kWave * 8, places = WAVES ? (int)teams : kTeamThreads / kWave;
+        if (places == 1) {
             store_some<ROWS>(to, at, v);
             return;
         }
         __syncthreads();
-        store(s_sum + mine * team * 8 + at.at, v);
+        if (WAVES || threadIdx.x % kWave < (unsigned)team) store(s_sum + (WAVES ? mine : threadIdx.x / kWave) * width + lane * 8, v);
         __syncthreads();
         for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
-            float sum = s_sum[c];
-            for (unsigned k = 1; k < teams; ++k) sum += s_sum[k * team * 8 + c];
+            float sum = s_sum[c] + s_sum[width + c];
+            if (places == 4) sum += s_sum[2 * width + c] + s_sum[3 * width + c];
             to[c] = sum;
         }
     };
@@ -249,8 +253,15 @@ __global__ __launch_bounds__(1024) void residual_join_kernel(const float *__rest
     const unsigned first = kind < 4 ? 0 : gate * chunks, count = kind < 4 ? blocks : chunks;
     const float *p = parts + ((size_t)first * kSums + min(kind, 4u)) * cols + min(c, cols - 1);
     double sum = 0;
-#pragma unroll 4
-    for (unsigned k = slice; k < count; k += 16) sum += p[(size_t)k * kSums * cols];
+    unsigned k = slice;
+    for (; k + 112 < count; k += 128) {             // eight on their way at once
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[(size_t)(k + 16 * i) * kSums * cols];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i];
+    }
+    for (; k < count; k += 16) sum += p[(size_t)k * kSums * cols];
     s_sum[slice][lane] = sum;
     __syncthreads();
     if (slice != 0 || c >= cols) return;
@@ -263,6 +274,8 @@ __global__ __launch_bounds__(256) void residual_clear_kernel(float *p, size_t co
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)gridDim.x * 256) p[i] = 0.f;
 }
 
+static_assert(kTeamThreads == 4 * kWave, "a block's teams are in one, two or four waves");
+
 static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
     const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 256 * 12 * kWave / t.threads;
     GradPlan p;
@@ -273,8 +286,8 @@ static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
         p.blocks = (unsigned)(((size_t)rows - 1) / ((size_t)p.each * t.teams) + 1);
         return p;
     }
-    // blocks of a gate: until there are enough of them, of two tokens a team at least, and 1024 at most
-    const unsigned most = (gate_rows - 1) / (2 * t.teams) + 1, least = (gate_rows - 1) / (1024 * t.teams) + 1;
+    // blocks of a gate: until there are enough of them, of 1024 tokens a team at most
+    const unsigned most = (gate_rows - 1) / t.teams + 1, least = (gate_rows - 1) / (1024 * t.teams) + 1;
     unsigned want = wanted / gates;
     if (want > most) want = most;
     if (want < least) want = least;

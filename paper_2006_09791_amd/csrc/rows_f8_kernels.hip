@@ -78,7 +78,8 @@ __global__ __launch_bounds__(512) void quantize_f8_turned_kernel(const T *__rest
     if (!qt) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {                       // over the four rows of lanes of the wave
-        const unsigned mine = max(max(finite_magnitude(v[0][e]), finite_magnitude(v[1][e])), max(finite_magnitude(v[2][e]), finite_magnitude(v[3][e])));
+        const float column[4] = {v[0][e], v[1][e], v[2][e], v[3][e]};
+        const unsigned mine = top_of(column);
         const auto a = __builtin_amdgcn_permlane16_swap(mine, mine, false, false);
         const unsigned m = max((unsigned)a[0], (unsigned)a[1]);
         const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
