@@ -71,35 +71,46 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
     const unsigned row = lane % 16, lane_off = row * p.pitch + lane / 16 * 16, lane_scale = row * p.s_pitch;
     const int begin = (int)part * p.stretch, end = min(begin + p.stretch, p.pitch / kBlock8), share = (end - begin + WAVES - 1) / WAVES;
     const int first = begin + wave * share, last = min(first + share, end);
+    static_assert(TN * TM <= WAVES, "a wave joins one product at most");
+    float bias[4] = {};                             // (on its way with the operands, not behind them)
+    if (p.bias && wave < TN * TM)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[e] = p.bias[min(n0 + wave / TM * 16 + lane / 16 * 4 + e, p.N - 1)];
     f32x4 acc[TN][TM] = {};
     u32x4 w[DEEP][TN][2], a[DEEP][TM][2];
-    unsigned sw[DEEP][TN], sa[DEEP][TM];
+    static_assert(DEEP <= 4, "DEEP steps' bytes are in two words");
+    uint64_t sw[TN], sa[TM], next_sw[TN], next_sa[TM];
+    const auto load_scales = [&](int step) {        // of this and the next DEEP - 1 steps, whatever their place in their words
+        const unsigned s = step & ~3;
+#pragma unroll
+        for (int i = 0; i < TN; ++i) next_sw[i] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(rsw, lane_scale + i * 16 * p.s_pitch + s, 0, 0));
+#pragma unroll
+        for (int j = 0; j < TM; ++j) next_sa[j] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(rsa, lane_scale + j * 16 * p.s_pitch + s, 0, 0));
+    };
     const auto load = [&](int d, int step) {
-        const unsigned k = step * kBlock8, s = step & ~3;       // four steps' bytes in a word
+        const unsigned k = step * kBlock8;
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
             const unsigned off = lane_off + i * 16 * p.pitch + k;
             w[d][i][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off, 0, 0));
             w[d][i][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off + 64, 0, 0));
-            sw[d][i] = __builtin_amdgcn_raw_buffer_load_b32(rsw, lane_scale + i * 16 * p.s_pitch + s, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
             const unsigned off = lane_off + j * 16 * p.pitch + k;
             a[d][j][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off, 0, 0));
             a[d][j][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off + 64, 0, 0));
-            sa[d][j] = __builtin_amdgcn_raw_buffer_load_b32(rsa, lane_scale + j * 16 * p.s_pitch + s, 0, 0);
         }
     };
     const auto multiply = [&](int d, int step) {
-        const int turn = (step & 3) * 8;
+        const int turn = ((step & 3) + d) * 8;
         if constexpr (WIDE) {
             Wide ww[TN];
 #pragma unroll
-            for (int i = 0; i < TN; ++i) ww[i] = widened(both(w[d][i][0], w[d][i][1]), sw[d][i] >> turn);
+            for (int i = 0; i < TN; ++i) ww[i] = widened(both(w[d][i][0], w[d][i][1]), (unsigned)(sw[i] >> turn));
 #pragma unroll
             for (int j = 0; j < TM; ++j) {
-                const Wide aw = widened(both(a[d][j][0], a[d][j][1]), sa[d][j] >> turn);
+                const Wide aw = widened(both(a[d][j][0], a[d][j][1]), (unsigned)(sa[j] >> turn));
 #pragma unroll
                 for (int i = 0; i < TN; ++i)
 #pragma unroll
@@ -111,17 +122,23 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
 #pragma unroll
                 for (int j = 0; j < TM; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(w[d][i][0], w[d][i][1]), both(a[d][j][0], a[d][j][1]), acc[i][j], 0,
-                                                                                  0, 0, (int)(sw[d][i] >> turn), 0, (int)(sa[d][j] >> turn));
+                                                                                  0, 0, (int)(sw[i] >> turn), 0, (int)((unsigned)(sa[j] >> turn)));
         }
     };
+    load_scales(first);
 #pragma unroll
     for (int d = 0; d < DEEP; ++d)
         if (first + d < last) load(d, first + d);
     for (int step = first; step < last; step += DEEP) {
 #pragma unroll
+        for (int i = 0; i < TN; ++i) sw[i] = next_sw[i];
+#pragma unroll
+        for (int j = 0; j < TM; ++j) sa[j] = next_sa[j];
+        if (step + DEEP < last) load_scales(step + DEEP);
+#pragma unroll
         for (int d = 0; d < DEEP; ++d)
             if (step + d < last) {
-                multiply(d, step + d);
+                multiply(d, step);
                 if (step + d + DEEP < last) load(d, step + d + DEEP);
             }
     }
@@ -130,25 +147,24 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
 #pragma unroll
         for (int j = 0; j < TM; ++j) s_part[wave][i * TM + j][lane] = acc[i][j];
     __syncthreads();
-    for (int t = wave; t < TN * TM; t += WAVES) {
-        f32x4 sum = s_part[0][t][lane];
+    if (wave >= TN * TM) return;
+    f32x4 sum = s_part[0][wave][lane];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += s_part[v][t][lane];
-        const size_t m = m0 + t % TM * 16 + row;
-        const int n = n0 + t / TM * 16 + lane / 16 * 4;
-        if (m >= p.M || n >= p.N) continue;
-        float v[4];
+    for (int v = 1; v < WAVES; ++v) sum += s_part[v][wave][lane];
+    const size_t m = m0 + wave % TM * 16 + row;
+    const int n = n0 + wave / TM * 16 + lane / 16 * 4;
+    if (m >= p.M || n >= p.N) return;
+    float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = p.bias ? sum[e] + p.bias[min(n + e, p.N - 1)] : sum[e];
-        T *o = static_cast<T *>(p.out) + part * p.part + m * p.ldo + n;
-        if (n + 3 < p.N) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any *>(o) = (f32x4){v[0], v[1], v[2], v[3]};
-            else *reinterpret_cast<u32x2_any *>(o) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-        } else {
+    for (int e = 0; e < 4; ++e) v[e] = sum[e] + bias[e];
+    T *o = static_cast<T *>(p.out) + part * p.part + m * p.ldo + n;
+    if (n + 3 < p.N) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_any *>(o) = (f32x4){v[0], v[1], v[2], v[3]};
+        else *reinterpret_cast<u32x2_any *>(o) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    } else {
 #pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (n + e < p.N) put(o + e, v[e]);
-        }
+        for (int e = 0; e < 3; ++e)
+            if (n + e < p.N) put(o + e, v[e]);
     }
 }
 
@@ -375,24 +391,26 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     const int steps = f8_pitch(K) / kBlock8;
     const auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * (size_t)((N + bn - 1) / bn); };
     PlanF8 p;
-    // (M x K x N, us of a call among others, bf16 outputs; both sides)
+    // (M x K x N, us of a call among others, bf16 outputs unless said; both sides)
     //   256 x 256 from 160 tiles on: 12544 x 512 x 1024 has 196, 13.0 against 15.8 in tiles of 128; 2048 x 512 x 4096 has 128, 12.0 against 9.0.  Not
     //   for 128 tokens or filters and fewer, where more than half of a tile is empty;
-    //   128 x 128 from 192 tiles on: 1000 x 2000 x 3000 has 192, 13.4 against 13.7 in 64 x 128; 512 x 4096 x 4096 has 128, 19.9 against 16.0.  Four
+    //   128 x 128 from 192 tiles on: 1000 x 2000 x 3000 has 192, 13.4 against 13.7 in 64 x 128; 512 x 4096 x 4096 has 128, 20.3 against 16.0.  Four
     //   stages where a compute unit has one block: 2048 x 65536 x 2048, 340 against 507 with two; 12544 x 512 x 1024 (784 tiles), 23.6 against 15.8;
-    //   without staging where a block's steps, or those of all blocks, are few: 197 x 1280 x 1001, 5.0 against 7.2 in 64 x 128; 64 x 4096 x 4096, 13.4
-    //   against 12.0.  In 16 x 16 where these are few, too: 16 x 4096 x 4096, 8.0 against 11.6 in 32 x 32, 8 x 8192 x 8192, 19.2 against 15.9 in 64 x 128;
-    //   64 x 512 x 512, 2.6 against 3.1; 200 x 1024 x 1024 (832 blocks), 6.6 against 4.3.
-    const size_t small = tiles(16, 16);
+    //   without staging, in 16 x 16: for up to 16 tokens and 16384 filters (8 x 8192 x 8192, 15.0 against 16.5 in 64 x 128 and stretches; 16 x 4096 x
+    //   32768, 36.0 against 33.7), or up to 256 blocks of up to 32 steps (64 x 512 x 512, 2.6 against 3.2 in 32 x 32; 256 x 1024 x 1024, 6.7 against
+    //   4.4); and in 32 x 32 for up to 256 blocks of up to 32 steps (64 x 4096 x 4096, 10.4 against 12.5 in 64 x 128 and stretches; 64 x 8192 x 2048,
+    //   18.8 against 13.4), or more of few steps (5000 x 64 x 64, 3.7 against 4.2; operands as bf16 are widened for fewer products in 64 x 128, 256 x
+    //   2048 x 2048 to fp32, 11.8 against 13.2, to bf16 11.1 against 8.9).
+    const size_t small = tiles(16, 16), middle = tiles(32, 32);
     if (!wide && M > 128 && N > 128 && tiles(256, 256) >= 160) p = {kTile256, 256, 256, 512, 1, steps};
     else if (M > 64 && tiles(128, 128) >= 192) p = {tiles(128, 128) <= 256 ? kTile128Deep : kTile128, 128, 128, 256, 1, steps};
-    else if ((M <= 16 && tiles(64, 128) < 256 && small * steps <= 16384) || (small <= 256 && small * steps <= 2560)) p = {kSmall1, 16, 16, 512, 1, steps};
-    else if (tiles(32, 32) * steps <= 2560) p = {kSmall2, 32, 32, 512, 1, steps};
+    else if ((M <= 16 && tiles(64, 128) <= 128) || (small <= 256 && steps <= 32)) p = {kSmall1, 16, 16, 512, 1, steps};
+    else if ((middle <= 256 && steps <= 32) || (middle <= 640 && steps <= 2) || (wide && middle <= 512 && steps <= 16)) p = {kSmall2, 32, 32, 512, 1, steps};
     else p = {kTile64, 64, 128, 256, 1, steps};
     // Few blocks of a long sum: stretches of K, of 8 steps at least (32, where the block's waves share them), until every compute unit has a block.  512 x
-    // 12544 x 512 has 32 tiles: 36.1 whole, 15.0 in eight stretches and their join; 64 x 4096 x 4096, 14.4 and 12.0 in four.
+    // 12544 x 512 has 32 tiles: 36.0 whole, 15.4 in eight stretches and their join; 512 x 4096 x 4096 has 128, 16.0 and 22.9 in two.
     const size_t count = tiles(p.bm, p.bn);
-    if (count <= 128) {
+    if (count <= 64) {
         const int want = (int)(256 / count), most = steps / (p.kernel < kTile64 ? 32 : 8), parts = want < most ? want : most;
         if (parts > 1) {
             p.stretch = ((steps + parts - 1) / parts + 3) / 4 * 4;
