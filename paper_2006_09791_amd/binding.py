@@ -877,7 +877,7 @@ def gspc_residual_norm_backward(dz, dxo, xo, h, stats, gate=None, post=NORM_NONE
     like = xo if xo is not None else dxo
     if like is None:
         raise GspcError(-1, "neither xo nor dxo is given")
-    C, f32 = like.shape[-1], _f32()
+    C, f32 = _on_gpu(like, "xo").shape[-1], _f32()
     if C == 0:
         raise GspcError(-2, "xo has no channels")
     rows = like.numel() // C
