@@ -394,8 +394,9 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     // (M x K x N, us of a call among others, bf16 outputs unless said; both sides)
     //   256 x 256 from 160 tiles on: 12544 x 512 x 1024 has 196, 13.0 against 15.8 in tiles of 128; 2048 x 512 x 4096 has 128, 12.0 against 9.0.  Not
     //   for 128 tokens or filters and fewer, where more than half of a tile is empty;
-    //   128 x 128 from 192 tiles on: 1000 x 2000 x 3000 has 192, 13.4 against 13.7 in 64 x 128; 512 x 4096 x 4096 has 128, 20.3 against 16.0.  Four
-    //   stages where a compute unit has one block: 2048 x 65536 x 2048, 340 against 507 with two; 12544 x 512 x 1024 (784 tiles), 23.6 against 15.8;
+    //   128 x 128 from 192 tiles on: 1000 x 2000 x 3000 has 192, 11.9 against 13.0 in 64 x 128; 512 x 4096 x 4096 has 128, 17.3 against 16.3.  Four
+    //   stages and eight waves where a compute unit has one block: 1000 x 2000 x 3000, 11.9 against 13.7 with four waves and 15.2 with two stages, too;
+    //   12544 x 512 x 1024 (784 tiles), 20.1, 23.8 and 15.4.  Eight waves in 64 x 128 too: 400 x 1280 x 1001, 6.8 against 7.3 with four;
     //   without staging, in 16 x 16: for up to 16 tokens and 16384 filters (8 x 8192 x 8192, 15.0 against 16.5 in 64 x 128 and stretches; 16 x 4096 x
     //   32768, 36.0 against 33.7), or up to 256 blocks of up to 32 steps (64 x 512 x 512, 2.6 against 3.2 in 32 x 32; 256 x 1024 x 1024, 6.7 against
     //   4.4); and in 32 x 32 for up to 256 blocks of up to 32 steps (64 x 4096 x 4096, 10.4 against 12.5 in 64 x 128 and stretches; 64 x 8192 x 2048,
@@ -403,10 +404,10 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     //   2048 x 2048 to fp32, 11.8 against 13.2, to bf16 11.1 against 8.9).
     const size_t small = tiles(16, 16), middle = tiles(32, 32);
     if (!wide && M > 128 && N > 128 && tiles(256, 256) >= 160) p = {kTile256, 256, 256, 512, 1, steps};
-    else if (M > 64 && tiles(128, 128) >= 192) p = {tiles(128, 128) <= 256 ? kTile128Deep : kTile128, 128, 128, 256, 1, steps};
+    else if (M > 64 && tiles(128, 128) >= 192) p = {tiles(128, 128) <= 256 ? kTile128Deep : kTile128, 128, 128, tiles(128, 128) <= 256 ? 512 : 256, 1, steps};
     else if ((M <= 16 && tiles(64, 128) <= 128) || (small <= 256 && steps <= 32)) p = {kSmall1, 16, 16, 512, 1, steps};
     else if ((middle <= 256 && steps <= 32) || (middle <= 640 && steps <= 2) || (wide && middle <= 512 && steps <= 16)) p = {kSmall2, 32, 32, 512, 1, steps};
-    else p = {kTile64, 64, 128, 256, 1, steps};
+    else p = {kTile64, 64, 128, 512, 1, steps};
     // Few blocks of a long sum: stretches of K, of 8 steps at least (32, where the block's waves share them), until every compute unit has a block.  512 x
     // 12544 x 512 has 32 tiles: 36.0 whole, 15.4 in eight stretches and their join; 512 x 4096 x 4096 has 128, 16.0 and 22.9 in two.
     const size_t count = tiles(p.bm, p.bn);
@@ -451,8 +452,8 @@ template <typename T, bool WIDE> static void run_f8(const PlanF8 &plan, ProductF
     switch (plan.kernel) {
     case kSmall1: return run(product_f8_small_kernel<T, WIDE, 1, 1, 8, 4>, "product_f8_small<1,1>");
     case kSmall2: return run(product_f8_small_kernel<T, WIDE, 2, 2, 8, 2>, "product_f8_small<2,2>");
-    case kTile64: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 1, 2, 3>, "product_f8_tile<64,128>");
-    case kTile128Deep: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 2, 2, 4>, "product_f8_tile<128,128>");
+    case kTile64: return run(product_f8_tile_kernel<T, WIDE, 2, 4, 1, 1, 3>, "product_f8_tile<64,128>");
+    case kTile128Deep: return run(product_f8_tile_kernel<T, WIDE, 2, 4, 2, 1, 4>, "product_f8_tile<128,128>");
     case kTile128: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 2, 2, 2>, "product_f8_tile<128,128>");
     }
     if constexpr (sizeof(T) == 2)
