@@ -175,7 +175,8 @@ def load():
             lib.gspc_group_norm_backward, lib.gspc_matmul_i8)], torch.float32, torch.bfloat16, torch.int8)
         _gspc_call.bind_block(*[ctypes.cast(f, vp).value for f in (
             lib.gspc_quantize_rows_f8, lib.gspc_dequantize_rows_f8, lib.gspc_matmul_f8, lib.gspc_dropout, lib.gspc_residual_norm,
-            lib.gspc_residual_norm_backward)], torch.float8_e4m3fn, torch.uint8, torch.int64)
+            lib.gspc_residual_norm_backward, lib.gspc_matmul_f8_workspace_bytes, lib.gspc_residual_norm_backward_workspace_bytes)],
+            torch.float8_e4m3fn, torch.uint8, torch.int64)
         _conv, _fast = _gspc_call.conv, _gspc_call
     _lib = lib
     return lib
@@ -672,6 +673,11 @@ def gspc_f8_scale_pitch(cols):
     return gspc_f8_pitch(cols) and (cols + 511) // 512 * 4
 
 
+def _scratch_for(nbytes, like):
+    """A workspace for a call that is made through _gspc_call."""
+    return _scratch(nbytes, like.device)
+
+
 def _rows_f8(pair, rows, cols, what):
     import torch
     q, scale = pair
@@ -733,13 +739,8 @@ def gspc_matmul_f8_workspace_bytes(M, N, K):
 def gspc_matmul_f8(a, w, bias=None, out=None, dtype=GSPC_BF16, cols=None, workspace=None):
     """8-bit float rows a (M tokens) and w (N filters) of the same length -> [M, N]; `out`: a tensor [..., N] to write into.  cols: that length,
     checked against both; without it all of the rows' pitch is summed, whose padding is zero."""
-    if out is not None and _fast is not None:
-        rc = _fast.matmul_f8(a, w, bias, out, cols, workspace)
-        if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
-            need = gspc_matmul_f8_workspace_bytes(a[0].shape[0], w[0].shape[0], a[0].shape[-1])
-            rc = _fast.matmul_f8(a, w, bias, out, cols, _scratch(need, out.device))
-        if _done(rc):
-            return out
+    if out is not None and _fast is not None and _done(_fast.matmul_f8(a, w, bias, out, cols, workspace, _scratch_for)):
+        return out
     lib = load()
     K = a[0].shape[-1]
     if K == 0 or w[0].shape[-1] != K:
@@ -862,17 +863,10 @@ def gspc_residual_norm_backward(dz, dxo, xo, h, stats, gate=None, post=NORM_NONE
                                 dpost_gamma=None, dpost_beta=None, dpre_gamma=None, dpre_beta=None, workspace=None):
     """The gradient of gspc_residual_norm: dz, dxo (either may be None for zero), xo, h and stats of the forward call, and its other arguments ->
     ResidualGradients, None for what was not there.  dx is of xo's type and may be dxo itself, dh of h's and may be h itself."""
-    given = (dx, dh, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta)
-    if dx is not None and _fast is not None and all((g is None) == (v is None) for g, v in zip(
-            given[1:], (h, gate, post_gamma, post_beta, pre_gamma, pre_beta))):
-        call = lambda ws: _fast.residual_norm_backward(dz, dxo, xo, h, stats, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta,  # noqa: E731
-                                                       act, scale, drop, seed, offset, step, *given, ws)
-        rc = call(workspace)
-        if rc == -6 and workspace is None:  # GSPC_ERR_SPACE: a call that needs one
-            C = dx.shape[-1]
-            rc = call(_scratch(gspc_residual_norm_backward_workspace_bytes(dx.numel() // C, C, 1 if gate is None else gate.numel() // C), dx.device))
-        if _done(rc):
-            return ResidualGradients(*given)
+    if dx is not None and _fast is not None and \
+            _done(_fast.residual_norm_backward(dz, dxo, xo, h, stats, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, drop, seed,
+                                               offset, step, dx, dh, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta, workspace, _scratch_for)):
+        return ResidualGradients(dx, dh, dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta)
     lib = load()
     like = xo if xo is not None else dxo
     if like is None:

@@ -331,16 +331,18 @@ static struct {
     dropout_fn dropout;
     residual_norm_fn residual_norm;
     residual_norm_backward_fn residual_norm_backward;
+    size_t (*matmul_bytes)(int64_t, int, int);
+    size_t (*residual_norm_backward_bytes)(int64_t, int, int64_t);
 } g_block;
 
 static PyObject *bind_block(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
-    if (n != 9) {
-        PyErr_SetString(PyExc_TypeError, "six addresses and three types");
+    if (n != 11) {
+        PyErr_SetString(PyExc_TypeError, "eight addresses and three types");
         return NULL;
     }
-    void *p[6];
-    for (int i = 0; i < 6; ++i) {
+    void *p[8];
+    for (int i = 0; i < 8; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i] && PyErr_Occurred()) return NULL;
     }
@@ -350,9 +352,11 @@ static PyObject *bind_block(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     g_block.dropout = (dropout_fn)p[3];
     g_block.residual_norm = (residual_norm_fn)p[4];
     g_block.residual_norm_backward = (residual_norm_backward_fn)p[5];
+    g_block.matmul_bytes = (size_t (*)(int64_t, int, int))p[6];
+    g_block.residual_norm_backward_bytes = (size_t (*)(int64_t, int, int64_t))p[7];
     for (int i = 0; i < 3; ++i) {
-        Py_INCREF(a[6 + i]);
-        g_types[F8 + i] = a[6 + i];
+        Py_INCREF(a[8 + i]);
+        g_types[F8 + i] = a[8 + i];
     }
     Py_RETURN_NONE;
 }
@@ -374,6 +378,28 @@ static int real(PyObject *v, double *out) {
 }
 static int is_dense(PyObject *t, tensor_t *o) { return tensor_of_any(t, o) && o->type <= BF16; }
 static int fits_f8(int64_t v) { return v > 0 && v <= 0x7ffffc00; }
+
+/* The workspace of a call: the caller's (`given`, a tensor or None), or what make(bytes, like) returns where some are needed.  0: what is given is
+ * no workspace; -1: an exception. */
+static int workspace(PyObject *given, size_t need, PyObject *make, PyObject *like, tensor_t *ws, PyObject **held) {
+    *held = NULL;
+    ws->ptr = NULL;
+    if (given != Py_None) return tensor_of_any(given, ws);
+    if (!need) return 1;
+    PyObject *bytes = PyLong_FromSize_t(need);
+    if (!bytes) return -1;
+    *held = PyObject_CallFunctionObjArgs(make, bytes, like, NULL);
+    Py_DECREF(bytes);
+    if (!*held) return -1;
+    return tensor_of_any(*held, ws);
+}
+#define CALL_WITH(held, expression)  \
+    int rc;                          \
+    Py_BEGIN_ALLOW_THREADS           \
+    rc = expression;                 \
+    Py_END_ALLOW_THREADS             \
+    Py_XDECREF(held);                \
+    return PyLong_FromLong(rc)
 
 /* quantize_f8(x [..., cols], (q, scale) or None, (qt, scale_t) or None) */
 static PyObject *quantize_f8(PyObject *self, PyObject *const *a, Py_ssize_t n) {
@@ -398,21 +424,28 @@ static PyObject *dequantize_f8(PyObject *self, PyObject *const *a, Py_ssize_t n)
     CALL(g_block.dequantize(q, scale, x.count / cols, cols, x.ptr, x.type, cols));
 }
 
-/* matmul_f8((q, scale), (q, scale), bias, out [..., N], cols or None: all of the pitch, workspace) */
+/* matmul_f8((q, scale), (q, scale), bias, out [..., N], cols or None: all of the pitch, workspace, make) */
 static PyObject *matmul_f8(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
     tensor_t x, w, out, ws = {0};
     void *sa, *sw, *bias;
     int cols = 0;
-    if (n != 6 || (a[4] != Py_None && (!small(a[4], &cols) || cols <= 0)) || !g_block.matmul || !PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 2 ||
+    if (n != 7 || (a[4] != Py_None && (!small(a[4], &cols) || cols <= 0)) || !g_block.matmul || !PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 2 ||
         !PyTuple_CheckExact(a[1]) || PyTuple_GET_SIZE(a[1]) != 2 || !tensor_of_any(PyTuple_GET_ITEM(a[0], 0), &x) ||
         !tensor_of_any(PyTuple_GET_ITEM(a[1], 0), &w) || x.type != F8 || w.type != F8 || x.dims != 2 || w.dims != 2 || x.last != w.last || x.last % 128 ||
         !fits_f8(x.last) || (cols && (cols + (int64_t)127) / 128 * 128 != x.last) || !fits(w.first) ||
         !vector(PyTuple_GET_ITEM(a[0], 1), U8, x.first * ((x.last + 511) / 512 * 4), 0, &sa) ||
         !vector(PyTuple_GET_ITEM(a[1], 1), U8, w.first * ((x.last + 511) / 512 * 4), 0, &sw) || !vector(a[2], F32, w.first, 1, &bias) ||
-        !is_dense(a[3], &out) || out.last != w.first || out.count != x.first * w.first || (a[5] != Py_None && !tensor_of_any(a[5], &ws)))
+        !is_dense(a[3], &out) || out.last != w.first || out.count != x.first * w.first)
         GENERAL;
-    CALL(g_block.matmul(x.ptr, sa, w.ptr, sw, bias, x.first, (int)w.first, (int)x.last, out.ptr, out.type, w.first, ws.ptr, bytes_of(&ws)));
+    PyObject *held;
+    const int ok = workspace(a[5], a[5] == Py_None ? g_block.matmul_bytes(x.first, (int)w.first, (int)x.last) : 0, a[6], a[3], &ws, &held);
+    if (ok < 0) return NULL;
+    if (!ok) {
+        Py_XDECREF(held);
+        GENERAL;
+    }
+    CALL_WITH(held, g_block.matmul(x.ptr, sa, w.ptr, sw, bias, x.first, (int)w.first, (int)x.last, out.ptr, out.type, w.first, ws.ptr, bytes_of(&ws)));
 }
 
 /* dropout(x [..., cols], drop, seed, offset, step, out) */
@@ -477,22 +510,32 @@ static PyObject *residual_norm(PyObject *self, PyObject *const *a, Py_ssize_t n)
 }
 
 /* residual_norm_backward(dz, dxo, xo, h, stats, gate, post, post_gamma, post_beta, pre, pre_gamma, pre_beta, act, scale, drop, seed, offset, step, dx, dh,
- * dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta, workspace) */
+ * dgate, dpost_gamma, dpost_beta, dpre_gamma, dpre_beta, workspace, make) */
 static PyObject *residual_norm_backward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
     tensor_t dz, dxo, xo, h, dx, dh, ws = {0};
     residual_t r;
     void *stats, *g[5];
-    if (n != 26 || !g_block.residual_norm_backward || !is_dense(a[18], &dx) || dx.last <= 0 || dx.last > 8192 || !alike(a[0], &dx, -1, &dz) ||
-        !alike(a[1], &dx, dx.type, &dxo) || !alike(a[2], &dx, dx.type, &xo) || !alike(a[3], &dx, -1, &h) || !alike(a[19], &dx, h.type, &dh) ||
-        (a[25] != Py_None && !tensor_of_any(a[25], &ws)))
+    if (n != 27 || !g_block.residual_norm_backward || !is_dense(a[18], &dx) || dx.last <= 0 || dx.last > 8192 || !alike(a[0], &dx, -1, &dz) ||
+        !alike(a[1], &dx, dx.type, &dxo) || !alike(a[2], &dx, dx.type, &xo) || !alike(a[3], &dx, -1, &h) || !alike(a[19], &dx, h.type, &dh))
         GENERAL;
+    /* a gradient that is to be made: of h, the gate and the four parameters */
+    static const int of[6] = {3, 5, 7, 8, 10, 11};
+    for (int i = 0; i < 6; ++i)
+        if ((a[of[i]] == Py_None) != (a[19 + i] == Py_None)) GENERAL;
     const int64_t rows = dx.count / dx.last, cols = dx.last;
     if (!residual(a + 5, a + 14, rows, cols, &r) || !vector(a[4], F32, rows * 4, 0, &stats) || !vector(a[20], F32, r.gates * cols, 1, &g[0])) GENERAL;
     for (int i = 1; i < 5; ++i)
         if (!vector(a[20 + i], F32, cols, 1, &g[i])) GENERAL;
     r.eps = 1.f;
-    CALL(g_block.residual_norm_backward(&r, dz.ptr, dz.type, cols, dxo.ptr, cols, xo.ptr, dx.type, cols, h.ptr, h.type, cols, stats, dx.ptr, cols, dh.ptr,
+    PyObject *held;
+    const int ok = workspace(a[25], a[25] == Py_None ? g_block.residual_norm_backward_bytes(rows, (int)cols, r.gates) : 0, a[26], a[18], &ws, &held);
+    if (ok < 0) return NULL;
+    if (!ok) {
+        Py_XDECREF(held);
+        GENERAL;
+    }
+    CALL_WITH(held, g_block.residual_norm_backward(&r, dz.ptr, dz.type, cols, dxo.ptr, cols, xo.ptr, dx.type, cols, h.ptr, h.type, cols, stats, dx.ptr, cols, dh.ptr,
                                         cols, g[0], g[1], g[2], g[3], g[4], ws.ptr, bytes_of(&ws)));
 }
 
