@@ -279,8 +279,8 @@ static_assert(kTeamThreads == 4 * kWave, "a block's teams are in one, two or fou
 static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
     const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 256 * 12 * kWave / t.threads;
     GradPlan p;
-    if (gates > 1 && gates >= wanted * t.teams) {       // whole gates for each team
-        const unsigned of_team = (gates - 1) / (wanted * t.teams) + 1, most = gate_rows < 1024 ? 1024 / gate_rows : 1;
+    if (gates > 1 && gates >= wanted * t.teams && gate_rows <= 1024) {      // whole gates for each team
+        const unsigned of_team = (gates - 1) / (wanted * t.teams) + 1, most = 1024 / gate_rows;
         p.chunks = 0;
         p.each = p.rows = (of_team < most ? of_team : most) * gate_rows;
         p.blocks = (unsigned)(((size_t)rows - 1) / ((size_t)p.each * t.teams) + 1);

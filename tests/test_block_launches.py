@@ -100,7 +100,7 @@ def test_residual_launches_reach_every_token(runtime, rows, cols, gates):  # noq
     if chunks:                                  # blocks of one gate
         assert n == chunks * gates and (chunks - 1) * chunk_rows < of_gate <= chunks * chunk_rows <= chunks * teams * each and each <= 1024
     else:                                       # whole gates for each team
-        assert each % of_gate == 0 and (n - 1) * teams * each < rows <= n * teams * each
+        assert each % of_gate == 0 and (n - 1) * teams * each < rows <= n * teams * each and each <= 1024       # (a sum's longest chain)
     (_, n, threads, (blocks, of, slabs)) = grad[1]
     assert number(blocks) == grad[0][1] and number(of) == chunks and n * threads < 1 << 32
     assert n == (4 + (gates if chunks > 1 else 0)) * number(slabs) and number(slabs) * 64 >= cols
