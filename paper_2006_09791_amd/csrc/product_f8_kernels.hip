@@ -24,7 +24,7 @@ struct ProductF8Args {
     size_t M, ldo;
     size_t part;            // elements between the outputs of two stretches of K
     int N, pitch, s_pitch;
-    int stretch;            // steps of 128 columns of a stretch of K (a multiple of four), and
+    int stretch;            // steps of 128 columns of a stretch of K, and
     unsigned tiles;         // blocks of one
     unsigned mtiles, ntiles;
     int past;               // out is stored past the caches
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_f8_tile_kernel(ProductF8
         __builtin_amdgcn_raw_ptr_buffer_load_lds(tokens ? ra : rw, (__attribute__((address_space(3))) void *)(stages + stage + base * kBlock8), 16,
                                                  off, 0, 0, 0);
     };
-    const auto load_scales = [&](int step) {        // of steps step .. step + 3
+    const auto load_scales = [&](int step) {        // of steps step .. step + 3, step a multiple of four
         if (wave < ROWS / kWave) {
             const bool tokens = wave < BM / kWave;
             const unsigned at = (unsigned)(wave * kWave - (tokens ? 0 : BM) + lane) * p.s_pitch + step;
@@ -252,7 +252,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_f8_tile_kernel(ProductF8
     // A stage in two halves of its columns.  As soon as a token fragment's products are under way the next half's is read into its registers.
     // Before the next stage's are read that has to be there, and every wave has all of this one in registers: what comes STAGES
     // later is loaded into its place, a few loads behind each fragment's products.  (That wait stands behind the last half's first products.)
-    load_scales(begin);
+    load_scales(begin & ~3);
+    if (begin & 3) load_scales((begin & ~3) + 4);       // (a stretch may begin anywhere)
 #pragma unroll
     for (int t = 0; t < STAGES; ++t)
 #pragma unroll
@@ -363,16 +364,21 @@ __global__ __launch_bounds__(256) void product_f8_join_kernel(const float *__res
     const int n = (i - m * nv) * 4, some = min(4, N - n);
     const float *p = part + (size_t)m * N + n;
     float v[4] = {};
-    for (unsigned k = 0; k < parts; ++k, p += each) {
-        if (some == 4) {
-            const f32x4 x = *reinterpret_cast<const f32x4_any *>(p);
+    if (some == 4) {
+        for (unsigned k = 0; k < parts; k += 4) {       // four on their way at once, whether they are there or not (no branch in front of a load)
+            f32x4 x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += x[e];
-        } else {
+            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const f32x4_any *>(p + min(k + i, parts - 1) * each);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += k + i < parts ? x[i][e] : 0.f;
+        }
+    } else {
+        for (unsigned k = 0; k < parts; ++k, p += each)
 #pragma unroll
             for (int e = 0; e < 3; ++e)
                 if (e < some) v[e] += p[e];
-        }
     }
     T *o = out + m * ldo + n;
 #pragma unroll
@@ -399,8 +405,8 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     //   12544 x 512 x 1024 (784 tiles), 20.1, 23.8 and 15.4.  Eight waves in 64 x 128 too: 400 x 1280 x 1001, 6.8 against 7.3 with four;
     //   without staging, in 16 x 16: for up to 16 tokens and 16384 filters (8 x 8192 x 8192, 15.0 against 16.5 in 64 x 128 and stretches; 16 x 4096 x
     //   32768, 36.0 against 33.7), or up to 256 blocks of up to 32 steps (64 x 512 x 512, 2.6 against 3.2 in 32 x 32; 256 x 1024 x 1024, 6.7 against
-    //   4.4), or up to 64 (96 x 16384 x 160 in four stretches, 10.0 against 13.7; 256 x 50176 x 128 has 128, 28.4 against 20.2); and in 32 x 32 for up to 256 blocks of up to 32 steps (64 x 4096 x 4096, 10.4 against 12.5 in 64 x 128 and stretches; 64 x 8192 x 2048,
-    //   18.8 against 13.4), or more of few steps (5000 x 64 x 64, 3.7 against 4.2; operands as bf16 are widened for fewer products in 64 x 128, 256 x
+    //   4.4), or up to 64 (96 x 16384 x 160 in four stretches, 10.0 against 13.7; 256 x 50176 x 128 has 128, 28.4 against 20.2); and in 32 x 32 for up
+    //   to 256 blocks of up to 32 steps (64 x 4096 x 4096, 10.4 against 12.5 in 64 x 128 and stretches; 64 x 8192 x 2048, 18.8 against 13.4), or more of few steps (5000 x 64 x 64, 3.7 against 4.2; operands as bf16 are widened for fewer products in 64 x 128, 256 x
     //   2048 x 2048 to fp32, 11.8 against 13.2, to bf16 11.1 against 8.9).
     const size_t small = tiles(16, 16), middle = tiles(32, 32);
     if (!wide && M > 128 && N > 128 && tiles(256, 256) >= 160) p = {kTile256, 256, 256, 512, 1, steps};
@@ -409,12 +415,13 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     else if ((middle <= 256 && steps <= 32) || (middle <= 640 && steps <= 2) || (wide && middle <= 512 && steps <= 16)) p = {kSmall2, 32, 32, 512, 1, steps};
     else p = {kTile64, 64, 128, 512, 1, steps};
     // Few blocks of a long sum: stretches of K, of 8 steps at least (32, where the block's waves share them), until every compute unit has a block.  512 x
-    // 12544 x 512 has 32 tiles: 36.0 whole, 15.4 in eight stretches and their join; 512 x 4096 x 4096 has 128, 16.0 and 22.9 in two.
+    // 12544 x 512 has 32 tiles: 36.2 whole, 14.3 in eight stretches and their join; 512 x 4096 x 4096 has 128, 15.6 and 22.7 in two.  Stretches of whole
+    // words of powers of two (of 28 steps instead of 25) take 1 us more on 1024 x 12544 x 512 to fp32, of 27.
     const size_t count = tiles(p.bm, p.bn);
     if (count <= 64) {
         const int want = (int)(256 / count), most = steps / (p.kernel < kTile64 ? 32 : 8), parts = want < most ? want : most;
         if (parts > 1) {
-            p.stretch = ((steps + parts - 1) / parts + 3) / 4 * 4;
+            p.stretch = (steps + parts - 1) / parts;
             p.parts = (steps + p.stretch - 1) / p.stretch;
         }
     }

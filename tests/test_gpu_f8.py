@@ -161,7 +161,7 @@ def test_every_tile(gpu, M, K, N, kernel):
     check_product(host(b.gspc_matmul_f8(a, w, dtype=b.GSPC_F32)), values(torch, a), values(torch, w), None, K, False)
 
 
-@pytest.mark.parametrize("M,K,N", [(96, 16384, 160), (256, 50176, 128), (64, 20000, 300), (1, 65536, 40)])
+@pytest.mark.parametrize("M,K,N", [(96, 16384, 160), (256, 50176, 128), (64, 20000, 300), (1, 65536, 40), (300, 6400, 520), (200, 9000, 333)])
 @pytest.mark.parametrize("to", ["float32", "bfloat16"])
 def test_long_sums_of_few_outputs(gpu, M, K, N, to):
     """A weight's gradient sums over all tokens: stretches of them, joined.  The workspace is as large as said, and what it held does not matter."""
