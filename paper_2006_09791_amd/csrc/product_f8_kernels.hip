@@ -404,14 +404,16 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     //   stages and eight waves where a compute unit has one block: 1000 x 2000 x 3000, 11.9 against 13.7 with four waves and 15.2 with two stages, too;
     //   12544 x 512 x 1024 (784 tiles), 20.1, 23.8 and 15.4.  Eight waves in 64 x 128 too: 400 x 1280 x 1001, 6.8 against 7.3 with four;
     //   without staging, in 16 x 16: for up to 16 tokens and 16384 filters (8 x 8192 x 8192, 15.0 against 16.5 in 64 x 128 and stretches; 16 x 4096 x
-    //   32768, 36.0 against 33.7), or up to 256 blocks of up to 32 steps (64 x 512 x 512, 2.6 against 3.2 in 32 x 32; 256 x 1024 x 1024, 6.7 against
-    //   4.4), or up to 64 (96 x 16384 x 160 in four stretches, 10.0 against 13.7; 256 x 50176 x 128 has 128, 28.4 against 20.2); and in 32 x 32 for up
-    //   to 256 blocks of up to 32 steps (64 x 4096 x 4096, 10.4 against 12.5 in 64 x 128 and stretches; 64 x 8192 x 2048, 18.8 against 13.4), or more of few steps (5000 x 64 x 64, 3.7 against 4.2; operands as bf16 are widened for fewer products in 64 x 128, 256 x
-    //   2048 x 2048 to fp32, 11.8 against 13.2, to bf16 11.1 against 8.9).
+    //   32768, 36.2 against 33.1), for up to 8 and rows of 4096 on (1 x 4096 x 50257, 39.6 against 43.6; 8 x 4096 x 50257, 45.4 against 48.0; 12,
+    //   49.2 against 48.2; 1 x 1024 x 50257, 15.3 against 11.1), or up to 256 blocks of up to 32 steps (64 x 512 x 512, 2.6 against 3.2 in 32 x 32;
+    //   256 x 1024 x 1024, 6.7 against 4.4), or up to 64 (96 x 16384 x 160 in four stretches, 10.0 against 13.7; 256 x 50176 x 128 has 128, 28.4
+    //   against 20.2); and in 32 x 32 for up to 256 blocks of up to 32 steps (64 x 4096 x 4096, 10.4 against 12.5 in 64 x 128 and stretches; 64 x
+    //   8192 x 2048, 18.8 against 13.4), or more of few steps (5000 x 64 x 64, 3.7 against 4.2; operands as bf16 are widened for fewer products in 64
+    //   x 128, 256 x 2048 x 2048 to fp32, 11.8 against 13.2, to bf16 11.1 against 8.9).
     const size_t small = tiles(16, 16), middle = tiles(32, 32);
     if (!wide && M > 128 && N > 128 && tiles(256, 256) >= 160) p = {kTile256, 256, 256, 512, 1, steps};
     else if (M > 64 && tiles(128, 128) >= 192) p = {tiles(128, 128) <= 256 ? kTile128Deep : kTile128, 128, 128, tiles(128, 128) <= 256 ? 512 : 256, 1, steps};
-    else if ((M <= 16 && tiles(64, 128) <= 128) || (small <= 256 && steps <= 32) || small <= 64) p = {kSmall1, 16, 16, 512, 1, steps};
+    else if ((M <= 16 && tiles(64, 128) <= 128) || (M <= 8 && steps >= 32) || (small <= 256 && steps <= 32) || small <= 64) p = {kSmall1, 16, 16, 512, 1, steps};
     else if ((middle <= 256 && steps <= 32) || (middle <= 640 && steps <= 2) || (wide && middle <= 512 && steps <= 16)) p = {kSmall2, 32, 32, 512, 1, steps};
     else p = {kTile64, 64, 128, 512, 1, steps};
     // Few blocks of a long sum: stretches of K, of 8 steps at least (32, where the block's waves share them), until every compute unit has a block.  512 x

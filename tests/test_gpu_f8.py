@@ -145,7 +145,8 @@ def test_product(gpu, shape, to):
 
 
 # every tile: from few tokens to many, sums cut into stretches, outputs past the caches
-TILES = [(8, 4096, 4096, "product_f8_small<1,1>"), (200, 1024, 1024, "product_f8_small<2,2>"), (1000, 2000, 3000, "product_f8_tile<128,128>"), (512, 4096, 4096, "product_f8_tile<64,128>"),
+TILES = [(8, 4096, 4096, "product_f8_small<1,1>"), (3, 4200, 20001, "product_f8_small<1,1>"), (9, 4200, 20001, "product_f8_tile<64,128>"),
+         (200, 1024, 1024, "product_f8_small<2,2>"), (1000, 2000, 3000, "product_f8_tile<128,128>"), (512, 4096, 4096, "product_f8_tile<64,128>"),
          (2048, 512, 4096, "product_f8_tile<128,128>"), (3000, 640, 4100, "product_f8_tile<256,256>")]
 
 
