@@ -330,6 +330,9 @@ int gspc_dequantize_rows_f8(const void *q, const uint8_t *scale, int64_t rows, i
 
 /* out[m][n] = sum over k < K of a[m][k] w[n][k] (+ bias[n]), a [M] and w [N] 8-bit float rows of K values, K at most 2^22.  The gradients of
  * y = x w^T are the same product: dx of dy's rows and w's columns form, dw of dy's and x's columns forms.
+ * fp32 outputs: products are exact and sums keep 24 bits.  bf16 outputs: eight products at a time are added with no bit below 2^-13 of the largest
+ * one's exponent, which is below 2^-10 of sum |a w| and about 2^-16 of a result on random values; then one rounding.  Blocks whose
+ * power of two is 2^-118 or less lose bits to fp32 outputs (their values are bf16 numbers, in steps of 2^-133).
  *   bias      : dev fp32 [N], or NULL
  *   out       : dense rows, fp32 or bf16 (out_dtype, ldo)
  *   workspace : dev, 16-byte aligned, as large as said (0: none is needed): parts of long sums of few outputs; not initialised */

@@ -56,7 +56,7 @@ __device__ __forceinline__ Wide widened(const i32x8 &v, unsigned code) {
 // A block has 16 TN channels x 16 TM tokens; its waves split the reduction into stretches, operands straight from memory into the registers of
 // v_mfma_scale_f32_16x16x128 (channels are the rows, tokens the columns of its result; a lane's 32 columns are two pieces of 16, so that a
 // load of sixteen rows is of 64 bytes of each), DEEP steps of 128 in flight, and join their sums in LDS.
-// WIDE: operands as bf16.
+// Bound by latency: 1 x 4096 x 4096, 17 MB, 6.0 us and 5.8 for the call; 1 x 4096 x 50257, 206 MB, 43 us (4.8 TB/s).  WIDE: operands as bf16.
 template <typename T, bool WIDE, int TN, int TM, int WAVES, int DEEP>
 __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8Args p) {
     __shared__ f32x4 s_part[WAVES][TN * TM][kWave];
@@ -174,6 +174,11 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
 // word of a row and come the same way, once in four stages.  Within a row the 16-byte pieces are permuted by the row's number, so that the lanes that read
 // one column of pieces spread over all banks; a load's lanes fetch from the addresses that this asks for.  A lane's 32 columns of a product are two
 // such pieces; which columns of the block they are does not matter as long as both operands agree.
+//
+// Bound by the matrix instructions where there is enough work: 8192 x 4096 x 8192 to bf16 in 256 x 256 takes 219 us (2.5 PFLOP/s; the
+// library's product without scales 216).  WIDE by the widening, sixteen clocks for 128 values, which each wave does for all of its operands: a step of 32 x 32
+// in a wave (64 x 128) takes 1024 clocks of it and 256 of products, one of 64 x 64 (128 x 128) 2048 and 1024 (8192 x 4096 x 8192 to fp32 in 128 x 128:
+// 461 us, 1.19 PFLOP/s; 1024 x 12544 x 512 in 64 x 128 and four stretches: 23 and a join of 4).
 template <typename T, bool WIDE, int WM, int WN, int TM, int TN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void product_f8_tile_kernel(ProductF8Args p) {
     constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES;
@@ -354,7 +359,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_f8_tile_kernel(ProductF8
     }
 }
 
-// Sums of stretches of K, in their order.
+// Sums of stretches of K, in their order (four of 1024 x 512: 4 us, latency).
 template <typename T>
 __global__ __launch_bounds__(256) void product_f8_join_kernel(const float *__restrict__ part, size_t each, unsigned parts, unsigned vectors, int N,
                                                               unsigned nv, unsigned m_nv, const float *__restrict__ bias, T *__restrict__ out, size_t ldo) {
