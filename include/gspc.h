@@ -314,7 +314,8 @@ int gspc_matmul_i8(const void *a, const float *a_scale, const void *w, const flo
  *                     4-byte aligned: the exponent, plus 127, of the power of two that they are multiplied by (255: no number).
  *
  * Zero rows are no work.  Sums are fp32 (over blocks of tokens fp64), results rounded once to their type.  No atomics: the same
- * call gives the same bits. */
+ * call gives the same bits.  Outputs overlap nothing but where a tensor may be another; a workspace is one call's at a time (calls
+ * that follow one another on a stream, or in a graph, may share it). */
 
 /* Bytes of one row's values, and of its powers of two.  0 if cols is not positive or too large. */
 int gspc_f8_pitch(int cols);
