@@ -73,10 +73,23 @@ __device__ __forceinline__ float ratio(float a, float n) {
     return fmaf(fmaf(-q, n, a), r, q);
 }
 
-// Mean and 1 / deviation of a token, of the values of v that are there (n of a lane's; the others are 0): a wave's own mean and the squares around it,
-// joined over the waves (so that an offset does not cancel in them).  seg: the wave's number in its team.
+// 1 for a lane's columns that are there, else 0.  A mean is subtracted times it, fmaf(-mean, there, v), so that what is not there stays 0 in every
+// sum, at no cost (conditions would be kept in pairs of scalar registers, of which there are not enough).
+template <Rows ROWS> struct There {
+    float one[ROWS == kWhole ? 1 : 8];          // (all of a lane's eight, or none)
+    __device__ __forceinline__ float operator[](int e) const { return one[ROWS == kWhole ? 0 : e]; }
+};
+template <Rows ROWS> __device__ __forceinline__ There<ROWS> columns_there(const Place &at) {
+    There<ROWS> t;
+#pragma unroll
+    for (int e = 0; e < (ROWS == kWhole ? 1 : 8); ++e) t.one[e] = e < at.n ? 1.f : 0.f;
+    return t;
+}
+
+// Mean and 1 / deviation of a token, of values of which those that are not there are 0: a wave's own mean and the squares around it, joined over the
+// waves (so that an offset does not cancel in them).  seg: the wave's number in its team.
 template <Rows ROWS, bool WAVES>
-__device__ __forceinline__ float2 team_stats(const float (&v)[8], int n, int cols, int kind, float eps, int team, int seg, TeamSums &t) {
+__device__ __forceinline__ float2 team_stats(const float (&v)[8], const There<ROWS> &there, int cols, int kind, float eps, int team, int seg, TeamSums &t) {
     const float count = (float)cols;
     float sum = 0.f;
     if (kind == kNormRms) {
@@ -91,10 +104,10 @@ __device__ __forceinline__ float2 team_stats(const float (&v)[8], int n, int col
     float mean = mine > 0.f ? ratio(wave_sum<WAVES>(make_float2(sum, 0.f), team).x, mine) : 0.f, squares = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float d = ROWS == kWhole || e < n ? v[e] - mean : 0.f;
+        const float d = fmaf(-mean, there[e], v[e]);
         squares = fmaf(d, d, squares);
     }
-    squares = wave_sum<WAVES>(make_float2(ROWS == kWhole && n == 0 ? 0.f : squares, 0.f), team).x;
+    squares = wave_sum<WAVES>(make_float2(squares, 0.f), team).x;
     if (WAVES && team > kWave) {
         const float2 o = team_exchange(make_float2(mean, squares), team, t);
         const int other = threadIdx.x % 16;             // (a wave that is not there has no columns)

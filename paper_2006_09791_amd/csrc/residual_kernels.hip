@@ -8,7 +8,7 @@ namespace gspc {
 // and z out: bound by memory without an h (50176 x 512 in bf16, 103 MB: 18 us, 5.7 TB/s), by vector instructions nearly as much with two
 // norms, dropout and SiLU (206 MB: 49.5 us, 4.2 TB/s; 340 instructions for a wave's 512 values, three quarters of the time).  H: there is an h.
 template <typename TX, typename TH, bool H, Rows ROWS, bool WAVES>
-__global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, ResidualForward f, int team, unsigned each, unsigned m_gate) {
+__global__ __launch_bounds__(WAVES ? kMaxTeam : kTeamThreads) void residual_norm_kernel(Residual a, ResidualForward f, int team, unsigned each, unsigned m_gate) {
     __shared__ float2 s_place[2][kMaxTeam / kWave];
     TeamSums sums{s_place, 0};
     const int lane = threadIdx.x & (team - 1), seg = lane / kWave;
@@ -30,6 +30,9 @@ __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, Res
     some_params<ROWS>(a.pre_beta, at, 0.f, b2);
     unsigned gate_row = ~0u;
     const uint64_t call = a.drop.offset + (a.drop.step ? *a.drop.step : 0);
+    const There<ROWS> some = columns_there<ROWS>(at);
+    const auto bytes = [&](int n) { return n >= 4 ? ~0u : n > 0 ? (1u << 8 * n) - 1 : 0u; };
+    const u32x2 codes = {bytes(at.n), bytes(at.n - 4)};         // of 8-bit float rows: zeros past the last column, whatever the token
     for (unsigned k = 0; k < each; ++k) {                       // as often in every team: there are barriers
         const unsigned row = first + k;
         const bool there = row < last;
@@ -44,9 +47,9 @@ __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, Res
         for (int e = 0; e < 8; ++e) v[e] *= a.scale;
         if constexpr (H) {
             if (a.post != kNormNone) {
-                st1 = team_stats<ROWS, WAVES>(u, at.n, a.cols, a.post, a.eps, team, seg, sums);
+                st1 = team_stats<ROWS, WAVES>(u, some, a.cols, a.post, a.eps, team, seg, sums);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = fmaf((u[e] - st1.x) * st1.y, g1[e], b1[e]);
+                for (int e = 0; e < 8; ++e) u[e] = fmaf(fmaf(-st1.x, some[e], u[e]) * st1.y, g1[e], b1[e]);
             }
             const unsigned now = a.gate ? fast_div_any(min(row, a.rows - 1), a.gate_rows, m_gate) : 0;
             if (now != gate_row) {
@@ -57,21 +60,19 @@ __global__ __launch_bounds__(kMaxTeam) void residual_norm_kernel(Residual a, Res
             }
             if (a.drop.limit) drop_some(a.drop, call, row, lane, u);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = ROWS == kWhole || e < at.n ? fmaf(gate[e], u[e], v[e]) : 0.f;
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(gate[e], u[e], v[e]);
         }
         if (there && f.xo) store_some<ROWS>(static_cast<TX *>(f.xo) + row * f.ldxo, at, v, f.past);
         if (a.pre != kNormNone) {
-            st2 = team_stats<ROWS, WAVES>(v, at.n, a.cols, a.pre, a.eps, team, seg, sums);
+            st2 = team_stats<ROWS, WAVES>(v, some, a.cols, a.pre, a.eps, team, seg, sums);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fmaf((v[e] - st2.x) * st2.y, g2[e], b2[e]);
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(fmaf(-st2.x, some[e], v[e]) * st2.y, g2[e], b2[e]);
             activate_all(a.act, v);
             if (f.z_dtype == GSPC_F8) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (ROWS == kWhole ? at.n > 0 : e < at.n) ? v[e] : 0.f;
                 const unsigned code = block_code(lanes_umax(top_of(v), 16));
                 const int pitch = f8_pitch(a.cols), s_pitch = f8_scale_pitch(a.cols);
                 if (there && at.at < (unsigned)pitch) {
-                    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(f.z) + (size_t)row * pitch + at.at) = f8_codes(v, block_up(code));
+                    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(f.z) + (size_t)row * pitch + at.at) = f8_codes(v, block_up(code)) & codes;
                     uint8_t *s = f.z_scale + (size_t)row * s_pitch + lane / 16;
                     if (lane % 16 == 0) *s = (uint8_t)code;
                     else if (lane / 16 == pitch / kBlock8 - 1 && lane / 16 + lane % 16 < s_pitch) s[lane % 16] = 0;

@@ -94,6 +94,31 @@ def test_forward(gpu, case):
     assert torch.equal(q8.view(torch.uint8), want8[0].view(torch.uint8)) and torch.equal(s8, want8[1])
 
 
+# a team's lanes are more than a token's channels, which no parameter says
+UNEVEN = [(7, 3), (7, 24), (60, 37), (7, 40), (5, 65), (9, 133), (3, 520), (3, 1000), (2, 1544), (2, 4104), (2, 5003)]
+
+
+@pytest.mark.parametrize("rows,C", UNEVEN)
+@pytest.mark.parametrize("post,pre", itertools.product((0, 1, 2), (1, 2)))
+def test_norms_without_parameters(gpu, rows, C, post, pre):
+    """Forward and gradient, whose sums have zeros where a lane has no channel."""
+    torch, b = gpu
+    rng = np.random.default_rng(rows * 1000 + C)
+    p = {"post": post, "pre": pre, "act": 0, "scale": 1.0, "drop": 0.0}
+    q = {**p, **dict.fromkeys(NAMES), "mask": None, "eps": 1e-5}
+    x, h, dz, dxo = (dev(torch, inputs(rng, rows, C) + np.float32(k)) for k in (1, 3, 0, 0))
+    stats = torch.empty(rows, 4, device="cuda")
+    xo, z = b.gspc_residual_norm(x, h, stats=stats, **p)
+    want = forward64(q, host(x), host(h))
+    for got, name, error in ((xo, "xo", "e_xo"), (z, "z", "e_z")):
+        assert (np.abs(host(got) - want[name]) <= want[error] + U * np.abs(want[name]) * 1.01 + 1e-30).all(), name
+    q8, s8 = b.gspc_residual_norm(x, h, dtype=b.GSPC_F8, **p)[1]
+    want8 = b.gspc_quantize_rows_f8(z)
+    assert torch.equal(q8.view(torch.uint8), want8[0].view(torch.uint8)) and torch.equal(s8, want8[1])
+    got = b.gspc_residual_norm_backward(dz, dxo, xo, h, stats, **p)
+    check_grads(torch, got, backward64(q, host(dz), host(dxo), host(xo), host(h), host(stats)), {})
+
+
 @pytest.mark.parametrize("rows,C", [(1, 1), (7, 60), (130, 130), (3, 1000), (2, 8192)])
 @pytest.mark.parametrize("kind", [1, 2])
 def test_norm_alone(gpu, rows, C, kind):
