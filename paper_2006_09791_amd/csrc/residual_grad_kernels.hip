@@ -19,13 +19,14 @@ struct GradPlan {
 // A team walks down its tokens and keeps the sums of its columns; a block's teams add theirs up and leave one part.  dz, dx', x' and h in, dx and dh out:
 // bound by memory and, nearly as much, by vector instructions (50176 x 512 in bf16, two norms, dropout and SiLU, 309 MB: 65.4 us, 4.7 TB/s; 460
 // instructions for a wave's 512 values).  GATES: a team's tokens have several gates, whose gradients it writes itself.  LARGE: teams of
-// more than 512 lanes, which leave 128 registers each: parameters are read again for each token, and no token ahead (4096 x 8192, 403 MB: 142 us;
-// 8192 x 4096, as many bytes, 100).
+// more than 512 lanes, which leave 128 registers each: parameters are in LDS, and no token is ahead (4096 x 8192, 403 MB: 108 us, and 134 with
+// parameters read again for each token; 8192 x 4096, as many bytes, 89).
 template <typename TX, typename TH, bool GATES, bool LARGE, Rows ROWS, bool WAVES>
 __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad_kernel(Residual a, ResidualBackward f, GradPlan g, int of_team, unsigned m_chunks,
                                                                  float *__restrict__ parts) {
     __shared__ float2 s_place[2][kMaxTeam / kWave];
     __shared__ float s_sum[kTeamThreads * 8];              // (of several teams)
+    __shared__ f32x4 s_mine[LARGE ? 6 : 1][LARGE ? kMaxTeam : 1];       // a lane's own parameters
     TeamSums sums{s_place, 0};
     const int team = LARGE ? kMaxTeam : of_team, lane = threadIdx.x & (team - 1);
     Place at = place_of(lane * 8, a.cols);
@@ -64,6 +65,7 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
         load_h(first);
     }
     const float inv = 1.f / (float)a.cols;
+    const There<ROWS> some = columns_there<ROWS>(at);
     const bool centre1 = a.post == kNormLayer, centre2 = a.pre == kNormLayer;
     const uint64_t call = a.drop.offset + (a.drop.step ? *a.drop.step : 0);
     float g2[8], b2[8], gg[8];                                  // gg: g1 gate, times what makes up for the dropped
@@ -71,16 +73,31 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
         some_params<ROWS>(a.pre_gamma, at, 1.f, g2);
         some_params<ROWS>(a.pre_beta, at, 0.f, b2);
     };
-    if constexpr (!LARGE) pre_params();
+    const auto keep = [&](int place, const float (&v)[8]) {     // (LARGE: in LDS instead of registers; nobody else reads them)
+        if constexpr (LARGE) {
+            s_mine[place][threadIdx.x] = (f32x4){v[0], v[1], v[2], v[3]};
+            s_mine[place + 1][threadIdx.x] = (f32x4){v[4], v[5], v[6], v[7]};
+        }
+    };
+    const auto get = [&](int place, float (&v)[8]) {
+        if constexpr (LARGE) {
+            const f32x4 a = s_mine[place][threadIdx.x], b = s_mine[place + 1][threadIdx.x];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+        }
+    };
+    pre_params();
+    keep(0, g2);
+    keep(2, b2);
     const auto new_gate = [&] {
         float gate[8];
         some_params<ROWS>(a.post_gamma, at, 1.f, gg);
         some_params<ROWS>(a.gate ? a.gate + (size_t)gate_row * a.cols : nullptr, at, 1.f, gate);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) gg[e] *= gate[e] * a.drop.up;
+        for (int e = 0; e < 8; ++e) gg[e] *= gate[e] * a.drop.up * some[e];
+        keep(4, gg);
     };
-    if constexpr (!LARGE)
-        if (!GATES || first < last) new_gate();
+    if (!GATES || first < last) new_gate();
     float sa[8] = {}, sb[8] = {}, sg2[8] = {}, sb2[8] = {}, sg1[GATES ? 8 : 1] = {}, sb1[GATES ? 8 : 1] = {};
     // A gate's tokens are through: its gradient, and what its sums are to the parameters'.
     const auto end_gate = [&](float (&dgate)[8], float (&dg1)[8], float (&db1)[8]) {
@@ -107,9 +124,14 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
         const unsigned row = first + k;
         const bool there = row < last;
         asm volatile("" : "+v"(at.at), "+v"(at.start));     // (no address of a lane's own is kept over tokens: two registers for each tensor)
-        if constexpr (LARGE) load_norm(row);
+        if constexpr (LARGE) {
+            load_norm(row);
+            if constexpr (!GATES) {
+                load_stream(row);
+                load_h(row);
+            }
+        }
         const float4 st = there ? r_st : make_float4(0.f, 1.f, 0.f, 1.f);
-        const int n = there ? at.n : 0;
         float dv[8] = {}, d[8] = {}, xh[8], hh[8];
         widen_any<ROWS>(r_dz, f.dz_dtype, at, dv, there && f.has_dz);
         widen_some<ROWS>(r_xo, at, xh, there);
@@ -121,15 +143,13 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             load_h(row + 1);
         }
         if (f.has_dz) {
-            if constexpr (LARGE) pre_params();
+            get(0, g2);
+            get(2, b2);
             phase();
             float2 s = make_float2(0.f, 0.f);
             float t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) xh[e] = (xh[e] - st.z) * st.w;
-            if constexpr (ROWS != kWhole)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) xh[e] = e < n ? xh[e] : 0.f;        // (dv is 0 where nothing is there, but a parameter's slope may be none)
+            for (int e = 0; e < 8; ++e) xh[e] = fmaf(-st.z, some[e], xh[e]) * st.w;
             if (a.act != kActNone) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -149,13 +169,13 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             const float m = centre2 ? s.x * inv : 0.f, c = s.y * inv;
             phase();
             if constexpr (LARGE) {
-                load_stream(row);
+                if constexpr (GATES) load_stream(row);
                 widen_some<ROWS>(r_dxo, at, d, there && f.has_dxo);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = fmaf(st.w, t[e] - m - xh[e] * c, d[e]);
         } else if constexpr (LARGE) {
-            load_stream(row);
+            if constexpr (GATES) load_stream(row);
             widen_some<ROWS>(r_dxo, at, d, there && f.has_dxo);
         }
         phase();
@@ -169,17 +189,16 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             if (a.drop.limit) drop_some(a.drop, call, row, lane, d);
             phase();
             if constexpr (LARGE) {
-                load_h(row);
+                if constexpr (GATES) load_h(row);
                 widen_some<ROWS>(r_h, at, hh, there);
-                if (there) new_gate();
+                get(4, gg);
             }
             phase();
             float2 s = make_float2(0.f, 0.f);
             float q[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] = (ROWS == kWhole ? n > 0 : e < n) ? d[e] : 0.f;
-                hh[e] = (hh[e] - st.x) * st.y;
+                hh[e] = fmaf(-st.x, some[e], hh[e]) * st.y;
                 sa[e] = fmaf(d[e], hh[e], sa[e]);
                 sb[e] += d[e];
                 q[e] = gg[e] * d[e];
@@ -203,8 +222,7 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sg1[e] += dg1[e], sb1[e] += db1[e], sa[e] = sb[e] = 0.f;
                     ++gate_row;
-                    if constexpr (!LARGE)
-                        if (row + 1 < last) new_gate();
+                    if (row + 1 < last) new_gate();
                 }
                 left = a.gate_rows;
             }
@@ -279,8 +297,11 @@ __global__ __launch_bounds__(256) void residual_clear_kernel(float *p, size_t co
 
 static_assert(kTeamThreads == 4 * kWave, "a block's teams are in one, two or four waves");
 
+// As many blocks as are at work at once: of 1024 lanes one a compute unit, of fewer eight waves.  (Twelve, which the registers would hold, have half
+// as many parts again to add up, and leave 1.5 blocks of 512 lanes for each compute unit: 12544 x 512 in bf16, layer norms, SiLU and dropout, with 4, 8, 12
+// and 16: 28.9, 25.0, 26.2, 32.5 us; 2000 x 4096: 46.4, 31.5, 43.8, 39.6.  Of 1024 lanes, 4096 x 8192, 8, 16 and 32: 234, 134, 144.)
 static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
-    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 256 * 12 * kWave / t.threads;
+    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 256 * (t.team > kMaxTeam / 2 ? 16 : 8) * kWave / t.threads;
     GradPlan p;
     if (gates > 1 && gates >= wanted * t.teams && gate_rows <= 1024) {      // whole gates for each team
         const unsigned of_team = (gates - 1) / (wanted * t.teams) + 1, most = 1024 / gate_rows;
