@@ -299,9 +299,13 @@ static_assert(kTeamThreads == 4 * kWave, "a block's teams are in one, two or fou
 
 // As many blocks as are at work at once: of 1024 lanes one a compute unit, of fewer eight waves.  (Twelve, which the registers would hold, have half
 // as many parts again to add up, and leave 1.5 blocks of 512 lanes for each compute unit: 12544 x 512 in bf16, layer norms, SiLU and dropout, with 4, 8, 12
-// and 16: 28.9, 25.0, 26.2, 32.5 us; 2000 x 4096: 46.4, 31.5, 43.8, 39.6.  Of 1024 lanes, 4096 x 8192, 8, 16 and 32: 234, 134, 144.)
+// and 16: 28.9, 25.0, 26.2, 32.5 us; 2000 x 4096: 46.4, 31.5, 43.8, 39.6.  Of 1024 lanes, 4096 x 8192, 8, 16 and 32: 234, 134, 144.)  Twelve all
+// the same where teams of one or two waves have 16 tokens each or more: 50176 x 512 behind its forward call 65.4 against 71, 30000 x 1024 86.5 against
+// 88.0; of 256 channels or 2048, 100352 and 20000 tokens, 75.2 against 71.8 and 115 against 110.
 static GradPlan plan_grad(const Residual &a, const TeamGrid &t) {
-    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows, wanted = 256 * (t.team > kMaxTeam / 2 ? 16 : 8) * kWave / t.threads;
+    const bool many = (t.team == kWave || t.team == 2 * kWave) && a.rows / (256 * 12 * kWave / t.threads * t.teams) >= 16;
+    const unsigned rows = a.rows, gates = a.gates, gate_rows = a.gate_rows;
+    const unsigned wanted = 256 * (t.team > kMaxTeam / 2 ? 16 : many ? 12 : 8) * kWave / t.threads;
     GradPlan p;
     if (gates > 1 && gates >= wanted * t.teams && gate_rows <= 1024) {      // whole gates for each team
         const unsigned of_team = (gates - 1) / (wanted * t.teams) + 1, most = 1024 / gate_rows;
