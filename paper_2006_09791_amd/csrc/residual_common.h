@@ -67,6 +67,11 @@ template <bool WAVES> __device__ __forceinline__ float2 team_sum(float2 v, int t
     return v;
 }
 
+template <bool WAVES> __device__ __forceinline__ float team_sum(float v, int team, TeamSums &t) {
+    v = wave_sum<WAVES>(make_float2(v, 0.f), team).x;       // (the zero's sum is not made)
+    return WAVES && team > kWave ? lanes_sum(team_exchange(make_float2(v, 0.f), team, t).x, 16) : v;
+}
+
 // a / n by the reciprocal, corrected once: exact where the quotient is a number (a constant token's mean is its value).
 __device__ __forceinline__ float ratio(float a, float n) {
     const float r = __builtin_amdgcn_rcpf(n), q = a * r;
@@ -95,7 +100,7 @@ __device__ __forceinline__ float2 team_stats(const float (&v)[8], const There<RO
     if (kind == kNormRms) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
-        return make_float2(0.f, rsqrtf(ratio(team_sum<WAVES>(make_float2(sum, 0.f), team, t).x, count) + eps));
+        return make_float2(0.f, rsqrtf(ratio(team_sum<WAVES>(sum, team, t), count) + eps));
     }
     const auto of = [&](int wave) { return (float)max(0, min(cols - wave * 8 * kWave, 8 * kWave)); };
 #pragma unroll
