@@ -172,6 +172,26 @@ def test_what_is_not_finite_stays_in_its_token(gpu, C):
     assert torch.equal(xo[3][m[3] == 0], x[3][m[3] == 0])       # where the block's output is dropped the stream goes on
 
 
+@pytest.mark.parametrize("C", [3, 24, 37, 130, 520, 4104])
+def test_tokens_that_are_no_number_as_8_bit_float_rows_and_back(gpu, C):
+    """What lies past their last column is zero all the same, and in the gradient they have no say in other tokens."""
+    torch, b = gpu
+    rng = np.random.default_rng(C)
+    x, h, dz, dxo = (dev(torch, inputs(rng, 9, C)) for _ in range(4))
+    h[3, C - 1], x[6, 0] = float("nan"), float("inf")
+    p = {"post": 2, "pre": 2, "act": 2}
+    stats = torch.empty(9, 4, device="cuda")
+    xo, z = b.gspc_residual_norm(x, h, stats=stats, **p)
+    q8, s8 = b.gspc_residual_norm(x, h, dtype=b.GSPC_F8, **p)[1]
+    want = b.gspc_quantize_rows_f8(z)
+    assert torch.equal(q8.view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(s8, want[1])
+    assert not bool(q8[:, C:].view(torch.uint8).any()) and bool(q8[3, :C].float().isnan().all())
+    got = b.gspc_residual_norm_backward(dz, dxo, xo, h, stats, **p)
+    keep = [0, 1, 2, 4, 5, 7, 8]
+    less = b.gspc_residual_norm_backward(*(t[keep].contiguous() for t in (dz, dxo, xo, h, stats)), **p)
+    assert torch.equal(got.dx[keep], less.dx) and torch.equal(got.dh[keep], less.dh) and bool(less.dx.isfinite().all())
+
+
 # ---- the gradient ------------------------------------------------------------------------------------------
 def check_grads(torch, got, want, types):
     for name, (w, size) in want.items():
