@@ -19,7 +19,10 @@ class ResidualBlocks:
     def __init__(self, weights, gates, post_gammas, pre_gammas, scale=1.0, drop=0.0, seed=0, norm=b.NORM_RMS, act=b.ACT_SILU, eps=1e-5):
         self.weights, self.gates, self.post, self.pre = weights, gates, post_gammas, pre_gammas
         self.scale, self.drop, self.seed, self.norm, self.act, self.eps = scale, drop, seed, norm, act, eps
-        self.rows8 = [b.gspc_quantize_rows_f8(w) for w in weights]      # for answers: once
+
+    def weight_rows(self):
+        """The weights as they are now, as 8-bit float rows: for answers of weights that stay, once."""
+        return [b.gspc_quantize_rows_f8(w) for w in self.weights]
 
     def _before(self, k):
         """The norm in front of block k, or none behind the last."""
@@ -32,10 +35,13 @@ class ResidualBlocks:
         return {"gate": self.gates[k], "post": self.norm, "post_gamma": self.post[k], "scale": self.scale, **self._before(k + 1),
                 **({"drop": self.drop, "seed": self.seed, "offset": k << 32, "step": step} if step is not None else {})}
 
-    def answer(self, x):
-        """x [N, P, C] -> [N, P, C], of its type."""
+    def answer(self, x, rows8=None):
+        """x [N, P, C] -> [N, P, C], of its type.  rows8: what weight_rows returned, while the weights are those of then; without it each answer
+        writes them anew."""
+        if rows8 is not None and len(rows8) != len(self.weights):
+            raise b.GspcError(-5, f"rows of {len(rows8)} weights, blocks {len(self.weights)}")
         _, z = b.gspc_residual_norm(x, dtype=b.GSPC_F8, **self._before(0))
-        for k, w in enumerate(self.rows8):
+        for k, w in enumerate(self.weight_rows() if rows8 is None else rows8):
             h = b.gspc_matmul_f8(z, w).view(x.shape)
             # (the stream is written in place from the second block on: x itself stays)
             x, z = b.gspc_residual_norm(x, h, xo=x if k else None, dtype=b.GSPC_F8, **self._block(k, None))
@@ -95,13 +101,14 @@ def main():
     import torch
     b.gspc_set_stream()
     net = random_blocks(a.channels, a.blocks, a.drop)
+    rows8 = net.weight_rows()
     x = torch.randn(a.images, a.pixels * a.pixels, a.channels, device="cuda").bfloat16()
     dy, step = torch.randn_like(x), torch.zeros(1, dtype=torch.int64, device="cuda")
 
     def train():
         net.train(x, dy, step)
         step.add_(1)
-    for name, call in (("answer", lambda: net.answer(x)), ("train", train)):
+    for name, call in (("answer", lambda: net.answer(x, rows8)), ("train", train)):
         for _ in range(5):
             call()
         torch.cuda.synchronize()

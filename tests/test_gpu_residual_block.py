@@ -99,6 +99,40 @@ def test_training_step_in_a_replayed_graph(gpu):
         del eager
 
 
+def test_answers_are_of_the_weights_as_they_are(gpu):
+    """Changed in place, by a write that torch does not see as one, or replaced: bit by bit a new network's answer, eager and replayed; rows that
+    were laid out before are the caller's."""
+    torch, b = gpu
+    from paper_2006_09791_amd import residual_block
+    C = 200
+    net = residual_block.random_blocks(C, 2, seed=5)
+    fresh = lambda: residual_block.ResidualBlocks(net.weights, net.gates, net.post, net.pre)  # noqa: E731
+    x = torch.randn(2, 30, C, device="cuda").bfloat16()
+    old, before = net.weight_rows(), net.answer(x)
+    with on_side_stream(torch, b) as s:
+        net.answer(x)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            held = net.answer(x)
+        other = torch.randn(C, C, device="cuda") * 0.1
+        for change in (lambda: net.weights[0].mul_(-1.5), lambda: net.weights[1].data.copy_(other), lambda: b.gspc_dropout(net.weights[0], 0.5, 3, out=net.weights[0])):
+            last = net.answer(x)
+            change()
+            graph.replay()
+            got, want = net.answer(x), fresh().answer(x)
+            s.synchronize()
+            assert torch.equal(got, want) and torch.equal(held, want) and not torch.equal(got, last)
+        net.weights[0] = other
+        got, want, given = net.answer(x), fresh().answer(x), net.answer(x, net.weight_rows())
+        s.synchronize()
+        assert torch.equal(got, want) and torch.equal(given, want)
+        stale = net.answer(x, old)
+        s.synchronize()
+        assert torch.equal(stale, before)
+    with pytest.raises(b.GspcError, match="rows of 1 weights"):
+        net.answer(x, old[:1])
+
+
 def test_command_prints_both_passes(gpu, capsys, monkeypatch):
     from paper_2006_09791_amd import residual_block
     monkeypatch.setattr("sys.argv", ["residual_block", "--images", "2", "--pixels", "5", "--channels", "72", "--blocks", "2", "--passes", "2"])
