@@ -15,14 +15,14 @@ __global__ __launch_bounds__(256) void dropout_kernel(Dropout d, const T *x, siz
     if (i >= vectors) return;
     const unsigned row = fast_div_any(i, nv, m_nv), vec = i - row * nv;
     const Place at = place_of(vec * 8, cols);
-    const Raw<T, 8> raw = fetch_some<ROWS>(x + row * ldx, at);
+    const Raw<T, 8> raw = fetch_some<ROWS, true>(x + row * ldx, at);
     const uint64_t call = d.offset + (d.step ? *d.step : 0);
     float v[8];
     widen_some<ROWS>(raw, at, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= d.up;
     drop_some(d, call, first + row, vec, v);
-    store_some<ROWS>(y + row * ldy, at, v, past);
+    store_some<ROWS, true>(y + row * ldy, at, v, past);
 }
 
 template <typename T> static hipError_t dropout(const Dropout &d, const T *x, size_t ldx, size_t rows, int cols, T *y, size_t ldy, hipStream_t s) {

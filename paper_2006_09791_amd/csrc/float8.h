@@ -3,6 +3,7 @@
 // they are multiplied by.
 #pragma once
 
+#include "row_place.h"
 #include "tokens.h"
 
 namespace gspc {
@@ -50,26 +51,8 @@ __device__ __forceinline__ void f8_values(u32x2 q, float (&v)[8]) {
         v[4 * i] = lo[0], v[4 * i + 1] = lo[1], v[4 * i + 2] = hi[0], v[4 * i + 3] = hi[1];
     }
 }
-// Eight columns of a row from `at` on, of which the first n (8, fewer at the row's end, or none) are there.  In rows of whole eights (kWhole) n is 8 or
-// 0.  What is there at the end of others (kRagged) is read as the row's last eight columns, in one access, and moved to its place when it is widened;
-// rows of fewer than eight columns (kThin) are read one by one.  Lanes without a column read the row's first ones: no load hangs on a branch, behind
-// which a wait for older loads would have to be one for all.
-enum Rows { kWhole, kRagged, kThin };
-inline Rows rows_of(int cols) { return cols % 8 == 0 ? kWhole : cols > 8 ? kRagged : kThin; }
-struct Place {
-    unsigned at, start;         // start: of what is read
-    int n, shift;
-};
-__device__ __forceinline__ Place place_of(int at, int cols) {
-    Place p;
-    p.at = at;
-    p.n = max(0, min(8, cols - at));
-    p.shift = p.n > 0 ? 8 - p.n : 0;
-    p.start = p.n > 0 ? at - p.shift : 0;
-    return p;
-}
-template <Rows ROWS, typename T> __device__ __forceinline__ Raw<T, 8> fetch_some(const T *row, const Place &p) {
-    if constexpr (ROWS != kThin) return fetch<8>(beyond(row, p.start * (unsigned)sizeof(T)));
+template <Rows ROWS, bool LONG = false, typename T> __device__ __forceinline__ Raw<T, 8> fetch_some(const T *row, const Place &p) {
+    if constexpr (ROWS != kThin) return fetch<8>(beyond(row, column_bytes<LONG>(p.start, sizeof(T))));
     else {
         Raw<T, 8> r{};
 #pragma unroll
@@ -103,8 +86,8 @@ __device__ __forceinline__ void store4(float *p, float a, float b, float c, floa
 __device__ __forceinline__ void store4(uint16_t *p, float a, float b, float c, float d) {
     *reinterpret_cast<u32x2_any *>(p) = (u32x2){bf16_pair(a, b), bf16_pair(c, d)};
 }
-template <Rows ROWS, typename T> __device__ __forceinline__ void store_some(T *row, const Place &p, const float (&v)[8], bool past = false) {
-    T *to = beyond(row, p.at * (unsigned)sizeof(T));
+template <Rows ROWS, bool LONG = false, typename T> __device__ __forceinline__ void store_some(T *row, const Place &p, const float (&v)[8], bool past = false) {
+    T *to = beyond(row, column_bytes<LONG>(p.at, sizeof(T)));
     if (p.n == 8) store(to, v, past);
     else if constexpr (ROWS != kWhole) {                 // four, two and one of them (by value: a choice between places would put v into memory)
         const bool four = p.n & 4, two = p.n & 2;

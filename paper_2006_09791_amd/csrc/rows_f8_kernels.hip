@@ -15,7 +15,7 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(const T *__restrict__ 
     const int block = unit - row * blocks, lane = threadIdx.x % 16, at = block * kBlock8 + lane * 8;
     const Place some = place_of(at, cols);
     float v[8];
-    widen_some<ROWS>(fetch_some<ROWS>(x + row * ldx, some), some, v);
+    widen_some<ROWS>(fetch_some<ROWS, true>(x + row * ldx, some), some, v);
     const unsigned code = block_code(lanes_umax(top_of(v), 16));
     *reinterpret_cast<u32x2 *>(q + (size_t)row * blocks * kBlock8 + at) = f8_codes(v, block_up(code));
     const int pitch = f8_scale_pitch(cols);
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t *__res
     f8_values(*reinterpret_cast<const u32x2 *>(q + (size_t)row * blocks * kBlock8 + at), v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= down;
-    store_some<ROWS>(x + row * ldx, place_of(at, cols), v, past);
+    store_some<ROWS, true>(x + row * ldx, place_of(at, cols), v, past);
 }
 
 // A tile of 128 rows and columns, read once: thread (tx, ty) holds columns 8 tx .. + 7 of rows 4 ty .. + 3.  A row's block is in sixteen
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(512) void quantize_f8_turned_kernel(const T *__rest
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const unsigned row = r0 + ty * 4 + i;
-        raw[i] = fetch_some<ROWS>(x + (size_t)min(row, rows - 1) * ldx, some);
+        raw[i] = fetch_some<ROWS, true>(x + (size_t)min(row, rows - 1) * ldx, some);
     }
     float v[4][8];
 #pragma unroll

@@ -46,8 +46,8 @@ template <> struct RawOf<uint16_t, 8> { typedef Raw16 type; };
 template <> struct RawOf<int8_t, 8> { typedef Raw8 type; };
 template <typename T, int V> using Raw = typename RawOf<T, V>::type;
 
-// Element `off` bytes beyond an address that is the same for the whole wave: the form that needs one register of address.
-template <typename T> __device__ __forceinline__ T *beyond(T *base, unsigned off) {
+// Element `off` bytes beyond an address that is the same for the whole wave: with `off` in 32 bits, the form that needs one register of address.
+template <typename T, typename Off> __device__ __forceinline__ T *beyond(T *base, Off off) {
     typedef typename std::conditional<std::is_const<T>::value, const char, char>::type byte;
     return reinterpret_cast<T *>(reinterpret_cast<byte *>(base) + off);
 }
