@@ -380,7 +380,8 @@ int gspc_residual_norm(const gspc_residual_t *r, const void *x, int x_dtype, int
  *   xo, h   : from the forward call (xo may be NULL where dz is; x_dtype is dx's type too, h_dtype dh's)
  *   stats   : from the forward call
  *   dx, dh  : dx may be dxo itself, dh may be h itself; dh NULL without h
- *   dgate [gates][cols], dpost_gamma, dpost_beta, dpre_gamma, dpre_beta [cols] : dev fp32, overwritten (zeros where there are no tokens), or NULL
+ *   dgate [gates][cols], dpost_gamma, dpost_beta, dpre_gamma, dpre_beta [cols] : dev fp32, overwritten (zeros where there are no tokens), or NULL; what
+ *   of h was dropped adds nothing to those of the gate and of h's norm, whatever it was
  *   workspace : dev, 16-byte aligned, as large as said; not initialised.  gates: 1 without a gate */
 size_t gspc_residual_norm_backward_workspace_bytes(int64_t rows, int cols, int64_t gates);
 int gspc_residual_norm_backward(const gspc_residual_t *r, const void *dz, int dz_dtype, int64_t lddz, const void *dxo, int64_t lddxo,

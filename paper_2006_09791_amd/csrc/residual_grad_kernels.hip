@@ -186,7 +186,11 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             store_some<ROWS>(static_cast<TX *>(f.dx) + row * f.lddx, at, out, f.past);
         }
         if (f.has_h) {
-            if (a.drop.limit) drop_some(a.drop, call, row, lane, d);
+            Philox which{};
+            if (a.drop.limit) {
+                which = drop_numbers(a.drop, call, row, lane);
+                drop_by(which, a.drop.limit, d);
+            }
             phase();
             if constexpr (LARGE) {
                 if constexpr (GATES) load_h(row);
@@ -197,9 +201,14 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             float2 s = make_float2(0.f, 0.f);
             float q[8];
 #pragma unroll
+            for (int e = 0; e < 8; ++e) hh[e] = fmaf(-st.x, some[e], hh[e]) * st.y;
+            float kept[8];                                      // (what was dropped has no say in the sums, whatever it was: 0 times it need not be 0)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) kept[e] = hh[e];
+            if (a.drop.limit) drop_by(which, a.drop.limit, kept);
+#pragma unroll
             for (int e = 0; e < 8; ++e) {
-                hh[e] = fmaf(-st.x, some[e], hh[e]) * st.y;
-                sa[e] = fmaf(d[e], hh[e], sa[e]);
+                sa[e] = fmaf(d[e], kept[e], sa[e]);
                 sb[e] += d[e];
                 q[e] = gg[e] * d[e];
                 s.x += q[e];
