@@ -350,7 +350,8 @@ int gspc_matmul_f8(const void *a, const uint8_t *a_scale, const void *w, const u
 int gspc_dropout(const void *x, int dtype, int64_t ldx, int64_t rows, int cols, double drop, uint64_t seed, uint64_t offset, const uint64_t *step,
                  void *y, int64_t ldy);
 
-/* Norm over a token's channels: NORM_RMS x / sqrt(mean x^2 + eps), NORM_LAYER (x - mean) / sqrt(var + eps). */
+/* Norm over a token's channels: NORM_RMS x / sqrt(mean x^2 + eps), NORM_LAYER (x - mean) / sqrt(var + eps).  Squares are added up in fp32: where a token's
+ * pass its range (finite values of 2 x 10^17 and more), 1 / sqrt counts as 0, and the norm's result as its offset parameter. */
 enum { GSPC_NORM_NONE = 0, GSPC_NORM_RMS = 1, GSPC_NORM_LAYER = 2 };
 
 /* Between two blocks: u = post_gamma * post(h) + post_beta, x' = scale * x + gate * dropout(u), z = act(pre_gamma * pre(x') + pre_beta): the output h of

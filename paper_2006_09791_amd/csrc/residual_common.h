@@ -72,10 +72,11 @@ template <bool WAVES> __device__ __forceinline__ float team_sum(float v, int tea
     return WAVES && team > kWave ? lanes_sum(team_exchange(make_float2(v, 0.f), team, t).x, 16) : v;
 }
 
-// a / n by the reciprocal, corrected once: exact where the quotient is a number (a constant token's mean is its value).
+// a / n by the reciprocal, corrected once: exact where the quotient is a number (a constant token's mean is its value).  A sum past fp32's range stays
+// infinite (its correction is no number, which the maximum drops), so that 1 / deviation becomes 0.
 __device__ __forceinline__ float ratio(float a, float n) {
     const float r = __builtin_amdgcn_rcpf(n), q = a * r;
-    return fmaf(fmaf(-q, n, a), r, q);
+    return fmaf(fmaxf(fmaf(-q, n, a), -__FLT_MAX__), r, q);
 }
 
 // 1 for a lane's columns that are there, else 0.  A mean is subtracted times it, fmaf(-mean, there, v), so that what is not there stays 0 in every

@@ -154,6 +154,35 @@ def test_offsets_outliers_and_constant_tokens(gpu):
         assert (np.abs(z - xh - host(beta)) <= tol)[keep].all()
 
 
+@pytest.mark.parametrize("C", [7, 24, 60, 512, 1000, 1100, 4100, 8192])
+@pytest.mark.parametrize("kind", [1, 2])
+def test_squares_past_fp32(gpu, C, kind):
+    """Finite tokens whose mean square fp32 does not hold: 1 / deviation is 0, the norm's result its offset parameter, and gradients are numbers.  A constant
+    token as large has no spread all the same."""
+    torch, b = gpu
+    g = torch.Generator(device="cuda").manual_seed(C)
+    x, h = torch.randn(12, C, device="cuda", generator=g), torch.randn(12, C, device="cuda", generator=g)
+    dz, dxo, beta = torch.randn(12, C, device="cuda", generator=g), torch.randn(12, C, device="cuda", generator=g), torch.randn(C, device="cuda", generator=g)
+    gate, gamma = torch.full((C,), 0.5, device="cuda"), torch.full((C,), 1.5, device="cuda")
+    kw = dict(gate=gate, post=kind, post_gamma=gamma, post_beta=beta, pre=kind, pre_gamma=gamma, pre_beta=beta)
+    clean = b.gspc_residual_norm(x, h, **kw)
+    h[3] *= 1e21
+    x[8] *= 1e21
+    x[8, 0] = h[3, 0] = 1e21                            # (one at least, of either norm)
+    stats = torch.empty(12, 4, device="cuda")
+    xo, z = b.gspc_residual_norm(x, h, stats=stats, **kw)
+    keep = [r for r in range(12) if r not in (3, 8)]
+    assert torch.equal(xo[keep], clean[0][keep]) and torch.equal(z[keep], clean[1][keep])
+    assert stats[3, 1] == 0 and stats[8, 3] == 0
+    assert torch.equal(xo[3], x[3] + 0.5 * beta) and torch.equal(z[8], beta)
+    grads = b.gspc_residual_norm_backward(dz, dxo, xo, h, stats, **kw)
+    assert all(bool(t.isfinite().all()) for t in grads)
+    assert torch.equal(grads.dx[8], dxo[8]) and bool((grads.dh[3] == 0).all())
+    x[5] = 2.0 ** 70
+    z = b.gspc_residual_norm(x, pre=kind, pre_beta=beta)[1]
+    assert torch.equal(z[5], beta) and bool(z.isfinite().all())
+
+
 @pytest.mark.parametrize("C", [60, 1024, 4100])
 def test_what_is_not_finite_stays_in_its_token(gpu, C):
     torch, b = gpu
