@@ -425,8 +425,8 @@ static PlanF8 plan_f8(size_t M, int N, int K, bool wide) {
     // 12544 x 512 has 32 tiles: 36.2 whole, 14.3 in eight stretches and their join; 512 x 4096 x 4096 has 128, 15.6 and 22.7 in two.  Stretches of whole
     // words of powers of two (of 28 steps instead of 25) take 1 us more on 1024 x 12544 x 512 to fp32, of 27.
     const size_t count = tiles(p.bm, p.bn);
-    if (count <= 64) {
-        const int want = (int)(256 / count), most = steps / (p.kernel < kTile64 ? 32 : 8), parts = want < most ? want : most;
+    if (count <= 64 && (p.kernel == kSmall1 || p.kernel == kTile64)) {
+        const int want = (int)(256 / count), most = steps / (p.kernel == kSmall1 ? 32 : 8), parts = want < most ? want : most;
         if (parts > 1) {
             p.stretch = (steps + parts - 1) / parts;
             p.parts = (steps + p.stretch - 1) / p.stretch;
@@ -444,8 +444,9 @@ size_t matmul_f8_bytes(size_t M, int N, int K) {        // for either type of ou
     return most;
 }
 
-// (parts of bf16 outputs are fp32, and not wide; large tiles are not wide either: their operands would not fit the registers)
-template <typename T, bool WIDE> static void run_f8(const PlanF8 &plan, ProductF8Args p, size_t M, int N, hipStream_t s, const char **name) {
+// (Parts of bf16 outputs are fp32, and not wide: only the plans that are cut into stretches have that form.  The largest tiles are not wide either: their
+// operands would not fit the registers.)
+template <typename T, bool WIDE> static hipError_t run_f8(const PlanF8 &plan, ProductF8Args p, size_t M, int N, hipStream_t s, const char **name) {
     const auto count = [](size_t all, unsigned of) { return (unsigned)((all - 1) / of + 1); };
     const auto run = [&](auto kern, const char *name_of) {
         *name = name_of;
@@ -462,16 +463,18 @@ template <typename T, bool WIDE> static void run_f8(const PlanF8 &plan, ProductF
                 q.mtiles = count(q.M, bm), q.ntiles = count(q.N, bn), q.tiles = q.mtiles * q.ntiles;
                 hipLaunchKernelGGL(kern, dim3(q.tiles * plan.parts), dim3(plan.threads), 0, s, q);
             }
+        return hipGetLastError();
     };
-    switch (plan.kernel) {
-    case kSmall1: return run(product_f8_small_kernel<T, WIDE, 1, 1, 8, 4>, "product_f8_small<1,1>");
-    case kSmall2: return run(product_f8_small_kernel<T, WIDE, 2, 2, 8, 2>, "product_f8_small<2,2>");
-    case kTile64: return run(product_f8_tile_kernel<T, WIDE, 2, 4, 1, 1, 3>, "product_f8_tile<64,128>");
-    case kTile128Deep: return run(product_f8_tile_kernel<T, WIDE, 2, 4, 2, 1, 4>, "product_f8_tile<128,128>");
-    case kTile128: return run(product_f8_tile_kernel<T, WIDE, 2, 2, 2, 2, 2>, "product_f8_tile<128,128>");
+    if (plan.kernel == kSmall1) return run(product_f8_small_kernel<T, WIDE, 1, 1, 8, 4>, "product_f8_small<1,1>");
+    if (plan.kernel == kTile64) return run(product_f8_tile_kernel<T, WIDE, 2, 4, 1, 1, 3>, "product_f8_tile<64,128>");
+    if constexpr (sizeof(T) == 2 || WIDE) {
+        if (plan.kernel == kSmall2) return run(product_f8_small_kernel<T, WIDE, 2, 2, 8, 2>, "product_f8_small<2,2>");
+        if (plan.kernel == kTile128Deep) return run(product_f8_tile_kernel<T, WIDE, 2, 4, 2, 1, 4>, "product_f8_tile<128,128>");
+        if (plan.kernel == kTile128) return run(product_f8_tile_kernel<T, WIDE, 2, 2, 2, 2, 2>, "product_f8_tile<128,128>");
     }
     if constexpr (sizeof(T) == 2)
-        if (plan.kernel == kTile256) run(product_f8_tile_kernel<T, WIDE, 2, 4, 4, 2, 2>, "product_f8_tile<256,256>");
+        if (plan.kernel == kTile256) return run(product_f8_tile_kernel<T, WIDE, 2, 4, 4, 2, 2>, "product_f8_tile<256,256>");
+    return hipErrorNotSupported;
 }
 
 template <typename T> static hipError_t product(const ProductF8 &in, float *ws, hipStream_t s, const char **name) {
@@ -481,12 +484,9 @@ template <typename T> static hipError_t product(const ProductF8 &in, float *ws, 
     const int past = bytes >= kPastCaches && (bytes < 2 * kPastCaches || whole_pieces(in.out, in.N * sizeof(T), in.ldo * sizeof(T)));
     ProductF8Args p{in.a, in.a_scale, in.w, in.w_scale, in.bias, in.out, in.M, in.ldo, 0, in.N, f8_pitch(in.K), f8_scale_pitch(in.K), plan.stretch,
                     0, 0, 0, past};
-    if (plan.parts == 1) {
-        run_f8<T, WIDE>(plan, p, in.M, in.N, s, name);
-        return hipGetLastError();
-    }
+    if (plan.parts == 1) return run_f8<T, WIDE>(plan, p, in.M, in.N, s, name);
     p.bias = nullptr, p.out = ws, p.ldo = in.N, p.part = in.M * in.N, p.past = 0;
-    run_f8<float, WIDE>(plan, p, in.M, in.N, s, name);
+    if (const hipError_t e = run_f8<float, WIDE>(plan, p, in.M, in.N, s, name)) return e;
     const unsigned nv = (in.N + 3) / 4, vectors = (unsigned)(in.M * nv);        // (below 256 tiles of at most 2^16 values)
     hipLaunchKernelGGL(product_f8_join_kernel<T>, dim3((vectors + 255) / 256), dim3(256), 0, s, ws, p.part, (unsigned)plan.parts, vectors, in.N, nv,
                        div_magic(nv), in.bias, static_cast<T *>(in.out), in.ldo);
