@@ -1,6 +1,8 @@
 """Kernels of a residual block's operators without a GPU: calls reach each form that is compiled, and no other is."""
 import itertools
 
+import pytest
+
 from paper_2006_09791_amd import binding as b
 from test_block_launches import BASE, OUT, SC, ST, WS, launches
 from test_block_resources import OPERATORS
@@ -54,3 +56,22 @@ def test_every_kernel_is_reached(runtime):  # noqa: F811
     names = reached(runtime, calls)
     compiled = {n for n in kernels() if any(f"{len(op)}{op}{end}" in n for op in OPERATORS for end in "IE")}
     assert compiled - names == set() and names <= compiled
+
+
+@pytest.mark.parametrize("cols", [1, 31, 32, 33, 64, 200, 1000, 8192])
+def test_parameters_sums_reach_every_column_once(runtime, cols):  # noqa: F811
+    """A block of the join has 32 columns (kJoinCols), 1024 threads of them."""
+    calls = list(residual(5000, cols, 4, 1, 1, False))[1:]
+    (rc, found), = launches(runtime, calls, {"residual_join_kernel": [(4, 4)]})
+    (blocks, threads, slabs), = [(n, threads, int.from_bytes(a[0], "little")) for k, n, threads, a in found if k == "residual_join_kernel"]
+    assert rc == 0 and threads == 1024 and (slabs - 1) * 32 < cols <= slabs * 32 and blocks % slabs == 0
+
+
+@pytest.mark.parametrize("M,K,N,waves", [(1000, 2000, 3000, 8), (2048, 512, 4096, 4)])
+def test_tiles_of_128_in_four_and_eight_waves(runtime, M, K, N, waves):  # noqa: F811
+    """Two forms that report one name: eight waves and four stages where a compute unit has one block."""
+    for dtype in (0, 1):
+        (rc, found), = launches(runtime, [product(M, K, N, dtype)], ARGUMENTS)
+        (kernel, blocks, threads, (name,)), = found
+        form = b"Li2ELi4ELi2ELi1ELi4E" if waves == 8 else b"Li2ELi2ELi2ELi2ELi2E"
+        assert rc == 0 and kernel == "product_f8_tile_kernel" and form in name and threads == 64 * waves and blocks == -(-M // 128) * -(-N // 128)
