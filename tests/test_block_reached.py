@@ -75,3 +75,14 @@ def test_tiles_of_128_in_four_and_eight_waves(runtime, M, K, N, waves):  # noqa:
         (kernel, blocks, threads, (name,)), = found
         form = b"Li2ELi4ELi2ELi1ELi4E" if waves == 8 else b"Li2ELi2ELi2ELi2ELi2E"
         assert rc == 0 and kernel == "product_f8_tile_kernel" and form in name and threads == 64 * waves and blocks == -(-M // 128) * -(-N // 128)
+
+
+@pytest.mark.parametrize("C,waves_of_a_team", [(264, 1), (320, 1), (512, 1), (520, 2), (640, 2), (1000, 2)])
+def test_waves_of_the_gradient_go_by_tokens_of_a_team(runtime, C, waves_of_a_team):  # noqa: F811
+    """Teams of one or two waves, four waves a block: twelve waves a compute unit from 8 tokens a team on, eight below, at any width."""
+    full = 256 * 12 // waves_of_a_team          # teams
+    for tokens, most in ((8 * full - 1, 8), (8 * full, 12), (11 * full + 77, 12), (40 * full, 12)):
+        calls = list(residual(tokens, C, 1, 1, 1, False))[1:]
+        (rc, found), = launches(runtime, calls, ARGUMENTS)
+        (blocks, threads), = [(n, threads) for k, n, threads, _ in found if k == "residual_grad_kernel"]
+        assert rc == 0 and threads == 256 and 0.9 * 256 * most < blocks * 4 <= 256 * most, (tokens, blocks)
