@@ -202,13 +202,21 @@ __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad
             float q[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) hh[e] = fmaf(-st.x, some[e], hh[e]) * st.y;
-            float kept[8];                                      // (what was dropped has no say in the sums, whatever it was: 0 times it need not be 0)
+            // What was dropped has no say in the sums, whatever it was: 0 times it need not be 0.  Behind a norm that is all of a token or nothing of it, as
+            // 1 / deviation tells (never 0 of numbers but where squares pass fp32); the selection for each token cost 4 us of 91 on 8192 x 4096.
+            if (a.drop.limit && (a.post == kNormNone || !(st.y > 0.f && st.y < __builtin_inff()))) {
+                float kept[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) kept[e] = hh[e];
-            if (a.drop.limit) drop_by(which, a.drop.limit, kept);
+                for (int e = 0; e < 8; ++e) kept[e] = hh[e];
+                drop_by(which, a.drop.limit, kept);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sa[e] = fmaf(d[e], kept[e], sa[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sa[e] = fmaf(d[e], hh[e], sa[e]);
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sa[e] = fmaf(d[e], kept[e], sa[e]);
                 sb[e] += d[e];
                 q[e] = gg[e] * d[e];
                 s.x += q[e];
