@@ -326,14 +326,16 @@ int gspc_f8_scale_pitch(int cols);
  * smallest from 2^-127 on that brings the largest finite magnitude to 448 at most (2^-127 where all are 0); values are rounded to nearest,
  * ties to even; infinities and NaN become NaN, in their places, and have no say in the power of two. */
 int gspc_quantize_rows_f8(const void *x, int dtype, int64_t ldx, int64_t rows, int cols, void *q, uint8_t *scale, void *qt, uint8_t *scale_t);
-/* Reads rows back (in bf16 exactly, down to its smallest normal number). */
+/* Reads rows back (in bf16 exactly, down to its smallest normal number; 2^128 and more as an infinity). */
 int gspc_dequantize_rows_f8(const void *q, const uint8_t *scale, int64_t rows, int cols, void *x, int dtype, int64_t ldx);
 
 /* out[m][n] = sum over k < K of a[m][k] w[n][k] (+ bias[n]), a [M] and w [N] 8-bit float rows of K values, K at most 2^22.  The gradients of
- * y = x w^T are the same product: dx of dy's rows and w's columns form, dw of dy's and x's columns forms.
+ * y = x w^T are the same product: dx of dy's rows and w's columns form, dw of dy's and x's columns forms.  (A bias' gradient, dy's sum over tokens, is the
+ * caller's.)
  * fp32 outputs: products are exact and sums keep 24 bits.  bf16 outputs: eight products at a time are added with no bit below 2^-13 of the largest
- * one's exponent, which is below 2^-10 of sum |a w| and about 2^-16 of a result on random values; then one rounding.  Blocks whose
- * power of two is 2^-118 or less lose bits to fp32 outputs (their values are bf16 numbers, in steps of 2^-133).
+ * one's exponent, which is below 2^-10 of sum |a w| and about 2^-16 of a result on random values; then one rounding.  To fp32 outputs, values are bf16
+ * numbers: in steps of 2^-133 (blocks whose power of two is 2^-125 or less lose bits), and infinite from 2^128 on (what finite numbers of 3.3 x 10^38 and
+ * more are rounded to).
  *   bias      : dev fp32 [N], or NULL
  *   out       : dense rows, fp32 or bf16 (out_dtype, ldo)
  *   workspace : dev, 16-byte aligned, as large as said (0: none is needed): parts of long sums of few outputs; not initialised */

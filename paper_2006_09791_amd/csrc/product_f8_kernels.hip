@@ -4,7 +4,8 @@
 // over all blocks stays in their fp32 accumulators and scaling costs no instruction.  These instructions add eight products at a time with no bit below
 // 2^-13 of the largest one's exponent (in e4m3 all do, the scaled ones and the older ones alike), each cut off there: less than 2^-10 of sum |a w|, and
 // 1.5e-5 of the result on random values, a hundredth of its rounding to bf16.  For fp32 outputs that is too much.  There the operands are widened to bf16
-// with their power of two (exact: four significant bits) and multiplied by the bf16 instructions, whose sums keep 24 bits (5e-9 on random values); the
+// with their power of two (exact: four significant bits, in steps of 2^-133 and below 2^128) and multiplied by the bf16 instructions, whose sums keep 24 bits
+// (5e-9 on random values); the
 // peak is half of that (loops in registers: 3.7 PFLOP/s and, with the widening, 1.46).
 #include "float8.h"
 #include "product_common.h"

@@ -197,6 +197,37 @@ def test_powers_of_two_at_the_ends_of_their_range(gpu, M, K, N):
         check_product(host(b.gspc_matmul_f8(a, w, dtype=kind)), values(torch, a), values(torch, w), None, K, kind == b.GSPC_BF16)
 
 
+@pytest.mark.parametrize("M,N", [(2, 126), (300, 520), (2048, 4096)])
+@pytest.mark.parametrize("power", [-127, -126, -125, -124, -118, -60, 0, 118])
+def test_every_code_at_the_ends_of_the_range(gpu, M, N, power):
+    """All positive codes times powers of two, one a filter: to fp32 exact in blocks of 2^-124 and more, and below within half of 2^-133."""
+    torch, b = gpu
+    codes = torch.zeros(128)
+    codes[:126] = torch.arange(1, 127).to(torch.uint8).view(torch.float8_e4m3fn).float()
+    x = (codes.double() * 2.0 ** power).float().cuda().repeat(M, 1)
+    other = 100 if power < 0 else -100
+    w = torch.zeros(N, 128)
+    w[torch.arange(126), torch.arange(126)] = 2.0 ** other
+    a = b.gspc_quantize_rows_f8(x)
+    assert bool((a[1][:, 0] == power + 127).all()) and torch.equal(a[0][0].float().cpu(), codes)
+    want = codes[:126].double() * 2.0 ** (power + other)
+    out = b.gspc_matmul_f8(a, b.gspc_quantize_rows_f8(w.cuda()), dtype=b.GSPC_F32)
+    assert bool((out == out[:1]).all()) and not bool(out[:, 126:].any())
+    off = (out[0, :126].cpu().double() - want).abs().max().item()
+    assert off <= (2.0 ** (-134 + other) if power < -124 else 0)
+    assert torch.equal(b.gspc_matmul_f8(a, b.gspc_quantize_rows_f8(w.cuda()))[0, :126].cpu(), want.bfloat16())
+
+
+def test_values_past_the_largest_number(gpu):
+    """What 3.4 x 10^38 is rounded to is 2^128: a number to bf16 outputs, and an infinity to fp32 outputs and to what reads it."""
+    torch, b = gpu
+    a = b.gspc_quantize_rows_f8(torch.full((2, 128), 3.4e38, device="cuda"))
+    w = b.gspc_quantize_rows_f8(torch.full((40, 128), 2.0 ** -100, device="cuda"))
+    assert bool((b.gspc_matmul_f8(a, w) == 2.0 ** 35).all()) and bool((b.gspc_matmul_f8(a, w, dtype=b.GSPC_F32) == float("inf")).all())
+    for dtype in (b.GSPC_F32, b.GSPC_BF16):
+        assert bool((b.gspc_dequantize_rows_f8(a, 128, dtype=dtype) == float("inf")).all())
+
+
 @pytest.mark.parametrize("M,K,N", [(3, 200, 40), (300, 640, 520), (2048, 256, 4096)])
 def test_what_is_not_finite_stays_in_its_outputs(gpu, M, K, N):
     torch, b = gpu
