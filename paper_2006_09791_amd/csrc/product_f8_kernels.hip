@@ -177,9 +177,11 @@ __global__ __launch_bounds__(64 * WAVES) void product_f8_small_kernel(ProductF8A
 // such pieces; which columns of the block they are does not matter as long as both operands agree.
 //
 // Bound by the matrix instructions where there is enough work: 8192 x 4096 x 8192 to bf16 in 256 x 256 takes 219 us (2.5 PFLOP/s; the
-// library's product without scales 216).  WIDE by the widening, sixteen clocks for 128 values, which each wave does for all of its operands: a step of 32 x 32
-// in a wave (64 x 128) takes 1024 clocks of it and 256 of products, one of 64 x 64 (128 x 128) 2048 and 1024 (8192 x 4096 x 8192 to fp32 in 128 x 128:
-// 461 us, 1.19 PFLOP/s; 1024 x 12544 x 512 in 64 x 128 and four stretches: 23 and a join of 4).
+// library's product without scales 216).  WIDE: each wave widens all of its operands, four clocks for 128 values (loops in registers, two waves a SIMD:
+// 32 such instructions 58 ns, exclusive ors 37; with 8 products that do not wait for them 160, where these alone take 147: they go side by side).  A step
+// of 64 x 64 in a wave (128 x 128) has 512 clocks of them and 1024 of products, and these bound it (8192 x 4096 x 8192 to fp32: 461 us, 1.19 PFLOP/s); one of 32 x 32
+// (64 x 128) 256 of either, and with loads and a barrier a step neither bounds it (1024 x 12544 x 512 in four stretches, 23.9 us and a join of 4.8: matrix
+// instructions at work 29 % of the time, vector instructions half of it; a wave waits 37 % of its time for loads and its block, 25 % for its turn).
 template <typename T, bool WIDE, int WM, int WN, int TM, int TN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void product_f8_tile_kernel(ProductF8Args p) {
     constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, ROWS = BM + BN, LOADS = ROWS / 8 / WAVES;

@@ -17,10 +17,10 @@ struct GradPlan {
 };
 
 // A team walks down its tokens and keeps the sums of its columns; a block's teams add theirs up and leave one part.  dz, dx', x' and h in, dx and dh out:
-// bound by memory and, nearly as much, by vector instructions (50176 x 512 in bf16, two norms, dropout and SiLU, 309 MB: 65.4 us, 4.7 TB/s; 460
+// bound by memory and, nearly as much, by vector instructions (50176 x 512 in bf16, two norms, dropout and SiLU, 309 MB: 66.5 us, 4.6 TB/s; 480
 // instructions for a wave's 512 values).  GATES: a team's tokens have several gates, whose gradients it writes itself.  LARGE: teams of
-// more than 512 lanes, which leave 128 registers each: parameters are in LDS, and no token is ahead (4096 x 8192, 403 MB: 108 us, and 134 with
-// parameters read again for each token; 8192 x 4096, as many bytes, 89).
+// more than 512 lanes, which leave 128 registers each: parameters are in LDS, and no token is ahead (4096 x 8192, 403 MB, with
+// the join: 113 us; with parameters read again for each token a quarter more; 8192 x 4096, as many bytes, 93).
 template <typename TX, typename TH, bool GATES, bool LARGE, Rows ROWS, bool WAVES>
 __global__ __launch_bounds__(LARGE ? kMaxTeam : kMaxTeam / 2) void residual_grad_kernel(Residual a, ResidualBackward f, GradPlan g, int of_team, unsigned m_chunks,
                                                                  float *__restrict__ parts) {

@@ -6,7 +6,7 @@ namespace gspc {
 
 // A team keeps its parameters and walks down consecutive tokens; the next token's values are on their way while this one's are worked on.  x and h in, x'
 // and z out: bound by memory without an h (50176 x 512 in bf16, 103 MB: 18 us, 5.7 TB/s), by vector instructions nearly as much with two
-// norms, dropout and SiLU (206 MB: 49.5 us, 4.2 TB/s; 340 instructions for a wave's 512 values, three quarters of the time).  H: there is an h.
+// norms, dropout and SiLU (206 MB: 50.2 us, 4.1 TB/s; 357 instructions for a wave's 512 values, three quarters of the time).  H: there is an h.
 template <typename TX, typename TH, bool H, Rows ROWS, bool WAVES>
 __global__ __launch_bounds__(WAVES ? kMaxTeam : kTeamThreads) void residual_norm_kernel(Residual a, ResidualForward f, int team, unsigned each, unsigned m_gate) {
     __shared__ float2 s_place[2][kMaxTeam / kWave];
