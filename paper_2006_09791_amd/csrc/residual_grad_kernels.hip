@@ -317,7 +317,8 @@ static_assert(kTeamThreads == 4 * kWave, "a block's teams are in one, two or fou
 // As many blocks as are at work at once: of 1024 lanes one a compute unit, of fewer eight waves.  (Twelve, which the registers would hold, have half
 // as many parts again to add up, and leave 1.5 blocks of 512 lanes for each compute unit: 12544 x 512 in bf16, layer norms, SiLU and dropout, with 4, 8, 12
 // and 16: 28.9, 25.0, 26.2, 32.5 us; 2000 x 4096: 46.4, 31.5, 43.8, 39.6.  Of 1024 lanes, 4096 x 8192, 8, 16 and 32: 234, 134, 144.)  Twelve all
-// the same where teams of one or two waves have 8 tokens each or more, with 8 waves and 12, behind the forward call: 24576 x 320 in bf16 56.7 and 54.4, 43008 x
+// the same where teams of one or two waves have 8 tokens each or more (faster at 52 of 70 sizes of 320 to 1024 channels, by 2.3 % in the mean of all), with 8
+// waves and 12, behind the forward call: 24576 x 320 in bf16 56.7 and 54.4, 43008 x
 // 320 90.8 and 84.5, 12288 x 640 62.5 and 59.4, 49152 x 640 207 and 190; where channels fill the team, 24576 x 512 63.6 and 62.2, 36864 x 512 88.6 and 90.7, 49152
 // x 512 116 and 112, 15360 x 1024 83.5 and 81.8, 24576 x 1024 119 and 111, 24576 x 512 in fp32 115.5 and 114.8; with fewer tokens, 12288 x 512 38.2 and 39.3, 6144 x
 // 1024 without dropout 33.0 and 34.3.  Teams of 32 or 256 lanes, 100352 x 256 and 20000 x 2048: 71.8 and 75.2, 110 and 115.
